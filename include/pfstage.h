@@ -262,7 +262,7 @@ pf_status pf_stage_profile_read(pf_stage *stage, double *ms, int64_t *launches);
 
 void pf_stage_destroy(pf_stage *stage); /* NULL-safe */
 const char *pf_status_str(pf_status s);
-const char *pf_last_error(const pf_stage *stage); /* "" if none; NULL stage: last creation error */
+const char *pf_last_error(const pf_stage *stage); /* "" if none; NULL stage: last error of a call without one on this thread */
 
 /* ------------------------------------------------------------------------------------------------
  * Single-operator entry points: the kernels of the path, callable on their own for unit parity tests
@@ -394,6 +394,140 @@ int pf_gemm_tile_map(int M, int N, int tile_m, int tile_n, unsigned workgroup, u
 /* Host-only, for tests: the workgroups that a wave-split-K launch on an M x N output and K has behind those of its 64x64 tiles, to read
  * operand rows into the L2s ahead of them.  A multiple of 8; 0 where the launch goes without. */
 int pf_gemm_read_ahead(int M, int N, int K);
+
+/* ------------------------------------------------------------------------------------------------
+ * Operators on packed rows: requests of different sizes in one call.
+ *
+ * The rows of all sequences (images of several resolutions, prompts) stand behind each other; cu[s] .. cu[s + 1] are those
+ * of sequence s (int32 [n_seqs + 1], device, non-decreasing).  Rows outside [cu[0], cu[n_seqs]) belong to no sequence and what
+ * an operator would write for them is left as it is.  Lengths, positions and page tables are device memory that the host
+ * does not read: the calls can be captured into a graph and replayed with other contents.  Every value read from them is
+ * bounded before it is used, so wrong ones give wrong rows and no access outside the arrays.
+ * The conventions above hold here too: nothing is allocated, nothing synchronises, errors of arguments are found before
+ * anything is launched.  Calls with no rows or no sequences do nothing and may pass NULL pointers.  Outputs may not overlap inputs
+ * except where it is said.  pf_last_error(NULL) says what was wrong.
+ * ---------------------------------------------------------------------------------------------- */
+
+/*
+ * Rotary positions.  Each of 1 to 3 position axes (time, row, column; one for text) turns axis_dim[a] channels of a head,
+ * one axis behind the other from channel 0 on; channels behind the last axis pass unchanged.  Pair i of an axis of width w
+ * turns by pos * f_i radians, f_i = theta^(-2i/w): (a, b) -> magnitude * (a cos - b sin, a sin + b cos).  The pair is
+ * channels (2i, 2i + 1) of the axis (interleaved) or (i, i + w/2) (half).  For contexts longer than the model was
+ * trained on the frequencies are changed:
+ *   LINEAR      f_i / factor.
+ *   NTK         theta replaced by theta * factor^(w / (w - 2)) (w > 2): the slowest pair ends up divided by `factor`.
+ *   RAMP_TURNS  pairs that make `high` or more turns over original_len positions keep f_i, those that make `low` or fewer
+ *               get f_i / factor, and between them the two are mixed linearly in the number of turns.
+ *   RAMP_INDEX  the same two ends, mixed linearly in i between the pair indexes (rounded outwards, inside [0, w - 1]) at
+ *               which a pair makes `high` and `low` turns.
+ * `factor` >= 1, high > low > 0, original_len >= 1 are read only where the scaling uses them.
+ */
+#define PF_ROPE_MAX_AXES 3
+#define PF_ROPE_MAX_PAIRS 64
+typedef enum { PF_ROPE_INTERLEAVED = 0, PF_ROPE_HALF = 1 } pf_rope_layout;
+typedef enum {
+  PF_ROPE_SCALE_NONE = 0, PF_ROPE_SCALE_LINEAR = 1, PF_ROPE_SCALE_NTK = 2, PF_ROPE_SCALE_RAMP_TURNS = 3,
+  PF_ROPE_SCALE_RAMP_INDEX = 4
+} pf_rope_scaling;
+typedef struct {
+  int32_t layout;                      /* pf_rope_layout */
+  int32_t n_axes;                      /* 1 .. 3 */
+  int32_t axis_dim[PF_ROPE_MAX_AXES];  /* even, >= 2; the sum is at most 128 */
+  float theta;                         /* > 1 */
+  int32_t scaling;                     /* pf_rope_scaling */
+  float factor, low, high;
+  int32_t original_len;
+  float magnitude;                     /* > 0, finite; 1 for plain rotation */
+} pf_rope_config;
+
+/* A rotation ready for use (host memory, plain data, may be copied): pair p of the head turns by pos * turns[p] turns. */
+typedef struct {
+  int32_t layout, n_axes;
+  int32_t axis_dim[PF_ROPE_MAX_AXES];
+  float magnitude;
+  double turns[PF_ROPE_MAX_PAIRS];
+} pf_rope;
+pf_status pf_rope_init(const pf_rope_config *cfg, pf_rope *out);   /* host only */
+
+/* Turns every head of x: x and out dtype [tokens, n_heads * head_dim] with row strides ldx, ldo; out may be x itself (then
+ * ldo = ldx).  pos int32 [tokens, n_axes], any value.  head_dim a multiple of 8, at most 128, and at least the sum of the axes;
+ * pointers 16-byte aligned, row strides multiples of 16 bytes. */
+pf_status pf_op_rope(int dtype, const pf_rope *rope, const int32_t *pos, const void *x, int64_t ldx, void *out, int64_t ldo,
+                     int tokens, int n_heads, int head_dim, void *stream);
+
+/*
+ * Keys and values in pages.  Page p of k holds [kv_heads][page_size][head_dim] elements from k + p * k_page_stride on,
+ * likewise v.  Slot t of sequence s lives in row t % page_size of page table[s * max_pages + t / page_size].  Entries of the
+ * table outside [0, n_pages) mean "no page": rows written there are dropped, keys there are not attended to.
+ */
+typedef struct {
+  void *k, *v;                             /* dtype, 16-byte aligned */
+  int64_t k_page_stride, v_page_stride;    /* elements; at least kv_heads * page_size * head_dim, multiples of 16 bytes */
+  const int32_t *table;                    /* device [n_seqs][max_pages] */
+  int32_t n_pages, page_size;              /* page_size: a power of two, 16 .. 1024 */
+  int32_t kv_heads, head_dim;              /* head_dim: a multiple of 8, at most 128 */
+  int32_t n_seqs, max_pages;
+} pf_kv_pages;
+
+/*
+ * Writes new rows of k and v (dtype [tokens, kv_heads * head_dim], row strides ldk, ldv) into the pages: row cu[s] + i goes to slot
+ * first[s] + i of sequence s - the end of a prompt, or a patch in the middle of a sequence whose other rows stay a step
+ * old.  rope != NULL: k is turned on the way (pos as in pf_op_rope), and so is q [tokens, n_heads * head_dim], which goes to q_out
+ * (may be q itself).  rope == NULL: q, if there is one, is copied.  q == NULL: n_heads must be 0.  Slots past max_pages *
+ * page_size, and negative ones, are dropped.  Two rows for one slot leave either.
+ */
+pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                          const int32_t *cu, const int32_t *first, int tokens, const pf_rope *rope, const int32_t *pos,
+                          const void *q, int64_t ldq, void *q_out, int64_t ldqo, int n_heads, void *stream);
+
+/*
+ * Attention of packed sequences: row i of sequence s, head h attends to that sequence's keys of head h * kv_heads / n_heads:
+ *   out = sum_j softmax_j(scale * q . k_j) v_j      (scale <= 0: 1 / sqrt(head_dim))
+ * q, out dtype [total_q, n_heads * head_dim]; k, v dtype [total_k, kv_heads * head_dim]; n_heads a multiple of kv_heads.
+ * cu_q, cu_k: the rows of each sequence among the queries and among the keys; they need not be alike.  causal != 0: query i
+ * of n_q sees the keys j <= i + n_k - n_q, so the last query sees all.  A row that sees no key gives zeros.
+ * lse != NULL: float [total_q, n_heads] receives log sum_j exp(scale * q . k_j) (-inf for a row that sees none), with which parts of a
+ * sequence can be joined.  Scores, softmax and sums are in 32 bits; for bf16 the weights are rounded to bf16 for the second product.
+ * Values of keys past the end of a sequence are not read; values that only the causal mask hides take part with weight zero.
+ * ws: pf_op_attention_rows_ws_bytes(.., max_kv = total_k) bytes (may be NULL if that is 0); calls that may run at the same
+ * time need one each.
+ */
+size_t pf_op_attention_rows_ws_bytes(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim,
+                                     int64_t max_kv);
+pf_status pf_op_attention_packed(int dtype, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                                 const int32_t *cu_q, const int32_t *cu_k, int n_seqs, int total_q, int total_k, int n_heads,
+                                 int kv_heads, int head_dim, float scale, int causal, void *out, int64_t ldo, float *lse, void *ws,
+                                 size_t ws_bytes, void *stream);
+
+/*
+ * The same over keys in pages: the rows cu_q[s] .. cu_q[s + 1] are new tokens (a patch, part of a prompt, one token) of sequence
+ * s whose row i sits in slot first[s] + i, and they attend to slots [0, kv_len[s]) - causal: to those up to first[s] + i.
+ * first (may be NULL when not causal) and kv_len int32 [n_seqs].  The workspace: max_kv = max_pages * page_size.
+ */
+pf_status pf_op_attention_paged(int dtype, const void *q, int64_t ldq, const pf_kv_pages *pages, const int32_t *cu_q,
+                                const int32_t *first, const int32_t *kv_len, int total_q, int n_heads, float scale, int causal,
+                                void *out, int64_t ldo, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The rows between two branches of a block:
+ *   x_out = x_scale * x + g(gate) * post(y)        h = pre(x_out) * (1 + scale) + shift
+ * x, x_out float [rows, d] (the residual stream), y (the branch's output) and h (the next branch's input) dtype [rows, d].  post and
+ * pre: norms over a row (NULL or kind NONE: none) with weight and bias dtype [d], either NULL; RMS: y / sqrt(mean y^2 + eps),
+ * LAYER: the same of y - mean y.  gate float, g the identity or tanh (gate_tanh); NULL: 1.  scale, shift float, either NULL.
+ * cu == NULL: one gate / scale / shift [d] for all rows; else sequence s uses gate + s * gate_stride and scale / shift + s *
+ * mod_stride.  y == NULL: no branch (x_out = x_scale * x).  x_out or h may be NULL if not wanted.  x_out may be x, h may be y.
+ * d a multiple of 8, at most 8192; pointers 16-byte aligned (y, h, weights of bf16: 8), strides multiples of 4 elements.
+ */
+typedef enum { PF_NORM_NONE = 0, PF_NORM_RMS = 1, PF_NORM_LAYER = 2 } pf_norm_kind;
+typedef struct {
+  int32_t kind;   /* pf_norm_kind */
+  float eps;      /* >= 0 */
+  const void *weight, *bias;
+} pf_norm;
+pf_status pf_op_norm_residual(int dtype, const void *y, int64_t ldy, const pf_norm *post, const float *gate, int64_t gate_stride,
+                              int gate_tanh, float x_scale, const float *x, int64_t ldx, float *x_out, int64_t ldxo,
+                              const pf_norm *pre, const float *shift, const float *scale, int64_t mod_stride, void *h,
+                              int64_t ldh, const int32_t *cu, int n_seqs, int rows, int d, void *stream);
 
 #ifdef __cplusplus
 }

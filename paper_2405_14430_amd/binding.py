@@ -55,7 +55,36 @@ EXPORTS = ["pf_stage_kv_bytes", "pf_stage_workspace_bytes", "pf_stage_create", "
            "pf_stage_profile",
            "pf_stage_profile_read", "pf_stage_destroy", "pf_status_str", "pf_last_error", "pf_op_modulation",
            "pf_op_ln_modulate", "pf_op_gemm", "pf_op_kv_scatter", "pf_op_attention_ws_bytes", "pf_op_attention", "pf_attention_kernel_name", "pf_probe_mfma_loop",
-           "pf_gemm_tile_count", "pf_gemm_tile_map", "pf_gemm_read_ahead", "pf_op_gemm_tile", "pf_static_scratch_bytes", "pf_op_attention_static", "pf_gemm_kernel_name", "pf_gemm_qkv_kernel_name", "pf_op_axpy", "pf_kv_view_image", "pf_op_axpby"]
+           "pf_gemm_tile_count", "pf_gemm_tile_map", "pf_gemm_read_ahead", "pf_op_gemm_tile", "pf_static_scratch_bytes", "pf_op_attention_static", "pf_gemm_kernel_name", "pf_gemm_qkv_kernel_name", "pf_op_axpy", "pf_kv_view_image", "pf_op_axpby",
+           "pf_rope_init", "pf_op_rope", "pf_op_kv_append", "pf_op_attention_rows_ws_bytes", "pf_op_attention_packed",
+           "pf_op_attention_paged", "pf_op_norm_residual"]
+
+PF_ROPE_MAX_AXES, PF_ROPE_MAX_PAIRS = 3, 64
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp_turns": 3, "ramp_index": 4}
+NORM_KINDS = {"none": 0, "rms": 1, "layer": 2}
+
+
+class PfRopeConfig(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("n_axes", C.c_int32), ("axis_dim", C.c_int32 * PF_ROPE_MAX_AXES), ("theta", C.c_float),
+                ("scaling", C.c_int32), ("factor", C.c_float), ("low", C.c_float), ("high", C.c_float),
+                ("original_len", C.c_int32), ("magnitude", C.c_float)]
+
+
+class PfRope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("n_axes", C.c_int32), ("axis_dim", C.c_int32 * PF_ROPE_MAX_AXES),
+                ("magnitude", C.c_float), ("turns", C.c_double * PF_ROPE_MAX_PAIRS)]
+
+
+class PfKvPages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_page_stride", C.c_int64), ("v_page_stride", C.c_int64),
+                ("table", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class PfNorm(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
 
 _lib = None
 
@@ -139,6 +168,24 @@ def load_library():
     lib.pf_gemm_read_ahead.argtypes = [i32, i32, i32]
     lib.pf_op_gemm_tile.restype = i32
     lib.pf_op_gemm_tile.argtypes = [i32] + lib.pf_op_gemm.argtypes
+    lib.pf_rope_init.restype = i32
+    lib.pf_rope_init.argtypes = [C.POINTER(PfRopeConfig), C.POINTER(PfRope)]
+    lib.pf_op_rope.restype = i32
+    lib.pf_op_rope.argtypes = [i32, C.POINTER(PfRope), vp, vp, i64, vp, i64, i32, i32, i32, vp]
+    lib.pf_op_kv_append.restype = i32
+    lib.pf_op_kv_append.argtypes = [i32, C.POINTER(PfKvPages), vp, i64, vp, i64, vp, vp, i32, C.POINTER(PfRope), vp, vp, i64,
+                                    vp, i64, i32, vp]
+    lib.pf_op_attention_rows_ws_bytes.restype = sz
+    lib.pf_op_attention_rows_ws_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i64]
+    lib.pf_op_attention_packed.restype = i32
+    lib.pf_op_attention_packed.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, i32, i32, f32, i32, vp,
+                                           i64, vp, vp, sz, vp]
+    lib.pf_op_attention_paged.restype = i32
+    lib.pf_op_attention_paged.argtypes = [i32, vp, i64, C.POINTER(PfKvPages), vp, vp, vp, i32, i32, f32, i32, vp, i64, vp, vp,
+                                          sz, vp]
+    lib.pf_op_norm_residual.restype = i32
+    lib.pf_op_norm_residual.argtypes = [i32, vp, i64, C.POINTER(PfNorm), vp, i64, i32, f32, vp, i64, vp, i64, C.POINTER(PfNorm),
+                                        vp, vp, i64, vp, i64, vp, i32, i32, i32, vp]
     _lib = lib
     return lib
 
@@ -394,3 +441,304 @@ def pf_op_axpby(x, y, a, b, out=None):
     out = torch.empty_like(x) if out is None else out
     _ok(lib.pf_op_axpby(_ptr(x), _ptr(y), float(a), float(b), _ptr(out), x.numel(), _stream_ptr()))
     return out
+
+
+# ---- operators on packed rows: requests of different sizes in one call -----------------------------------------------------
+# Rows of all sequences stand behind each other, cu [n_seqs + 1] (int32, device) says where each one's begin.  Tensors have to
+# be on one GPU; the work goes to that GPU's current stream.
+_DT = {torch.float32: PF_F32, torch.bfloat16: PF_BF16}
+
+
+def _raise(st):
+    raise PfError(st, load_library().pf_last_error(None).decode())
+
+
+def _rows(name, t, dtype=None, device=None):
+    """A 2-d tensor of rows as the kernels read them: any row stride, channels next to each other."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise PfError(-3, f"{name}: rows of contiguous channels are needed, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return _plain(name, t, dtype, device)
+
+
+def _plain(name, t, dtype=None, device=None):
+    if not t.is_cuda:
+        raise PfError(-3, f"{name}: is on {t.device}, a GPU tensor is needed")
+    if device is not None and t.device != device:
+        raise PfError(-3, f"{name}: is on {t.device}, the call's other tensors on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise PfError(-4, f"{name}: is {t.dtype}, {dtype} is needed")
+    if t.dtype not in _DT and dtype is None:
+        raise PfError(-4, f"{name}: {t.dtype} is neither float32 nor bfloat16")
+    return t
+
+
+def _ints(name, t, shape, device):
+    """An int32 tensor of lengths, positions or pages, contiguous and of the given shape."""
+    _plain(name, t, torch.int32, device)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise PfError(-3, f"{name}: shape {tuple(t.shape)}, a contiguous {tuple(shape)} is needed")
+    return t
+
+
+def _vectors(name, t, d, n_seqs, device):
+    """float [d], or [n_seqs, d] for a call with sequences; returns the stride between sequences."""
+    if t is None:
+        return 0
+    _plain(name, t, torch.float32, device)
+    shape = (d,) if n_seqs is None else (n_seqs, d)
+    if tuple(t.shape) != shape or (d > 1 and t.stride(-1) != 1):
+        raise PfError(-3, f"{name}: shape {tuple(t.shape)}, {shape} is needed")
+    return 0 if n_seqs in (None, 1) else t.stride(0)
+
+
+def _ld(t):
+    # the stride of a single row (or of none) may be anything: rows are then as far apart as they are wide
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 8)
+
+
+class _on:
+    """Makes a tensor's GPU the current one for a launch."""
+    __slots__ = ("index", "before")
+
+    def __init__(self, device):
+        self.index = device.index
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+        return C.c_void_p(torch.cuda.current_stream(self.index).cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def make_rope(axis_dims, layout="interleaved", theta=1e4, scaling="none", factor=1.0, low=1.0, high=32.0, original_len=1,
+              magnitude=1.0):
+    """A rotation for pf_op_rope / pf_op_kv_append (pf_rope_init): made once, used by every call."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        raise PfError(-2, f"rope: layout {layout!r}, scaling {scaling!r}")
+    dims = [int(w) for w in axis_dims]
+    c = PfRopeConfig(layout=ROPE_LAYOUTS[layout], n_axes=len(dims), theta=theta, scaling=ROPE_SCALINGS[scaling], factor=factor,
+                     low=low, high=high, original_len=original_len, magnitude=magnitude)
+    c.axis_dim[:min(len(dims), PF_ROPE_MAX_AXES)] = dims[:PF_ROPE_MAX_AXES]
+    rope = PfRope()
+    st = load_library().pf_rope_init(C.byref(c), C.byref(rope))
+    if st != 0:
+        _raise(st)
+    return rope
+
+
+def _heads(name, t, head_dim):
+    if head_dim < 1 or t.shape[1] % head_dim:
+        raise PfError(-3, f"{name}: rows of {t.shape[1]} channels are no whole heads of {head_dim}")
+    return t.shape[1] // head_dim
+
+
+def _positions(rope, pos, tokens, device):
+    n = rope.n_axes
+    return _ints("pos", pos, (tokens,) if pos.dim() == 1 and n == 1 else (tokens, n), device)
+
+
+def pf_op_rope(x, rope, pos, head_dim, out=None):
+    """x [tokens, heads * head_dim] with every head turned by its row's position(s); pos int32 [tokens, n_axes] (or [tokens] for
+    one axis).  out may be x."""
+    _rows("x", x)
+    tokens, dev = x.shape[0], x.device
+    heads = _heads("x", x, head_dim)
+    _positions(rope, pos, tokens, dev)
+    out = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else _out("out", out, x.shape, x.dtype, dev)
+    with _on(dev) as stream:
+        st = load_library().pf_op_rope(_DT[x.dtype], C.byref(rope), pos.data_ptr(), x.data_ptr(), _ld(x), out.data_ptr(), _ld(out),
+                                       tokens, heads, head_dim, stream)
+    if st != 0:
+        _raise(st)
+    return out
+
+
+def _out(name, t, shape, dtype, device):
+    _rows(name, t, dtype, device)
+    if tuple(t.shape) != tuple(shape):
+        raise PfError(-3, f"{name}: shape {tuple(t.shape)}, {tuple(shape)} is needed")
+    return t
+
+
+class KvPages:
+    """Keys and values in pages: k and v [n_pages, kv_heads, page_size, head_dim] (pages any distance apart, a page contiguous),
+    table int32 [n_seqs, max_pages] of page numbers (those outside [0, n_pages): no page).  Holds the tensors it was given;
+    their contents, the table's among them, may change between calls."""
+
+    def __init__(self, k, v, table):
+        for name, t in (("k", k), ("v", v)):
+            _plain(name, t, None if t is k else k.dtype, k.device)
+            if t.dim() != 4 or t.shape != k.shape or not (t.shape[0] == 0 or t[0].is_contiguous()):
+                raise PfError(-3, f"{name} pages: shape {tuple(t.shape)}, strides {t.stride()}")
+        if table.dim() != 2:
+            raise PfError(-3, f"table: shape {tuple(table.shape)}, [n_seqs, max_pages] is needed")
+        _ints("table", table, table.shape, k.device)
+        self.k, self.v, self.table = k, v, table
+        n, self.kv_heads, self.page_size, self.head_dim = k.shape
+        block = self.kv_heads * self.page_size * self.head_dim
+        self.n_seqs, self.max_pages = table.shape
+        self.c = PfKvPages(k=k.data_ptr(), v=v.data_ptr(), k_page_stride=k.stride(0) if n > 1 else block,
+                           v_page_stride=v.stride(0) if n > 1 else block, table=table.data_ptr(), n_pages=n,
+                           page_size=self.page_size, kv_heads=self.kv_heads, head_dim=self.head_dim, n_seqs=self.n_seqs,
+                           max_pages=self.max_pages)
+
+
+def pf_op_kv_append(pages, k, v, cu, first, rope=None, pos=None, q=None, q_out=None):
+    """Writes rows of k and v [tokens, kv_heads * head_dim] into the pages, row cu[s] + i of sequence s into slot first[s] + i, k
+    turned by `rope` on the way; returns q turned likewise (None without q)."""
+    dt, dev = pages.k.dtype, pages.k.device
+    _rows("k", k, dt, dev)
+    _out("v", v, k.shape, dt, dev)
+    tokens = k.shape[0]
+    if k.shape[1] != pages.kv_heads * pages.head_dim:
+        raise PfError(-3, f"k: rows of {k.shape[1]} channels for {pages.kv_heads} heads of {pages.head_dim}")
+    _ints("cu", cu, (pages.n_seqs + 1,), dev)
+    _ints("first", first, (pages.n_seqs,), dev)
+    if rope is not None:
+        if pos is None:
+            raise PfError(-1, "pos")
+        _positions(rope, pos, tokens, dev)
+    heads = 0
+    if q is not None:
+        _rows("q", q, dt, dev)
+        if q.shape[0] != tokens:
+            raise PfError(-3, f"q: {q.shape[0]} rows, k has {tokens}")
+        heads = _heads("q", q, pages.head_dim)
+        q_out = torch.empty(q.shape, dtype=dt, device=dev) if q_out is None else _out("q_out", q_out, q.shape, dt, dev)
+    elif q_out is not None:
+        raise PfError(-1, "q_out without q")
+    with _on(dev) as stream:
+        st = load_library().pf_op_kv_append(
+            _DT[dt], C.byref(pages.c), k.data_ptr(), _ld(k), v.data_ptr(), _ld(v), cu.data_ptr(), first.data_ptr(), tokens,
+            None if rope is None else C.byref(rope), None if rope is None else pos.data_ptr(),
+            None if q is None else q.data_ptr(), 0 if q is None else _ld(q), None if q is None else q_out.data_ptr(),
+            0 if q is None else _ld(q_out), heads, stream)
+    if st != 0:
+        _raise(st)
+    return q_out
+
+
+def _attention_buffers(q, heads, kv_heads, head_dim, n_seqs, max_kv, out, want_lse):
+    dev = q.device
+    out = torch.empty(q.shape, dtype=q.dtype, device=dev) if out is None else _out("out", out, q.shape, q.dtype, dev)
+    lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=dev) if want_lse else None
+    n = load_library().pf_op_attention_rows_ws_bytes(_DT[q.dtype], q.shape[0], n_seqs, heads, kv_heads, head_dim, max_kv)
+    return out, lse, torch.empty(n, dtype=torch.uint8, device=dev) if n else None, n
+
+
+def pf_op_attention_packed(q, k, v, cu_q, cu_k, head_dim, causal=False, scale=None, out=None, want_lse=False):
+    """Attention of packed sequences: q [total_q, heads * head_dim], k and v [total_k, kv_heads * head_dim], cu_q and cu_k int32
+    [n_seqs + 1].  causal: the last query of a sequence sees all its keys, the one before all but one, ...  Returns out, or
+    (out, lse) with lse float [total_q, heads]; rows of no sequence are not written."""
+    _rows("q", q)
+    _rows("k", k, q.dtype, q.device)
+    _out("v", v, k.shape, q.dtype, q.device)
+    heads, kv_heads = _heads("q", q, head_dim), _heads("k", k, head_dim)
+    if cu_q.dim() != 1 or cu_q.shape[0] < 1:
+        raise PfError(-3, f"cu_q: shape {tuple(cu_q.shape)}, [n_seqs + 1] is needed")
+    n_seqs = cu_q.shape[0] - 1
+    _ints("cu_q", cu_q, (n_seqs + 1,), q.device)
+    _ints("cu_k", cu_k, (n_seqs + 1,), q.device)
+    if scale is not None and not scale > 0:
+        raise PfError(-3, f"scale: {scale}")
+    with _on(q.device) as stream:
+        out, lse, ws, ws_bytes = _attention_buffers(q, heads, kv_heads, head_dim, n_seqs, max(k.shape[0], 1), out, want_lse)
+        st = load_library().pf_op_attention_packed(
+            _DT[q.dtype], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k), v.data_ptr(), _ld(v), cu_q.data_ptr(), cu_k.data_ptr(),
+            n_seqs, q.shape[0], k.shape[0], heads, kv_heads, head_dim, 0.0 if scale is None else scale, int(causal),
+            out.data_ptr(), _ld(out), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes,
+            stream)
+    if st != 0:
+        _raise(st)
+    return (out, lse) if want_lse else out
+
+
+def pf_op_attention_paged(q, pages, cu_q, first, kv_len, causal=True, scale=None, out=None, want_lse=False):
+    """Attention of new rows q [total_q, heads * head_dim], cu_q[s] .. cu_q[s + 1] those of sequence s from its slot first[s] on,
+    over slots [0, kv_len[s]) of the pages; causal: row i sees slots up to first[s] + i.  first may be None if not causal.
+    Returns out, or (out, lse) with lse float [total_q, heads]; rows of no sequence are not written."""
+    _rows("q", q, pages.k.dtype, pages.k.device)
+    heads = _heads("q", q, pages.head_dim)
+    _ints("cu_q", cu_q, (pages.n_seqs + 1,), q.device)
+    _ints("kv_len", kv_len, (pages.n_seqs,), q.device)
+    if first is not None:
+        _ints("first", first, (pages.n_seqs,), q.device)
+    if scale is not None and not scale > 0:
+        raise PfError(-3, f"scale: {scale}")
+    with _on(q.device) as stream:
+        out, lse, ws, ws_bytes = _attention_buffers(q, heads, pages.kv_heads, pages.head_dim, pages.n_seqs,
+                                                    pages.max_pages * pages.page_size, out, want_lse)
+        st = load_library().pf_op_attention_paged(
+            _DT[q.dtype], q.data_ptr(), _ld(q), C.byref(pages.c), cu_q.data_ptr(), None if first is None else first.data_ptr(),
+            kv_len.data_ptr(), q.shape[0], heads, 0.0 if scale is None else scale, int(causal), out.data_ptr(), _ld(out),
+            None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes, stream)
+    if st != 0:
+        _raise(st)
+    return (out, lse) if want_lse else out
+
+
+class Norm:
+    """A norm over rows for pf_op_norm_residual (make_norm)."""
+
+    def __init__(self, kind, weight, bias, eps):
+        if kind not in NORM_KINDS:
+            raise PfError(-2, f"norm: kind {kind!r}")
+        self.weight, self.bias = weight, bias
+        for name, t in (("weight", weight), ("bias", bias)):
+            if t is not None and (t.dim() != 1 or not _plain("norm " + name, t).is_contiguous()):
+                raise PfError(-3, f"norm {name}: shape {tuple(t.shape)}, a contiguous [d] is needed")
+        self.c = PfNorm(kind=NORM_KINDS[kind], eps=eps, weight=None if weight is None else weight.data_ptr(),
+                        bias=None if bias is None else bias.data_ptr())
+
+
+def make_norm(kind, weight=None, bias=None, eps=1e-6):
+    """kind "rms" or "layer", weight and bias [d] in the type of the branch or None."""
+    return Norm(kind, weight, bias, eps)
+
+
+def pf_op_norm_residual(y, x, post=None, pre=None, gate=None, gate_tanh=False, x_scale=1.0, scale=None, shift=None, cu=None,
+                        x_out=None, h_out=None, dtype=None, want_h=True):
+    """x_out = x_scale * x + g(gate) * post(y), h = pre(x_out) * (1 + scale) + shift; returns (x_out, h).  x float [rows, d], y and h
+    in `dtype` (y's; without a branch, y None, it has to be given).  gate / scale / shift float [d], or [n_seqs, d] with cu
+    int32 [n_seqs + 1].  want_h False: only the residual (h None)."""
+    _rows("x", x, torch.float32)
+    rows, d = x.shape
+    dev = x.device
+    if y is not None:
+        _rows("y", y, dtype, dev)
+        if y.shape != x.shape:
+            raise PfError(-3, f"y: shape {tuple(y.shape)}, x has {tuple(x.shape)}")
+        dtype = y.dtype
+    if dtype not in _DT:
+        raise PfError(-4, f"dtype {dtype}")
+    for name, n in (("post", post), ("pre", pre)):
+        for t in () if n is None else (n.weight, n.bias):
+            if t is not None and tuple(_plain(name + " norm", t, dtype, dev).shape) != (d,):
+                raise PfError(-3, f"{name} norm: {tuple(t.shape)}, ({d},) is needed")
+    n_seqs = None
+    if cu is not None:
+        if cu.dim() != 1 or cu.shape[0] < 1:
+            raise PfError(-3, f"cu: shape {tuple(cu.shape)}, [n_seqs + 1] is needed")
+        n_seqs = cu.shape[0] - 1
+        _ints("cu", cu, (n_seqs + 1,), dev)
+    gs = _vectors("gate", gate, d, n_seqs, dev)
+    ms = _vectors("scale", scale, d, n_seqs, dev)
+    ms2 = _vectors("shift", shift, d, n_seqs, dev)
+    if scale is not None and shift is not None and ms != ms2:
+        raise PfError(-3, f"scale and shift: {ms} and {ms2} elements between sequences")
+    x_out = torch.empty(rows, d, dtype=torch.float32, device=dev) if x_out is None else _out("x_out", x_out, x.shape, torch.float32, dev)
+    if want_h:
+        h_out = torch.empty(rows, d, dtype=dtype, device=dev) if h_out is None else _out("h_out", h_out, x.shape, dtype, dev)
+    with _on(dev) as stream:
+        st = load_library().pf_op_norm_residual(
+            _DT[dtype], _ptr(y), 0 if y is None else _ld(y), None if post is None else C.byref(post.c), _ptr(gate), gs,
+            int(gate_tanh), x_scale, x.data_ptr(), _ld(x), x_out.data_ptr(), _ld(x_out), None if pre is None else C.byref(pre.c),
+            _ptr(shift), _ptr(scale), max(ms, ms2), _ptr(h_out) if want_h else None, _ld(h_out) if want_h else 0, _ptr(cu),
+            n_seqs or 0, rows, d, stream)
+    if st != 0:
+        _raise(st)
+    return x_out, h_out if want_h else None

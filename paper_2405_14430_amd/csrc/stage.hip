@@ -12,6 +12,7 @@
 
 #include "../../include/pfstage.h"
 #include "ops.h"
+#include "requests.h"
 
 using namespace pf;
 
@@ -224,6 +225,15 @@ pf_status fail(pf_stage *s, pf_status st, const std::string &msg) {
   if (s) s->err = msg; else g_create_error = msg;
   return st;
 }
+
+}  // namespace
+
+pf_status pf::note_error(pf_status st, const char *text) {
+  try { g_create_error = text; } catch (...) {}   // no memory for the text: the status still says what happened
+  return st;
+}
+
+namespace {
 
 hipEvent_t get_event(pf_stage *s) {
   if (!s->pool.empty()) { hipEvent_t e = s->pool.back(); s->pool.pop_back(); return e; }

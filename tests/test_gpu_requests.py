@@ -1,0 +1,546 @@
+"""The operators on packed rows against their plain 64-bit forms (tests/requests_ref.py), element by element."""
+import math
+import random
+
+import pytest
+import torch
+
+import requests_ref as R
+from paper_2405_14430_amd import (KvPages, make_norm, make_rope, pf_op_attention_packed, pf_op_attention_paged, pf_op_gemm,
+                                  pf_op_kv_append, pf_op_norm_residual, pf_op_rope)
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+CANARY = 77.0
+
+
+def dev(*shape, dtype=BF16, seed=0, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * std).to(dtype).cuda()
+
+
+def ints(*values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def cu(lengths, start=0):
+    out = [start]
+    for n in lengths:
+        out.append(out[-1] + n)
+    return ints(*out)
+
+
+def wide(rows, width, dtype, seed, extra=16):
+    """Rows further apart than they are wide, so that a wrong stride shows."""
+    return dev(rows, width + extra, dtype=dtype, seed=seed)[:, :width]
+
+
+# ---- rotary positions ------------------------------------------------------------------------------------------------------
+ROPES = [
+    dict(axes=(128,), head_dim=128, layout="half", theta=1e4),
+    dict(axes=(64,), head_dim=128, layout="half", theta=5e5, scaling="ramp_turns", factor=8.0, low=1.0, high=4.0, original_len=8192),
+    dict(axes=(50,), head_dim=64, layout="half", theta=1e4),                      # odd half width, channels behind the axis
+    dict(axes=(10,), head_dim=64, layout="interleaved", theta=1e4, scaling="linear", factor=4.0),   # ends inside a unit
+    dict(axes=(72,), head_dim=72, layout="half", theta=1e4, scaling="ntk", factor=2.0),
+    dict(axes=(16, 56, 56), head_dim=128, layout="interleaved", theta=1e4),
+    dict(axes=(16, 24, 24), head_dim=64, layout="half", theta=1e4),
+    dict(axes=(36, 36), head_dim=72, layout="interleaved", theta=1e4),
+    dict(axes=(2, 6, 4), head_dim=16, layout="half", theta=100.0, magnitude=1.25),
+    dict(axes=(96,), head_dim=96, layout="interleaved", theta=1e6, scaling="ramp_index", factor=16.0, low=1.0, high=32.0,
+         original_len=4096, magnitude=1.1),
+    dict(axes=(8,), head_dim=8, layout="half", theta=1e4),
+]
+
+
+def make(r):
+    kw = {k: v for k, v in r.items() if k not in ("axes", "head_dim")}
+    return make_rope(r["axes"], **kw)
+
+
+def rope_args(r):
+    return {k: v for k, v in r.items()}
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("tokens,heads,far", [(1, 1, 3), (5, 3, 1000000), (130, 7, 4096), (4097, 2, 100)])
+@pytest.mark.parametrize("r", ROPES, ids=lambda r: f"{r['axes']}-{r['layout']}")
+def test_rope(r, tokens, heads, far, dtype):
+    dh = r["head_dim"]
+    x = wide(tokens, heads * dh, dtype, seed=tokens)
+    pos = torch.randint(-far, far + 1, (tokens, len(r["axes"])), generator=torch.Generator().manual_seed(1), dtype=torch.int32).cuda()
+    want, bound = R.rope(x, pos, **rope_args(r))
+    out = torch.full((tokens, heads * dh + 8), CANARY, dtype=dtype, device="cuda")
+    pf_op_rope(x, make(r), pos, dh, out=out[:, :heads * dh])
+    R.check(out[:, :heads * dh], want, R.stored(bound, want, dtype), "rope")
+    assert (out[:, heads * dh:] == CANARY).all()
+    assert torch.equal(pf_op_rope(x, make(r), pos, dh), out[:, :heads * dh])
+    pf_op_rope(x, make(r), pos, dh, out=x)   # in place
+    assert torch.equal(x, out[:, :heads * dh])
+
+
+def test_rope_extreme_positions_and_values_behind_the_axes():
+    """The ends of the int32 range turn by the right angle; infinities and NaN behind the axes pass, and stay there."""
+    x = dev(4, 64, dtype=F32)
+    x[:, 40], x[:, 63] = math.inf, math.nan
+    pos = ints(2 ** 31 - 1, -2 ** 31, 0, 1)
+    want, bound = R.rope(x, pos, 64, (10,), "interleaved", 1e4)
+    # a position of 2^31 times a frequency rounded to 53 bits: 2^-21 of a turn
+    R.check(pf_op_rope(x, make_rope((10,), theta=1e4), pos, 64), want, bound + 2 * math.pi * 2.0 ** -21 * 2 * x[:, :10].abs().max().item(), "rope")
+
+
+# ---- the paged cache ---------------------------------------------------------------------------------------------------------
+def make_pages(kv_heads, head_dim, page, need, dtype, seed=0, fill=None, spare=3, gap=0):
+    """Pools with `need` pages per sequence in an arbitrary order; gap: elements between pages."""
+    n = sum(need) + spare
+    order = list(range(n))
+    random.Random(seed).shuffle(order)
+    width = max(max(need), 1)
+    table, at = [], 0
+    for c in need:
+        table.append(order[at:at + c] + [-1] * (width - c))
+        at += c
+    block = kv_heads * page * head_dim
+
+    def pool(s):
+        flat = dev(n, block + gap, dtype=dtype, seed=s) if fill is None else torch.full((n, block + gap), fill, dtype=dtype, device="cuda")
+        return flat[:, :block].unflatten(1, (kv_heads, page, head_dim))
+
+    return KvPages(pool(seed + 100), pool(seed + 200), torch.tensor(table, dtype=torch.int32).cuda())
+
+
+def slot_rows(pages, pool, s, n):
+    """Slots [0, n) of sequence s, [n, kv_heads * head_dim], and which of them have a page."""
+    table = pages.table.cpu()
+    out = torch.zeros(n, pages.kv_heads * pages.head_dim, dtype=torch.float64)
+    have = torch.zeros(n, dtype=torch.bool)
+    p = R.d64(pool)
+    for t in range(n):
+        if t // pages.page_size >= pages.max_pages:
+            continue
+        pg = int(table[s, t // pages.page_size])
+        if 0 <= pg < pool.shape[0]:
+            out[t], have[t] = p[pg, :, t % pages.page_size].reshape(-1), True
+    return out, have
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("page,heads,kv_heads,new,first,ri", [
+    (16, 8, 2, [1] * 5, [0, 15, 16, 31, 40], 0),
+    (32, 4, 4, [33, 0, 7, 64], [5, 3, 30, 0], 3),
+    (64, 6, 3, [130, 1], [0, 200], 6),
+    (256, 0, 1, [300], [17], 4),
+    (16, 3, 1, [4200, 50], [0, 7], 5),
+])
+def test_kv_append(page, heads, kv_heads, new, first, ri, dtype):
+    r = ROPES[ri]
+    dh = r["head_dim"]
+    tokens, lead, tail = sum(new), 2, 3          # rows of no sequence in front and behind
+    rows = lead + tokens + tail
+    # (a page more than needed would take the dropped rows: none here)
+    pages = make_pages(kv_heads, dh, page, [(f + n + page - 1) // page for f, n in zip(first, new)], dtype, fill=CANARY, gap=8)
+    qkv = dev(rows, (heads + 2 * kv_heads) * dh, dtype=dtype, seed=3)
+    q, k, v = qkv.split((heads * dh, kv_heads * dh, kv_heads * dh), dim=1)
+    pos = torch.randint(0, 500, (rows, len(r["axes"])), generator=torch.Generator().manual_seed(2), dtype=torch.int32).cuda()
+    q_out = torch.full((rows, heads * dh), CANARY, dtype=dtype, device="cuda") if heads else None
+    got = pf_op_kv_append(pages, k, v, cu(new, lead), ints(*first), rope=make(r), pos=pos, q=q if heads else None, q_out=q_out)
+    want_k, bound_k = R.rope(k, pos, **rope_args(r))
+    written = torch.zeros(pages.k.shape[0], page, dtype=torch.bool)
+    at = lead
+    for s, (n, f) in enumerate(zip(new, first)):
+        kr, have = slot_rows(pages, pages.k, s, f + n)
+        vr, _ = slot_rows(pages, pages.v, s, f + n)
+        assert have.all()
+        R.check(kr[f:], want_k[at:at + n], R.stored(bound_k, want_k, dtype)[at:at + n], ("k", s))
+        assert torch.equal(vr[f:], R.d64(v[at:at + n])), s
+        for t in range(f, f + n):
+            written[int(pages.table[s, t // page]), t % page] = True
+        at += n
+    for pool in (pages.k, pages.v):
+        assert (pool.cpu().permute(0, 2, 1, 3)[~written] == CANARY).all()
+    if heads:
+        want, bound = R.rope(q, pos, **rope_args(r))
+        R.check(got[lead:lead + tokens], want[lead:lead + tokens], R.stored(bound, want, dtype)[lead:lead + tokens], "q")
+        assert (got[:lead] == CANARY).all() and (got[lead + tokens:] == CANARY).all()
+    else:
+        assert got is None
+
+
+def test_kv_append_without_rope_copies():
+    pages = make_pages(2, 72, 16, [3, 1], BF16, fill=CANARY)
+    k, v, q = (dev(20, n * 72, seed=i) for i, n in enumerate((2, 2, 4)))
+    q_out = pf_op_kv_append(pages, k, v, cu([12, 8]), ints(30, 2), q=q)
+    assert torch.equal(q_out, q)
+    for s, (f, a, b) in enumerate(((30, 0, 12), (2, 12, 20))):
+        assert torch.equal(slot_rows(pages, pages.k, s, f + b - a)[0][f:], R.d64(k[a:b]))
+        assert torch.equal(slot_rows(pages, pages.v, s, f + b - a)[0][f:], R.d64(v[a:b]))
+
+
+def test_kv_append_drops_rows_without_a_place():
+    """Negative slots, slots past the table and table entries that are no page: nothing is written anywhere."""
+    pages = make_pages(1, 64, 16, [2, 2, 2], BF16, fill=CANARY)
+    t = pages.table
+    t[1, 0], t[1, 1] = -5, pages.k.shape[0]
+    k, v = dev(60, 64, seed=1), dev(60, 64, seed=2)
+    pf_op_kv_append(pages, k, v, cu([20, 20, 20]), ints(-4, 6, 2 ** 31 - 5))
+    kr, _ = slot_rows(pages, pages.k, 0, 32)
+    assert torch.equal(kr[:16], R.d64(k[4:20])) and (kr[16:] == CANARY).all()
+    keep = torch.ones(pages.k.shape[0], dtype=torch.bool)
+    keep[int(t[0, 0])] = False
+    assert (pages.k[keep.cuda()] == CANARY).all() and (pages.v[keep.cuda()] == CANARY).all()
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------------
+PACKED = [
+    # head_dim, heads, kv_heads, query lengths, key lengths (None: the same), causal
+    (128, 4, 1, [1], None, True),
+    (64, 4, 4, [1, 2, 3, 0, 17, 64, 65], None, True),
+    (64, 2, 1, [63, 1, 128, 129], None, False),
+    (72, 3, 3, [100, 31], [257, 64], False),
+    (72, 2, 2, [1100], [1300], True),
+    (80, 2, 1, [33, 70], None, True),
+    (96, 4, 2, [50, 200], [1, 130], False),
+    (128, 8, 2, [300, 5], None, True),
+    (128, 7, 1, [40, 9], [500, 70], True),            # an odd number of heads to a key head
+    (128, 2, 2, [20, 5, 4, 8], [7, 5, 0, 1], True),    # rows that see nothing: more queries than keys, no keys at all
+    (128, 2, 1, [3, 0, 2], [0, 9, 4], False),
+    (8, 2, 1, [70], None, True),
+    (40, 1, 1, [129], [200], False),
+    (64, 1, 1, [1], [5000], False),                    # few rows over many keys
+    (128, 16, 2, [2, 1], [3000, 1200], True),
+    (120, 2, 2, [260, 300], None, True),
+]
+
+
+def packed_reference(q, k, v, dh, nq, nk, causal, lead, scale=None):
+    outs, at_q, at_k = [], lead, lead
+    for n, m in zip(nq, nk):
+        last = torch.arange(n) + (m - n) + 1 if causal else torch.full((n,), m)
+        outs.append(R.attention(q[at_q:at_q + n], k[at_k:at_k + m], v[at_k:at_k + m], dh, last, scale))
+        at_q, at_k = at_q + n, at_k + m
+    return [torch.cat([o[i] for o in outs]) for i in range(5)]
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("dh,heads,kv_heads,nq,nk,causal", PACKED)
+def test_attention_packed(dh, heads, kv_heads, nq, nk, causal, dtype):
+    nk = nq if nk is None else nk
+    lead = 2
+    tq, tk = sum(nq) + lead + 3, sum(nk) + lead + 70
+    q = wide(tq, heads * dh, dtype, 1)
+    kv = dev(tk, 2 * kv_heads * dh, dtype=dtype, seed=2)
+    kv[:lead] = math.nan                     # rows of no sequence: not read
+    kv[sum(nk) + lead:] = math.nan
+    k, v = kv.split(kv_heads * dh, dim=1)
+    out = torch.full((tq, heads * dh), CANARY, dtype=dtype, device="cuda")
+    got, lse = pf_op_attention_packed(q, k, v, cu(nq, lead), cu(nk, lead), dh, causal=causal, out=out, want_lse=True)
+    want, want_lse, b16, b32, bl = packed_reference(q, k, v, dh, nq, nk, causal, lead)
+    mid = slice(lead, lead + sum(nq))
+    R.check(got[mid], want, R.stored(b16 if dtype == BF16 else b32, want, dtype), "out")
+    R.check(lse[mid], want_lse, bl + 4 * R.U * want_lse.abs().nan_to_num(posinf=0.0), "lse")
+    assert (got[:lead] == CANARY).all() and (got[lead + sum(nq):] == CANARY).all()
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+def test_attention_packed_many_sequences_and_scale(dtype):
+    """More sequences than one round of the search covers, many of them empty, and a scale of the caller's."""
+    rng = random.Random(5)
+    nq = [rng.choice([0, 0, 1, 2, 9]) for _ in range(300)]
+    nk = [n + rng.choice([0, 1, 20]) for n in nq]
+    q, k, v = dev(sum(nq), 2 * 64, dtype=dtype, seed=1), dev(sum(nk), 64, dtype=dtype, seed=2), dev(sum(nk), 64, dtype=dtype, seed=3)
+    got = pf_op_attention_packed(q, k, v, cu(nq), cu(nk), 64, causal=True, scale=0.31)
+    want, _, b16, b32, _ = packed_reference(q, k, v, 64, nq, nk, True, 0, 0.31)
+    R.check(got, want, R.stored(b16 if dtype == BF16 else b32, want, dtype), "out")
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("kind", ["rising", "falling", "one", "far", "same"])
+def test_attention_packed_score_patterns(kind, dtype):
+    """Scores that rise or fall along the keys, one key far above the rest, all far below zero, all alike."""
+    n, m, dh = 70, 700, 64
+    q, k, v = dev(n, dh, dtype=dtype, seed=1), torch.zeros(m, dh, dtype=dtype, device="cuda"), dev(m, dh, dtype=dtype, seed=3)
+    q[:, 0] = 8.0
+    ramp = torch.linspace(0, 60, m, device="cuda")
+    k[:, 0] = {"rising": ramp, "falling": -ramp, "one": torch.zeros_like(ramp), "far": ramp - 3000, "same": torch.ones_like(ramp)}[kind].to(dtype)
+    if kind == "one":
+        k[523, 0] = 200.0
+    for causal in (False, True):
+        got = pf_op_attention_packed(q, k, v, cu([n]), cu([m]), dh, causal=causal)
+        want, _, b16, b32, _ = packed_reference(q, k, v, dh, [n], [m], causal, 0)
+        R.check(got, want, R.stored(b16 if dtype == BF16 else b32, want, dtype), kind)
+
+
+PAGED = [
+    # head_dim, heads, kv_heads, page, new lengths, first slots, kv lengths, causal
+    (128, 8, 2, 16, [1, 1, 1, 1], [0, 15, 16, 700], None, True),
+    (128, 4, 4, 64, [1], [2000], None, True),
+    (64, 8, 1, 32, [1, 3, 0, 17], [100, 0, 5, 64], None, True),
+    (64, 3, 3, 128, [128, 128], [130, 0], [600, 300], False),          # patches inside their caches
+    (72, 2, 2, 16, [70, 1], [33, 9], None, True),
+    (72, 2, 2, 256, [70, 33], [0, 0], [513, 200], False),
+    (96, 4, 1, 16, [40], [0], [39], True),                              # a cache shorter than its chunk
+    (128, 2, 1, 16, [2, 3, 4], [5, -2, 3], [0, 20, 2], True),           # no keys; rows before the first slot; fewer keys than slots
+    (128, 16, 2, 16, [5, 1, 2], [1000, 3, 333], None, True),
+    (8, 2, 2, 16, [20], [45], None, True),
+    (128, 1, 1, 1024, [300], [900], None, True),
+]
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("dh,heads,kv_heads,page,new,first,kv,causal", PAGED)
+def test_attention_paged(dh, heads, kv_heads, page, new, first, kv, causal, dtype):
+    kv = [f + n for f, n in zip(first, new)] if kv is None else kv
+    lead = 1
+    pages = make_pages(kv_heads, dh, page, [(n + page - 1) // page for n in kv], dtype, gap=8)
+    # rows behind a sequence's keys, pages of nobody: not read
+    used = torch.zeros(pages.k.shape[0], page, dtype=torch.bool)
+    for s, n in enumerate(kv):
+        for t in range(n):
+            used[int(pages.table[s, t // page]), t % page] = True
+    for pool in (pages.k, pages.v):
+        pool.permute(0, 2, 1, 3)[~used.cuda()] = math.nan
+    tq = sum(new) + lead + 2
+    q = wide(tq, heads * dh, dtype, 4)
+    out = torch.full((tq, heads * dh), CANARY, dtype=dtype, device="cuda")
+    got, lse = pf_op_attention_paged(q, pages, cu(new, lead), ints(*first), ints(*kv), causal=causal, out=out, want_lse=True)
+    at = lead
+    for s, n in enumerate(new):
+        k, have = slot_rows(pages, pages.k, s, kv[s])
+        v, _ = slot_rows(pages, pages.v, s, kv[s])
+        last = (torch.arange(n) + first[s] + 1).clamp(max=kv[s]) if causal else torch.full((n,), kv[s])
+        want, want_lse, b16, b32, bl = R.attention(q[at:at + n], k, v, dh, last, present=have)
+        R.check(got[at:at + n], want, R.stored(b16 if dtype == BF16 else b32, want, dtype), ("out", s))
+        R.check(lse[at:at + n], want_lse, bl + 4 * R.U * want_lse.abs().nan_to_num(posinf=0.0), ("lse", s))
+        at += n
+    assert (got[:lead] == CANARY).all() and (got[at:] == CANARY).all()
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("new,causal", [([1, 1], True), ([40, 150], False), ([40, 150], True)])
+def test_attention_paged_missing_pages_and_long_lengths(new, causal, dtype):
+    """Table entries that are no page hide their keys; a length past the table's end stops there."""
+    pages = make_pages(2, 64, 16, [14, 14], dtype)
+    t = pages.table
+    t[0, 3], t[0, 4], t[1, 0], t[1, 13] = -1, pages.k.shape[0], -2 ** 31, 2 ** 31 - 1
+    kv = [10 ** 9, 14 * 16]
+    first = [200 - new[0], 224 - new[1]]
+    q = dev(sum(new), 4 * 64, dtype=dtype, seed=2)
+    got = pf_op_attention_paged(q, pages, cu(new), ints(*first), ints(*kv), causal=causal)
+    at = 0
+    for s, n in enumerate(new):
+        m = 224
+        k, have = slot_rows(pages, pages.k, s, m)
+        v, _ = slot_rows(pages, pages.v, s, m)
+        last = (torch.arange(n) + first[s] + 1).clamp(max=m) if causal else torch.full((n,), m)
+        want, _, b16, b32, _ = R.attention(q[at:at + n], k, v, 64, last, present=have)
+        R.check(got[at:at + n], want, R.stored(b16 if dtype == BF16 else b32, want, dtype), s)
+        at += n
+
+
+def test_attention_paged_without_any_page_gives_zeros():
+    pages = make_pages(1, 128, 16, [4, 4], BF16)
+    pages.table.fill_(-1)
+    q = dev(3, 2 * 128)
+    got, lse = pf_op_attention_paged(q, pages, cu([1, 2]), ints(40, 50), ints(41, 52), want_lse=True)
+    assert (got == 0).all() and (lse == -math.inf).all()
+
+
+def test_lse_joins_two_halves_of_the_keys():
+    """Attention over the whole of a sequence from attention over its two parts and their log-sum-exps."""
+    q, k, v = dev(50, 256, dtype=F32, seed=1), dev(600, 128, dtype=F32, seed=2), dev(600, 128, dtype=F32, seed=3)
+    parts = [pf_op_attention_packed(q, k[a:b], v[a:b], cu([50]), cu([b - a]), 128, want_lse=True) for a, b in ((0, 211), (211, 600))]
+    (o1, l1), (o2, l2) = parts
+    top = torch.logaddexp(l1, l2)
+    whole = torch.exp(l1 - top)[..., None] * o1.view(50, 2, 128) + torch.exp(l2 - top)[..., None] * o2.view(50, 2, 128)
+    want, _, _, b32, _ = packed_reference(q, k, v, 128, [50], [600], False, 0)
+    R.check(whole.reshape(50, 256), want, 4 * b32 + 1e-30, "joined")
+
+
+# ---- norms, gate and residual ---------------------------------------------------------------------------------------------------
+NORMS = [("none", "rms"), ("rms", "none"), ("rms", "layer"), ("layer", "rms"), ("layer", "layer"), ("none", "none")]
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("post,pre", NORMS)
+@pytest.mark.parametrize("rows,d,tanh", [([1], 8, False), ([3, 0, 70], 264, True), ([5, 2], 1152, False), ([2, 1], 8192, True),
+                                         ([9, 8], 2056, False), ([2000, 2100], 520, True)])
+def test_norm_residual(rows, d, tanh, post, pre, dtype):
+    n, lead = sum(rows), 1
+    total = n + lead + 2
+    y, x = wide(total, d, dtype, 1, extra=8), wide(total, d, F32, 2, extra=8) + 0.5
+    gate, both = dev(len(rows), d, dtype=F32, seed=3), dev(len(rows), 2 * d, dtype=F32, seed=4, std=0.3)
+    scale, shift = both[:, :d], both[:, d:]
+    side = {k: (kind, None if kind == "none" else dev(d, dtype=dtype, seed=5), dev(d, dtype=dtype, seed=6) if kind == "layer" else None, 1e-5)
+            for k, kind in (("post", post), ("pre", pre))}
+    x_out, h_out = torch.full((total, d), CANARY, device="cuda"), torch.full((total, d), CANARY, dtype=dtype, device="cuda")
+    norms = {k: None if s[0] == "none" else make_norm(s[0], s[1], s[2], eps=s[3]) for k, s in side.items()}
+    pf_op_norm_residual(y, x, gate=gate, gate_tanh=tanh, x_scale=0.75, scale=scale, shift=shift, cu=cu(rows, lead), x_out=x_out, h_out=h_out, **norms)
+    seg = torch.repeat_interleave(torch.arange(len(rows)), torch.tensor(rows))
+    mid = slice(lead, lead + n)
+    wx, wh, bx, bh = R.norm_residual(y[mid], x[mid], seg, side["post"], side["pre"], gate, tanh, 0.75, scale, shift)
+    R.check(x_out[mid], wx, bx + 1e-30, "x")
+    R.check(h_out[mid], wh, R.stored(bh, wh, dtype), "h")
+    for t in (x_out, h_out):
+        assert (t[:lead] == CANARY).all() and (t[lead + n:] == CANARY).all()
+    # in place, and one set of vectors for all rows
+    one = dict(gate=gate[0].contiguous(), scale=scale[0].contiguous(), shift=shift[0].contiguous())
+    a = pf_op_norm_residual(y, x, gate_tanh=tanh, **one, **norms)
+    b = pf_op_norm_residual(y, x, gate_tanh=tanh, x_out=x, h_out=y, **one, **norms)
+    assert b[0] is x and b[1] is y and torch.equal(a[0], x) and torch.equal(a[1], y)
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+def test_norm_residual_parts(dtype):
+    """Without a branch, without gate and modulation, without h; norms without weights."""
+    x, y = dev(6, 96, dtype=F32, seed=1), dev(6, 96, dtype=dtype, seed=2)
+    layer = ("layer", None, None, 1e-6)
+    xo, h = pf_op_norm_residual(None, x, pre=make_norm("layer"), dtype=dtype)
+    _, wh, _, bh = R.norm_residual(None, x, None, pre=layer)
+    assert torch.equal(xo, x)
+    R.check(h, wh, R.stored(bh, wh, dtype), "h")
+    xo, h = pf_op_norm_residual(y, x, post=make_norm("layer"), want_h=False)
+    wx, _, bx, _ = R.norm_residual(y, x, None, post=layer)
+    assert h is None
+    R.check(xo, wx, bx + 1e-30, "x")
+
+
+def test_norm_residual_rows_stay_apart():
+    """A row of zeros, one of infinities and one of NaN change no other row; a row of equal values has no variance."""
+    x, y = torch.zeros(6, 512, device="cuda"), dev(6, 512, seed=1)
+    x[1], x[2, 7], x[3] = math.inf, math.nan, 3.0
+    y[0], y[3] = 0, 0
+    xo, h = pf_op_norm_residual(y, x, post=make_norm("rms"), pre=make_norm("layer", eps=1e-6))
+    assert (h[0] == 0).all() and (h[3] == 0).all() and torch.isnan(h[1]).all() and torch.isnan(h[2]).all()
+    wx, wh, bx, bh = R.norm_residual(y[4:], x[4:], None, post=("rms", None, None, 1e-6), pre=("layer", None, None, 1e-6))
+    R.check(xo[4:], wx, bx + 1e-30, "x")
+    R.check(h[4:], wh, R.stored(bh, wh, BF16), "h")
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------------
+class Block:
+    """One attention block of a program that serves images and prompts of different sizes, on the library's operators, and the
+    same in 64 bits with the roundings the stored tensors have."""
+
+    def __init__(self, dtype, seed=0):
+        self.dt, self.H, self.Hk, self.dh, self.page = dtype, 4, 2, 64, 16
+        self.d = self.H * self.dh
+        self.w_qkv = dev((self.H + 2 * self.Hk) * self.dh, self.d, dtype=dtype, seed=seed + 1, std=0.06)
+        self.w_o = dev(self.d, self.d, dtype=dtype, seed=seed + 2, std=0.06)
+        self.pre, self.post = dev(self.d, dtype=dtype, seed=seed + 3), dev(self.d, dtype=dtype, seed=seed + 4)
+        self.rope_kw = dict(axes=(32, 32), layout="interleaved", theta=1e4)
+        self.rope = make_rope((32, 32), layout="interleaved", theta=1e4)
+
+    def run(self, x, cu_rows, first, kv_len, pos, pages, gate, causal):
+        zero = torch.zeros(self.w_qkv.shape[0], dtype=self.dt, device="cuda")
+        _, h = pf_op_norm_residual(None, x, pre=make_norm("rms", self.pre), dtype=self.dt)
+        qkv = pf_op_gemm(h, self.w_qkv, zero)
+        q, k, v = qkv.split((self.H * self.dh, self.Hk * self.dh, self.Hk * self.dh), dim=1)
+        q = pf_op_kv_append(pages, k, v, cu_rows, first, rope=self.rope, pos=pos, q=q)
+        o = pf_op_attention_paged(q, pages, cu_rows, first, kv_len, causal=causal)
+        y = pf_op_gemm(o, self.w_o, zero[:self.d])
+        x2, _ = pf_op_norm_residual(y, x, post=make_norm("rms", self.post), gate=gate, gate_tanh=True, cu=cu_rows, want_h=False)
+        return x2
+
+    def plain(self, x, new, first, kv_len, pos, cache, gate, causal):
+        """cache: per sequence [k, v] of 64-bit rows; the new rows are written into it."""
+        rnd = lambda t: t.to(self.dt).double()
+        x = R.d64(x)
+        h = rnd(R.norm(x, "rms", self.pre, None, 1e-6)[0])
+        qkv = rnd(h @ R.d64(self.w_qkv).T)
+        q, k, v = qkv.split((self.H * self.dh, self.Hk * self.dh, self.Hk * self.dh), dim=1)
+        turn = lambda t: rnd(R.rope(t, pos, self.dh, **self.rope_kw)[0])
+        q, k = turn(q), turn(k)
+        outs, at = [], 0
+        for s, n in enumerate(new):
+            cache[s][0][first[s]:first[s] + n], cache[s][1][first[s]:first[s] + n] = k[at:at + n], v[at:at + n]
+            m = kv_len[s]
+            last = torch.arange(n) + first[s] + 1 if causal else torch.full((n,), m)
+            outs.append(R.attention(q[at:at + n], cache[s][0][:m], cache[s][1][:m], self.dh, last)[0])
+            at += n
+        y = rnd(rnd(torch.cat(outs)) @ R.d64(self.w_o).T)
+        seg = torch.repeat_interleave(torch.arange(len(new)), torch.tensor(new))
+        return x + torch.tanh(R.d64(gate))[seg] * R.norm(y, "rms", self.post, None, 1e-6)[0]
+
+
+def rel_rms(got, want):
+    return float(((R.d64(got) - want) ** 2).mean().sqrt() / (want ** 2).mean().sqrt())
+
+
+@pytest.mark.parametrize("dtype,tol", [(BF16, 1e-2), (F32, 1e-5)])
+def test_a_block_on_patches_then_tokens(dtype, tol):
+    """Warm-up of two sequences, a patch in the middle of one while the other grows by single tokens: the operators of a block one after
+    the other, against the block in 64 bits.  An output is x plus a unit-variance branch times a gate below one; the
+    branch's five stored tensors carry roundings of 2^-8 (bf16), each less than 2^-8 of the result in rms."""
+    blk = Block(dtype)
+    new, first, kv = [100, 37], [0, 0], [100, 37]
+    pages = make_pages(blk.Hk, blk.dh, blk.page, [7, 4], dtype)
+    cache = [[torch.zeros(128, blk.Hk * blk.dh, dtype=torch.float64) for _ in range(2)] for _ in range(2)]
+    gate = dev(2, blk.d, dtype=F32, seed=9)
+    for step in range(4):
+        if step:
+            new, first = [25, 1], [25 * step, 36 + step]
+            kv = [100, 37 + step]
+        x = dev(sum(new), blk.d, dtype=F32, seed=20 + step)
+        pos = torch.cat([torch.stack([torch.arange(f, f + n) // 10, torch.arange(f, f + n) % 10], 1) for f, n in zip(first, new)]).int().cuda()
+        got = blk.run(x, cu(new), ints(*first), ints(*kv), pos, pages, gate, causal=False)
+        want = blk.plain(x, new, first, kv, pos, cache, gate, causal=False)
+        assert rel_rms(got, want) < tol, (step, rel_rms(got, want))
+
+
+def test_a_captured_block_replays_with_other_lengths():
+    """One graph of the operators of a block serves every step of a growing batch:
+    lengths, positions and tables are read on the device.  Each replay equals the eager calls."""
+    blk = Block(BF16)
+    steps = 5
+    caches = [make_pages(blk.Hk, blk.dh, blk.page, [7, 40], BF16, seed=1) for _ in range(2)]
+    x = torch.zeros(3, blk.d, device="cuda")
+    st = dict(cu_rows=cu([2, 1]), first=ints(50, 3), kv_len=ints(52, 4), pos=torch.zeros(3, 2, dtype=torch.int32, device="cuda"))
+    gate = dev(2, blk.d, dtype=F32, seed=9)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        blk.run(x, pages=caches[0], gate=gate, causal=True, **st)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for c in caches:
+        c.k.zero_()
+        c.v.zero_()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = blk.run(x, pages=caches[0], gate=gate, causal=True, **st)
+    for i in range(steps):
+        x.copy_(dev(3, blk.d, dtype=F32, seed=30 + i))
+        lens = [(2, 1), (1, 2), (0, 3), (3, 0), (1, 1)][i]
+        first = [60 + 3 * i, 100 * i + 5]
+        st["cu_rows"].copy_(cu(lens))
+        st["first"].copy_(ints(*first))
+        st["kv_len"].copy_(ints(first[0] + lens[0], first[1] + lens[1]))
+        st["pos"].copy_(torch.randint(0, 60, (3, 2), generator=torch.Generator().manual_seed(i), dtype=torch.int32))
+        out.fill_(CANARY)
+        g.replay()
+        torch.cuda.synchronize()
+        want = torch.full_like(out, CANARY)
+        n = sum(lens)
+        eager = blk.run(x, pages=caches[1], gate=gate, causal=True, **st)
+        want[:n] = eager[:n]
+        assert torch.equal(out, want), i
+        assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v, caches[1].v), i
+
+
+def test_two_streams_at_once():
+    """Calls of one kind on two streams share nothing."""
+    work = []
+    for i in range(2):
+        pages = make_pages(2, 128, 16, [200], BF16, seed=i)
+        work.append((dev(2, 8 * 128, seed=i), pages))
+    run = lambda q, pages: pf_op_attention_paged(q, pages, cu([2]), ints(3100), ints(3102))
+    want = [run(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    got = [[], []]
+    for _ in range(20):
+        for i, (w, s) in enumerate(zip(work, streams)):
+            with torch.cuda.stream(s):
+                got[i].append(run(*w))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
