@@ -17,6 +17,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          # packed-fp32 arithmetic is kept off for all device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
+# attn_rows.hip: results of matrix instructions in ordinary registers also in the kernels with more than 256 of them.  Left to
+# itself the compiler puts all of them into accumulation registers there, and every score, which the vector unit works on
+# next, is copied out of them.
+FILE_FLAGS = {"attn_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 # Kernels that must not use scratch memory: their LDS fragment reads are asynchronous inline-assembly loads whose
 # completion is tracked by hand, so a register spill between a read and its wait would save a value that has not
@@ -44,7 +49,7 @@ def _check_no_scratch(src, log):
 def _compile(src, objdir=OBJ, extra=()):
     obj = os.path.join(objdir, src.replace(".hip", ".o"))
     check = ["-Rpass-analysis=kernel-resource-usage"] if src in NO_SCRATCH else []
-    cmd = [HIPCC, *FLAGS, *extra, *check, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [HIPCC, *FLAGS, *FILE_FLAGS.get(src, []), *extra, *check, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     log = r.stdout + r.stderr
     out = "\n".join(l for l in log.splitlines() if "packed-fp32-ops" not in l and "kernel-resource-usage" not in l)

@@ -16,15 +16,27 @@
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
 // bounds of the buffer loads give zeros for rows past the last key, for pages that are none and for channels past the head, so
 // neither the scores nor 0 * v meets what lies there.  LDS rows are swizzled by 16-byte pieces against bank conflicts.
+#include <type_traits>
+
 #include "requests.h"
 
 namespace pf {
 namespace {
 
+// f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>), in order
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled(F &&f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    unrolled<N, I + 1>(f);
+  }
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -46,6 +58,14 @@ struct Buffer {
 };
 __device__ s16x4 lds_read_transposed(const unsigned char *) { return s16x4{}; }
 #endif
+
+// A pointer or number that all lanes agree on, in scalar registers.
+template <typename T>
+__device__ __forceinline__ const T *uniform(const T *p) {
+  const uint64_t u = (uint64_t)p;
+  return (const T *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 struct RowsKernelArgs {
   RowsAttn a;
@@ -100,6 +120,172 @@ __device__ __forceinline__ int sequence_keys(const RowsAttn &a, int s, int &k0) 
   }
 }
 
+// The rows and keys of a workgroup.  Workgroup id -> (key head, row tile, chunk): neighbouring ids are different key heads - ids go
+// round the 8 XCDs, so with 8 or more key heads a head's workgroups meet in one L2 - and later row tiles, which see more
+// keys, come first.  Row tiles of sequence s are slots floor(cu[s] G / ROWS) + s and on: enough of them for any start.
+struct Work {
+  int hk, sp, s;
+  int q0, n;              // the sequence's first row and its number of rows
+  int r_first;            // first (token, head) row of the tile
+  int k0, k_end;          // packed: row of key 0; keys that some row of the tile sees lie before k_end
+  int kb, ke;             // the chunk's
+  int64_t first;          // slot of query 0
+};
+template <bool PAGED, int ROWS, int UNIT>
+__device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Work &w) {
+  const RowsAttn &a = p.a;
+  const int G = p.group;
+  const int rest = blockIdx.x / a.kv_heads;
+  w.hk = blockIdx.x % a.kv_heads;
+  w.sp = rest % a.splits;
+  const int slot = p.slots - 1 - rest / a.splits;
+  w.s = wave_search(a.n_seqs - 1, lane, slot, [&](int i) { return clampi(a.cu_q[i], 0, a.total_q) * G / ROWS + i; });
+  if (w.s < 0) return false;
+  int q1;
+  sequence_rows(a.cu_q, w.s, a.total_q, w.q0, q1);
+  w.n = q1 - w.q0;
+  w.r_first = (slot - (w.q0 * G / ROWS + w.s)) * ROWS;
+  if (w.r_first < 0 || w.r_first >= w.n * G) return false;
+  const int kn = sequence_keys<PAGED>(a, w.s, w.k0);
+  w.first = !a.causal ? 0 : PAGED ? a.first[w.s] : kn - w.n;
+  const int t_last = (w.r_first + ROWS < w.n * G ? w.r_first + ROWS - 1 : w.n * G - 1) / G;
+  w.k_end = kn;
+  if (a.causal && w.first + t_last + 1 < w.k_end) w.k_end = w.first + t_last + 1 < 0 ? 0 : (int)(w.first + t_last + 1);
+  w.kb = 0;
+  w.ke = w.k_end;
+  if (a.splits > 1) {
+    int longest = 0;
+    for (int i = lane; i < a.n_seqs; i += 64) {
+      int unused;
+      longest = max(longest, sequence_keys<PAGED>(a, i, unused));
+    }
+    for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, kWave));
+    const int64_t c = (int64_t)chunk_tiles((longest + UNIT - 1) / UNIT, a.splits) * UNIT;
+    w.kb = (int)min((int64_t)w.k_end, w.sp * c);
+    w.ke = (int)min((int64_t)w.k_end, (w.sp + 1) * c);
+  }
+  return true;
+}
+
+// Brings a wave's RW rows (from row LW on) of K and V tiles of TK keys from memory into registers, and from there into LDS.  The rows
+// of a load lie in one group of 16 keys, so in one page.
+template <typename C, typename T, bool PAGED>
+struct TileLoader {
+  static constexpr int TK = C::TK, ROWB = C::ROWB;
+  static constexpr int GROUPS = C::RW > 16 ? C::RW / 16 : 1;      // page groups a wave loads per tile
+  static constexpr int GL = C::LOADS / GROUPS;                     // loads per group
+  static constexpr int GROWS = C::RW / GROUPS;
+  static constexpr int TPB = 1024 / TK;                            // tiles per block of 64 groups
+  static constexpr unsigned kOutside = 0x7fff0000u;
+  static constexpr unsigned kAllGroups = (1u << (TK / 16)) - 1;
+  const RowsAttn &a;
+  const int lane, lw, s, kb, ke;
+  unsigned k_row, v_row;                                           // bytes between rows
+  unsigned k_off[C::LOADS], v_off[C::LOADS];                       // the lane's bytes from a group's first row
+  const T *k_head, *v_head;
+  // Pages: lane i holds the page of 16-key group i of the current 1024 keys, and of the next 1024 (loaded that far ahead).
+  int page_now = -1, page_next = -1;
+  unsigned groups = kAllGroups;                                    // which groups of the tile in the registers have a page
+  const T *k_from[GROUPS], *v_from[GROUPS];
+  int in_group[GROUPS];                                            // rows of the group that there are
+  u32x4 k_reg[C::LOADS], v_reg[C::LOADS];
+
+  __device__ __forceinline__ TileLoader(const RowsAttn &args, const Work &w, int lane_, int lw_, int kb_, int ke_)
+      : a(args), lane(lane_), lw(lw_), s(w.s), kb(kb_), ke(ke_) {
+    const int dh = a.head_dim;
+    k_row = (unsigned)((PAGED ? (int64_t)dh : a.ldk) * (int64_t)sizeof(T));
+    v_row = (unsigned)((PAGED ? (int64_t)dh : a.ldv) * (int64_t)sizeof(T));
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) {
+      const int off = i * 1024 + lane * 16, row = off / ROWB, piece = (off % ROWB) >> 4;
+      const int in_tile = lw * C::RW + row, at = row % GROWS;
+      const int kc = piece ^ C::kkey(in_tile), vc = piece ^ C::vkey(in_tile);
+      k_off[i] = kc * 16 < dh * (int)sizeof(T) ? at * k_row + kc * 16 : kOutside;
+      v_off[i] = vc * 16 < dh * (int)sizeof(T) ? at * v_row + vc * 16 : kOutside;
+    }
+    if constexpr (PAGED) {
+      k_head = (const T *)a.pages.k + ((int64_t)w.hk << a.pages.page_shift) * dh;
+      v_head = (const T *)a.pages.v + ((int64_t)w.hk << a.pages.page_shift) * dh;
+      page_next = table_entry(0);
+    } else {
+      k_head = (const T *)a.k + (int64_t)w.k0 * a.ldk + (int64_t)w.hk * dh;
+      v_head = (const T *)a.v + (int64_t)w.k0 * a.ldv + (int64_t)w.hk * dh;
+    }
+  }
+  __device__ __forceinline__ int table_entry(int block) const {
+    const int64_t key = (int64_t)kb + block * 1024 + lane * 16;
+    int pg = -1;
+    if (key < ke) pg = a.pages.table[(int64_t)s * a.pages.max_pages + (key >> a.pages.page_shift)];
+    return pg >= 0 && pg < a.pages.n_pages ? pg : -1;
+  }
+  // Sets the sources of tile t's loads.  Tiles have to be taken in order, each once; tiles behind the last one read as zeros.
+  __device__ __forceinline__ void aim(int t) {
+    if constexpr (PAGED) {
+      if (t % TPB == 0) {
+        page_now = page_next;
+        page_next = table_entry(t / TPB + 1);
+      }
+      groups = (unsigned)(__builtin_amdgcn_ballot_w64(page_now >= 0) >> ((t % TPB) * (TK / 16))) & kAllGroups;
+    }
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int key = kb + t * TK + lw * C::RW + g * GROWS;       // wave-uniform
+      int rows = clampi(ke - key, 0, GROWS);
+      if constexpr (PAGED) {
+        const int pg = __builtin_amdgcn_readlane(page_now, (t % TPB) * (TK / 16) + ((lw * C::RW + g * GROWS) >> 4));
+        if (pg < 0) rows = 0;
+        const int64_t at = (int64_t)(key & ((1 << a.pages.page_shift) - 1)) * a.head_dim;
+        k_from[g] = uniform(k_head + (pg < 0 ? 0 : pg * a.pages.k_stride + at));
+        v_from[g] = uniform(v_head + (pg < 0 ? 0 : pg * a.pages.v_stride + at));
+      } else {
+        k_from[g] = uniform(k_head + (rows ? key * a.ldk : 0));
+        v_from[g] = uniform(v_head + (rows ? key * a.ldv : 0));
+      }
+      in_group[g] = uniform(rows);
+    }
+  }
+  __device__ __forceinline__ void load_k(int i) { k_reg[i] = Buffer(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[i]); }
+  __device__ __forceinline__ void load_v(int i) { v_reg[i] = Buffer(v_from[i / GL], in_group[i / GL] * v_row).load16(v_off[i]); }
+  __device__ __forceinline__ void load(int t) {
+    aim(t);
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) load_k(i);
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) load_v(i);
+  }
+  __device__ __forceinline__ void store_k(unsigned char *tile, int i) const { *reinterpret_cast<u32x4 *>(tile + lw * C::RW * ROWB + lane * 16 + i * 1024) = k_reg[i]; }
+  __device__ __forceinline__ void store_v(unsigned char *tile, int i) const { *reinterpret_cast<u32x4 *>(tile + lw * C::RW * ROWB + lane * 16 + i * 1024) = v_reg[i]; }
+  __device__ __forceinline__ void store(unsigned char *k_tile, unsigned char *v_tile) const {
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) store_k(k_tile, i);
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) store_v(v_tile, i);
+  }
+};
+
+// One row's channels c .. c + 3 of the result, or of its partial result.
+template <typename T>
+__device__ __forceinline__ void put4(const RowsAttn &a, int sp, int64_t row, int head, int c, float inv, float x0, float x1, float x2, float x3) {
+  if (a.splits > 1) {
+    float *dst = a.ws + (((int64_t)sp * a.total_q + row) * a.n_heads + head) * a.head_dim + c;
+    *reinterpret_cast<float4 *>(dst) = make_float4(x0, x1, x2, x3);
+    return;
+  }
+  T *dst = (T *)a.out + row * a.ldo + (int64_t)head * a.head_dim + c;
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst) = make_float4(x0 * inv, x1 * inv, x2 * inv, x3 * inv);
+  else *reinterpret_cast<bf16x4 *>(dst) = bf16x4{(bf16_t)(x0 * inv), (bf16_t)(x1 * inv), (bf16_t)(x2 * inv), (bf16_t)(x3 * inv)};
+}
+// m: the reference exponent (of 2) that l is relative to
+__device__ __forceinline__ void put_stats(const RowsAttn &a, int sp, int64_t row, int head, float m, float l) {
+  const int64_t at = row * a.n_heads + head;
+  if (a.splits > 1) {
+    float *dst = a.ws + (int64_t)a.splits * a.total_q * a.n_heads * a.head_dim + ((int64_t)sp * a.total_q * a.n_heads + at) * 2;
+    *reinterpret_cast<float2 *>(dst) = make_float2(l > 0.f ? m : -INFINITY, l);
+  } else if (a.lse) {
+    a.lse[at] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+  }
+}
+
 template <typename T, int DHP, bool PAGED, int NW, int KW>
 __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void attn_rows_kernel(RowsKernelArgs p) {
   using C = Tile<T, DHP, NW, KW>;
@@ -109,58 +295,25 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
   const int dh = a.head_dim, G = p.group;
-
-  // ---- workgroup -> (key head, row tile, chunk).  Neighbouring ids are different key heads: ids go round the 8 XCDs, so with 8
-  // or more key heads a head's workgroups meet in one L2.  Later row tiles, which see more keys, come first.
-  const int hk = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int sp = rest % a.splits, slot = p.slots - 1 - rest / a.splits;
-  // row tiles of sequence s: slots floor(cu[s] G / ROWS) + s and on, enough for any start of the sequence
-  const int s = wave_search(a.n_seqs - 1, lane, slot, [&](int i) { return clampi(a.cu_q[i], 0, a.total_q) * G / C::ROWS + i; });
-  if (s < 0) return;
-  int q0, q1;
-  sequence_rows(a.cu_q, s, a.total_q, q0, q1);
-  const int n = q1 - q0;
-  const int r_first = (slot - (q0 * G / C::ROWS + s)) * C::ROWS;
-  if (r_first < 0 || r_first >= n * G) return;
-
-  // ---- keys: those of the sequence, for causal rows up to the tile's last row's; the chunk's share of them
-  int k0;
-  const int kn = sequence_keys<PAGED>(a, s, k0);
-  const int64_t first = !a.causal ? 0 : PAGED ? a.first[s] : kn - n;      // the slot of query 0
-  const int t_last = (r_first + C::ROWS < n * G ? r_first + C::ROWS - 1 : n * G - 1) / G;
-  int k_end = kn;
-  if (a.causal && first + t_last + 1 < k_end) k_end = first + t_last + 1 < 0 ? 0 : (int)(first + t_last + 1);
-  constexpr int UNIT = 64 * KW;      // keys per chunk tile: a multiple of what all waves walk in a step
-  int kb = 0, ke = k_end;
-  if (a.splits > 1) {
-    int longest = 0;
-    for (int i = lane; i < a.n_seqs; i += 64) {
-      int unused;
-      longest = max(longest, sequence_keys<PAGED>(a, i, unused));
-    }
-    for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, kWave));
-    const int64_t c = (int64_t)chunk_tiles((longest + UNIT - 1) / UNIT, a.splits) * UNIT;
-    kb = (int)min((int64_t)k_end, sp * c);
-    ke = (int)min((int64_t)k_end, (sp + 1) * c);
-  }
+  Work w;
+  if (!find_work<PAGED, C::ROWS, 64 * KW>(p, lane, w)) return;   // chunks: whole tiles for all waves
+  int kb = w.kb, ke = w.ke;
   if constexpr (KW > 1) {            // the wave's quarter
     const int q = ((ke - kb + KW - 1) / KW + TK - 1) / TK * TK;
-    const int wb = min(ke, kb + (wave / NW) * q);
-    ke = min(ke, wb + q);
-    kb = wb;
+    kb = min(ke, kb + wave * q);
+    ke = min(ke, kb + q);
   }
   kb = __builtin_amdgcn_readfirstlane(kb);
   ke = __builtin_amdgcn_readfirstlane(ke);
   const int tiles = (ke - kb + TK - 1) / TK;
 
   // ---- the lane's row
-  const int wr = KW > 1 ? 0 : wave;
-  const int r = r_first + wr * 32 + l32;
-  const bool row_ok = r < n * G;
+  const int r = w.r_first + (KW > 1 ? 0 : wave) * 32 + l32;
+  const bool row_ok = r < w.n * G;
   const int tok = row_ok ? r / G : 0;
-  const int head = hk * G + (row_ok ? r - tok * G : 0);
+  const int head = w.hk * G + (row_ok ? r - tok * G : 0);
   int limit = ke;                    // keys before this one are seen
-  if (row_ok && a.causal && first + tok + 1 < limit) limit = first + tok + 1 < 0 ? 0 : (int)(first + tok + 1);
+  if (row_ok && a.causal && w.first + tok + 1 < limit) limit = w.first + tok + 1 < 0 ? 0 : (int)(w.first + tok + 1);
   int least = limit;                 // of all rows of the wave: tiles below it need no mask
   for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
   least = __builtin_amdgcn_readfirstlane(least);
@@ -169,7 +322,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   constexpr int NQ = C::F32 ? DHP / 8 : DHP / 16;
   u32x4 qf[NQ];
   {
-    const T *qp = (const T *)a.q + (int64_t)(q0 + tok) * a.ldq + (int64_t)head * dh;
+    const T *qp = (const T *)a.q + (int64_t)(w.q0 + tok) * a.ldq + (int64_t)head * dh;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int c = C::F32 ? i * 8 + hi * 4 : i * 16 + hi * 8;
@@ -177,80 +330,9 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       if (row_ok && c < dh) qf[i] = *reinterpret_cast<const u32x4 *>(qp + c);
     }
   }
-
-  // ---- tile loads.  A wave brings in rows [w * RW, (w + 1) * RW) of a tile, all of one 16-row group, so of one page (the key
-  // kernel's 32 rows: two groups, loaded one after the other).
-  const int lw = KW > 1 ? 0 : wave;
-  constexpr int GROUPS = C::RW > 16 ? C::RW / 16 : 1;            // page groups a wave loads per tile
-  constexpr int GL = C::LOADS / GROUPS;                           // loads per group
-  constexpr int GROWS = C::RW / GROUPS;
-  const unsigned k_row = (unsigned)((PAGED ? (int64_t)dh : a.ldk) * (int64_t)sizeof(T));
-  const unsigned v_row = (unsigned)((PAGED ? (int64_t)dh : a.ldv) * (int64_t)sizeof(T));
-  constexpr unsigned kOutside = 0x7fff0000u;
-  unsigned k_off[C::LOADS], v_off[C::LOADS];                      // from the group's first row
-#pragma unroll
-  for (int i = 0; i < C::LOADS; ++i) {
-    const int off = i * 1024 + lane * 16, row = off / ROWB, piece = (off % ROWB) >> 4;
-    const int in_tile = lw * C::RW + row, in_group = row % GROWS;
-    const int kc = piece ^ C::kkey(in_tile), vc = piece ^ C::vkey(in_tile);
-    k_off[i] = kc * 16 < dh * (int)sizeof(T) ? in_group * k_row + kc * 16 : kOutside;
-    v_off[i] = vc * 16 < dh * (int)sizeof(T) ? in_group * v_row + vc * 16 : kOutside;
-  }
-  unsigned char *const ring = smem + (KW > 1 ? (wave / NW) * C::BUFS * 2 * C::TILE_B : 0);
-  const T *const k_head = PAGED ? (const T *)a.pages.k + ((int64_t)hk << a.pages.page_shift) * dh : (const T *)a.k + (int64_t)k0 * a.ldk + (int64_t)hk * dh;
-  const T *const v_head = PAGED ? (const T *)a.pages.v + ((int64_t)hk << a.pages.page_shift) * dh : (const T *)a.v + (int64_t)k0 * a.ldv + (int64_t)hk * dh;
-
-  // Pages: lane i holds the page of 16-key group i of the current 1024 keys, and of the next 1024 (loaded that far ahead).
-  // kb is a multiple of TK; groups count from kb rounded down to 16.
-  constexpr int TPB = 1024 / TK;                                  // tiles per block of 64 groups
-  int page_now = -1, page_next = -1;
-  auto table_entry = [&](int block) __attribute__((always_inline)) {
-    const int64_t key = (int64_t)kb + block * 1024 + lane * 16;
-    int pg = -1;
-    if (key < ke) pg = a.pages.table[(int64_t)s * a.pages.max_pages + (key >> a.pages.page_shift)];
-    return pg >= 0 && pg < a.pages.n_pages ? pg : -1;
-  };
-  if constexpr (PAGED) page_next = table_entry(0);
-
-  u32x4 k_reg[C::LOADS], v_reg[C::LOADS];
-  unsigned groups_ahead = 0;        // which 16-key groups of the tile in the registers have a page
-  auto load_tile = [&](int t) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
-      if (t % TPB == 0) {
-        page_now = page_next;
-        page_next = table_entry(t / TPB + 1);
-      }
-      groups_ahead = (unsigned)(__builtin_amdgcn_ballot_w64(page_now >= 0) >> ((t % TPB) * (TK / 16))) & ((1u << (TK / 16)) - 1);
-    }
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int key = kb + t * TK + lw * C::RW + g * GROWS;       // wave-uniform
-      int rows = clampi(ke - key, 0, GROWS);
-      const T *ks, *vs;
-      if constexpr (PAGED) {
-        const int pg = __builtin_amdgcn_readlane(page_now, (t % TPB) * (TK / 16) + ((lw * C::RW + g * GROWS) >> 4));
-        if (pg < 0) rows = 0;
-        const int64_t at = (int64_t)(key & ((1 << a.pages.page_shift) - 1)) * dh;
-        ks = k_head + (pg < 0 ? 0 : pg * a.pages.k_stride + at);
-        vs = v_head + (pg < 0 ? 0 : pg * a.pages.v_stride + at);
-      } else {
-        ks = k_head + (rows ? key * a.ldk : 0);
-        vs = v_head + (rows ? key * a.ldv : 0);
-      }
-      const Buffer kbuf(ks, rows * k_row), vbuf(vs, rows * v_row);
-#pragma unroll
-      for (int i = 0; i < GL; ++i) k_reg[g * GL + i] = kbuf.load16(k_off[g * GL + i]);
-#pragma unroll
-      for (int i = 0; i < GL; ++i) v_reg[g * GL + i] = vbuf.load16(v_off[g * GL + i]);
-    }
-  };
-  auto store_tile = [&](int buf) __attribute__((always_inline)) {
-    unsigned char *kd = ring + buf * 2 * C::TILE_B + lw * C::RW * ROWB + lane * 16, *vd = kd + C::TILE_B;
-#pragma unroll
-    for (int i = 0; i < C::LOADS; ++i) *reinterpret_cast<u32x4 *>(kd + i * 1024) = k_reg[i];
-#pragma unroll
-    for (int i = 0; i < C::LOADS; ++i) *reinterpret_cast<u32x4 *>(vd + i * 1024) = v_reg[i];
-  };
+  TileLoader<C, T, PAGED> ld(a, w, lane, KW > 1 ? 0 : wave, kb, ke);
+  unsigned char *const ring = smem + (KW > 1 ? wave * C::BUFS * 2 * C::TILE_B : 0);
+  auto store_tile = [&](int buf) __attribute__((always_inline)) { ld.store(ring + buf * 2 * C::TILE_B, ring + (buf * 2 + 1) * C::TILE_B); };
 
   f32x16 o[CB];
 #pragma unroll
@@ -294,7 +376,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       }
     }
     const int key0 = kb + t * TK;
-    if (key0 + TK > least || (PAGED && groups != (1u << (TK / 16)) - 1)) {
+    if (key0 + TK > least || (PAGED && groups != ld.kAllGroups)) {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -354,13 +436,13 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     }
   };
 
-  if (tiles > 0) load_tile(0);
+  if (tiles > 0) ld.load(0);
   if constexpr (NW > 1) {
     // two LDS buffers: behind the barrier tile t is whole in one and nobody reads the other, which tile t + 1 goes to
-    unsigned groups = groups_ahead;
+    unsigned groups = ld.groups;
     if (tiles > 0) {
       store_tile(0);
-      if (tiles > 1) load_tile(1);
+      if (tiles > 1) ld.load(1);
     }
     for (int t = 0; t < tiles; ++t) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -368,18 +450,18 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       asm volatile("" ::: "memory");
       const unsigned now = groups;
       if (t + 1 < tiles) {
-        groups = groups_ahead;
+        groups = ld.groups;
         store_tile((t + 1) & 1);
-        if (t + 2 < tiles) load_tile(t + 2);
+        if (t + 2 < tiles) ld.load(t + 2);
       }
       work_tile(t, t & 1, now);
     }
   } else {
     // a wave's LDS operations are carried out in order: its own tile needs no barrier
     for (int t = 0; t < tiles; ++t) {
-      const unsigned now = groups_ahead;
+      const unsigned now = ld.groups;
       store_tile(0);
-      if (t + 1 < tiles) load_tile(t + 1);
+      if (t + 1 < tiles) ld.load(t + 1);
       work_tile(t, 0, now);
     }
   }
@@ -405,85 +487,305 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     __syncthreads();
     float m_all = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < KW; ++w) m_all = fmaxf(m_all, ml[(w * 32 + l32) * 2]);
+    for (int v = 0; v < KW; ++v) m_all = fmaxf(m_all, ml[(v * 32 + l32) * 2]);
     const float m_use = m_all == -INFINITY ? 0.f : m_all;
     float wt[KW];
     l_tot = 0.f;
 #pragma unroll
-    for (int w = 0; w < KW; ++w) {
-      wt[w] = __builtin_amdgcn_exp2f((ml[(w * 32 + l32) * 2] - m_use) * p.sl2);
-      l_tot += wt[w] * ml[(w * 32 + l32) * 2 + 1];
+    for (int v = 0; v < KW; ++v) {
+      wt[v] = __builtin_amdgcn_exp2f((ml[(v * 32 + l32) * 2] - m_use) * p.sl2);
+      l_tot += wt[v] * ml[(v * 32 + l32) * 2 + 1];
     }
     m_run = m_all;
     // the lane's channels: 4 hi + 8 (wave + 4 i) .. + 3
     if (row_ok) {
       const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-      const int64_t qr = q0 + tok;
 #pragma unroll
       for (int i = 0; i < (DHP / 8 + KW - 1) / KW; ++i) {
         const int c = 4 * hi + 8 * (wave + KW * i);
         if (c < dh) {
           float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int w = 0; w < KW; ++w) {
-            const float4 x = *reinterpret_cast<const float4 *>(om + (w * 32 + l32) * OSTR + c);
-            acc[0] = fmaf(wt[w], x.x, acc[0]);
-            acc[1] = fmaf(wt[w], x.y, acc[1]);
-            acc[2] = fmaf(wt[w], x.z, acc[2]);
-            acc[3] = fmaf(wt[w], x.w, acc[3]);
+          for (int v = 0; v < KW; ++v) {
+            const float4 x = *reinterpret_cast<const float4 *>(om + (v * 32 + l32) * OSTR + c);
+            acc[0] = fmaf(wt[v], x.x, acc[0]);
+            acc[1] = fmaf(wt[v], x.y, acc[1]);
+            acc[2] = fmaf(wt[v], x.z, acc[2]);
+            acc[3] = fmaf(wt[v], x.w, acc[3]);
           }
-          if (a.splits > 1) {
-            float *dst = a.ws + (((int64_t)sp * a.total_q + qr) * a.n_heads + head) * dh + c;
-            *reinterpret_cast<float4 *>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-          } else {
-            T *dst = (T *)a.out + qr * a.ldo + (int64_t)head * dh + c;
-            if constexpr (C::F32) {
-              *reinterpret_cast<float4 *>(dst) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-            } else {
-              bf16x4 v;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(acc[e] * inv);
-              *reinterpret_cast<bf16x4 *>(dst) = v;
-            }
-          }
+          put4<T>(a, w.sp, w.q0 + tok, head, c, inv, acc[0], acc[1], acc[2], acc[3]);
         }
       }
     }
     if (wave != 0) return;
   } else if (row_ok) {
     const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-    const int64_t qr = q0 + tok;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int c = cb * 32 + 8 * g + 4 * hi;
-        if (c < dh) {
-          if (a.splits > 1) {
-            float *dst = a.ws + (((int64_t)sp * a.total_q + qr) * a.n_heads + head) * dh + c;
-            *reinterpret_cast<float4 *>(dst) = make_float4(o[cb][4 * g], o[cb][4 * g + 1], o[cb][4 * g + 2], o[cb][4 * g + 3]);
-          } else {
-            T *dst = (T *)a.out + qr * a.ldo + (int64_t)head * dh + c;
-            if constexpr (C::F32) {
-              *reinterpret_cast<float4 *>(dst) = make_float4(o[cb][4 * g] * inv, o[cb][4 * g + 1] * inv, o[cb][4 * g + 2] * inv, o[cb][4 * g + 3] * inv);
-            } else {
-              bf16x4 v;
+        if (c < dh) put4<T>(a, w.sp, w.q0 + tok, head, c, inv, o[cb][4 * g], o[cb][4 * g + 1], o[cb][4 * g + 2], o[cb][4 * g + 3]);
+      }
+  }
+  if (row_ok && hi == 0) put_stats(a, w.sp, w.q0 + tok, head, m_run * p.sl2, l_tot);
+}
+
+// The tile kernel for launches with many rows (bf16): four waves of 64 rows, one workgroup per CU.
+//
+// At 32 rows a wave every MFMA needs a 1 KB fragment from LDS: at the matrix units' rate that is all of the LDS's 128 bytes a
+// clock.  With 64 rows two MFMAs share a fragment.  That leaves one wave per SIMD, so its vector work has to run under its own
+// matrix work: a step on 32 keys is one block of instructions in which the score products of the next 32 keys and
+// the value products of the 32 before go on while the vector unit turns the scores of this step into weights.
+//
+// Weights are taken relative to a reference exponent per row that is not the running maximum: p = 2^(s - ref) is right for
+// any ref while nothing overflows, and the sum of a lane's weights, which is formed anyway, says when it has grown too
+// large.  Only then (and on the first keys of a row, whose ref is -inf) is the maximum found, the reference moved, and the
+// step's weights formed again.
+template <int DHP, bool PAGED>
+__global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p) {
+  using T = bf16_t;
+  using C = Tile<T, DHP, 4, 1>;
+  constexpr int TK = C::TK, CB = C::CB, ROWB = C::ROWB, KS = DHP / 16;
+  constexpr float kSumLimit = 8192.f;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // three K tiles, three V tiles
+  unsigned char *const vring = smem + 3 * C::TILE_B;
+  const RowsAttn &a = p.a;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int l32 = lane & 31, hi = lane >> 5;
+  const int dh = a.head_dim, G = p.group;
+  Work w;
+  if (!find_work<PAGED, 256, 64>(p, lane, w)) return;
+  const int kb = __builtin_amdgcn_readfirstlane(w.kb), ke = __builtin_amdgcn_readfirstlane(w.ke);
+  const int tiles = (ke - kb + TK - 1) / TK;
+
+  // ---- the lane's two rows
+  int tok[2], head[2], limit[2];
+  bool row_ok[2];
+  int least = ke;
+  u32x4 qf[2][KS];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] = (bf16_t)(o[cb][4 * g + e] * inv);
-              *reinterpret_cast<bf16x4 *>(dst) = v;
-            }
+  for (int rb = 0; rb < 2; ++rb) {
+    const int r = w.r_first + wave * 64 + rb * 32 + l32;
+    row_ok[rb] = r < w.n * G;
+    tok[rb] = row_ok[rb] ? r / G : 0;
+    head[rb] = w.hk * G + (row_ok[rb] ? r - tok[rb] * G : 0);
+    limit[rb] = ke;
+    if (row_ok[rb] && a.causal && w.first + tok[rb] + 1 < ke) limit[rb] = w.first + tok[rb] + 1 < 0 ? 0 : (int)(w.first + tok[rb] + 1);
+    least = min(least, limit[rb]);
+    const T *qp = (const T *)a.q + (int64_t)(w.q0 + tok[rb]) * a.ldq + (int64_t)head[rb] * dh;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int c = i * 16 + hi * 8;
+      qf[rb][i] = u32x4{0, 0, 0, 0};
+      if (row_ok[rb] && c < dh) qf[rb][i] = *reinterpret_cast<const u32x4 *>(qp + c);
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
+  least = __builtin_amdgcn_readfirstlane(least);
+
+  TileLoader<C, T, PAGED> ld(a, w, lane, wave, kb, ke);
+
+  f32x16 o[2][CB];
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[rb][cb][i] = 0.f;
+  float ref[2] = {-INFINITY, -INFINITY};     // reference exponents (of 2)
+  float l_run[2] = {0.f, 0.f};
+
+  const int i16 = lane & 15, g1 = (lane >> 4) & 1;
+  const int v_row0 = 4 * hi + (i16 >> 2);
+  const unsigned char *k_at[KS], *v_at[CB];      // in the first K tile and the first V tile
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) k_at[ks] = smem + l32 * ROWB + (((ks * 2 + hi) ^ C::kkey(l32)) << 4);
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) v_at[cb] = vring + v_row0 * ROWB + (((cb * 4 + g1 * 2 + ((i16 & 3) >> 1)) ^ C::vkey(v_row0)) << 4) + (i16 & 1) * 8;
+
+  struct Scores { f32x16 v[2]; };
+  struct Weights { bf16x8 v[2][2]; };
+  const f32x16 zero = {};
+  constexpr int HALF = 32 * ROWB;
+  auto k_fragment = [&](int ks, int at) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + at); };
+  auto v_fragment = [&](int j, int cb, int at) __attribute__((always_inline)) {
+    struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(v_at[cb] + at + j * 16 * ROWB), lds_read_transposed(v_at[cb] + at + (j * 16 + 8) * ROWB)};
+    return __builtin_bit_cast(bf16x8, v8);
+  };
+  auto weights = [&](const f32x16 &x, float neg, bf16x8 (&y)[2]) __attribute__((always_inline)) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(x[i], p.sl2, neg));
+      sum += e;
+      y[i >> 3][i & 7] = (bf16_t)e;
+    }
+    return sum;
+  };
+  // One step: weights of the 32 keys from key0 on (scores `cur`, pages `groups`), scores of the next 32 (K at kt), values of the 32
+  // before (V at vt); SIDE: stores and loads of the tiles to come go along.
+  auto step = [&](int key0, unsigned groups, Scores &cur, Scores &nxt, const Weights &before, Weights &now, int kt, int vt, int side,
+                  auto with_side) __attribute__((always_inline)) {
+    if (key0 + 32 > least || (PAGED && groups != 3)) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int at = 8 * (i >> 2) + (i & 3);
+          if (key0 + at + 4 * hi >= limit[rb] || (PAGED && !((groups >> (at >> 4)) & 1))) cur.v[rb][i] = -INFINITY;
+        }
+    }
+    // The block, in slots of one MFMA with its share of the vector work behind it.  Fragments come from LDS PD fragments ahead of
+    // their two MFMAs; an element passes through its multiply-add, its exponential and its sum in slots behind each other.
+    constexpr int NF = KS + 2 * CB, MF = 2 * NF, PD = 2;
+    bf16x8 ring[PD + 1];
+    auto fragment = [&](auto f_c) __attribute__((always_inline)) {
+      constexpr int f = decltype(f_c)::value;
+      if constexpr (f < KS) return k_fragment(f, kt);
+      else return v_fragment((f - KS) / CB, (f - KS) % CB, vt);
+    };
+    unrolled<PD>([&](auto f_c) __attribute__((always_inline)) { ring[decltype(f_c)::value] = fragment(f_c); });
+    float arg[32], e[32], sum[2] = {0.f, 0.f};
+    unrolled<MF>([&](auto i_c) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_c)::value, f = i / 2, rb = i & 1;
+      if constexpr (rb == 0 && f + PD < NF) ring[(f + PD) % (PD + 1)] = fragment(std::integral_constant<int, f + PD>{});
+      const bf16x8 &fr = ring[f % (PD + 1)];
+      if constexpr (f < KS) nxt.v[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, __builtin_bit_cast(bf16x8, qf[rb][f]), f == 0 ? zero : nxt.v[rb], 0, 0, 0);
+      else o[rb][(f - KS) % CB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, before.v[rb][(f - KS) / CB], o[rb][(f - KS) % CB], 0, 0, 0);
+      // the 2 LOADS registers of a tile, in turn: to LDS, and the next tile's load into them
+      if constexpr (decltype(with_side)::value) {
+        constexpr int U = 2 * C::LOADS, u = i * U / MF;
+        if constexpr (i == 0 || u != (i - 1) * U / MF) {
+          if constexpr (u < C::LOADS) {
+            ld.store_k(smem + side, u);
+            ld.load_k(u);
+          } else {
+            ld.store_v(vring + side, u - C::LOADS);
+            ld.load_v(u - C::LOADS);
           }
         }
       }
-  }
-  if (row_ok && hi == 0) {
-    const int64_t at = (int64_t)(q0 + tok) * a.n_heads + head;
-    if (a.splits > 1) {
-      float *dst = a.ws + (int64_t)a.splits * a.total_q * a.n_heads * dh + ((int64_t)sp * a.total_q * a.n_heads + at) * 2;
-      *reinterpret_cast<float2 *>(dst) = make_float2(l_tot > 0.f ? m_run * p.sl2 : -INFINITY, l_tot);
-    } else if (a.lse) {
-      a.lse[at] = l_tot > 0.f ? m_run * p.sl2 * kLn2 + logf(l_tot) : -INFINITY;
+      constexpr int N = MF - 2;
+      auto from = [](int slot) { return slot < 0 ? 0 : slot > N ? 32 : slot * 32 / N; };
+#pragma unroll
+      for (int x = from(i); x < from(i + 1); ++x) {
+        arg[x] = fmaf(cur.v[x >> 4][x & 15], p.sl2, -ref[x >> 4]);
+        asm volatile("" : "+v"(arg[x]));   // stays in this slot
+      }
+#pragma unroll
+      for (int x = from(i - 1); x < from(i); ++x) {
+        e[x] = __builtin_amdgcn_exp2f(arg[x]);
+        asm volatile("" : "+v"(e[x]));
+      }
+#pragma unroll
+      for (int x = from(i - 2); x < from(i - 1); ++x) {
+        sum[x >> 4] += e[x];
+        if (x & 1) {
+          const bf16x2 e2 = {(bf16_t)e[x - 1], (bf16_t)e[x]};
+          unsigned u = __builtin_bit_cast(unsigned, e2);
+          asm volatile("" : "+v"(u));      // rounded here, not behind the test of the sum where it is next used
+          const bf16x2 r2 = __builtin_bit_cast(bf16x2, u);
+          now.v[x >> 4][(x & 15) >> 3][(x & 7) - 1] = r2[0];
+          now.v[x >> 4][(x & 15) >> 3][x & 7] = r2[1];
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (__builtin_amdgcn_ballot_w64(!(sum[0] < kSumLimit) || !(sum[1] < kSumLimit)) != 0) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        float m = cur.v[rb][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, cur.v[rb][i]);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+        m = fmaxf(ref[rb], fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * p.sl2);
+        const float use = m == -INFINITY ? 0.f : m;                 // a row that has seen no key yet: weights 2^-inf = 0
+        const float alpha = __builtin_amdgcn_exp2f(ref[rb] - use);
+        ref[rb] = m;
+        l_run[rb] *= alpha;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[rb][cb][i] *= alpha;
+        sum[rb] = weights(cur.v[rb], -use, now.v[rb]);
+      }
     }
+    l_run[0] += sum[0];
+    l_run[1] += sum[1];
+  };
+
+  // Tile t lies in LDS buffer t % 3.  Its first half's weights are formed while its second half's scores run, and so on.  Tile t + 1 goes
+  // to LDS before the barrier in the middle of tile t, from which on nobody reads tile t - 1's buffer.
+  if (tiles > 0) {
+    Scores s0, s1;
+    Weights w0, w1;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w1.v[rb][j][i] = (bf16_t)0.f;
+    auto meet = [&]() __attribute__((always_inline)) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    ld.load(0);
+    unsigned groups_now = ld.groups;
+    ld.store(smem, vring);
+    ld.load(1);
+    unsigned groups_next = ld.groups;
+    // the values "before tile 0" have weight zero, so that they must be finite: the third buffer's second half
+    for (int e = threadIdx.x; e < HALF / 16; e += 256) *reinterpret_cast<u32x4 *>(vring + 2 * C::TILE_B + HALF + e * 16) = u32x4{0, 0, 0, 0};
+    meet();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 kf = k_fragment(ks, 0);
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) s0.v[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, qf[rb][ks]), ks == 0 ? zero : s0.v[rb], 0, 0, 0);
+    }
+    auto last_values = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const bf16x8 vf = v_fragment(j, cb, at);
+#pragma unroll
+          for (int rb = 0; rb < 2; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, w1.v[rb][j], o[rb][cb], 0, 0, 0);
+        }
+    };
+    int b0 = 0, b1 = C::TILE_B, b2 = 2 * C::TILE_B;      // buffers of tiles t, t + 1 and t - 1
+    for (int t = 0; t < tiles; ++t) {
+      const int key0 = kb + t * TK;
+      ld.aim(t + 2);
+      step(key0, groups_now & 3, s0, s1, w1, w0, b0 + HALF, b2 + HALF, b1, std::true_type{});
+      meet();
+      step(key0 + 32, groups_now >> 2, s1, s0, w0, w1, b1, b0, 0, std::false_type{});
+      groups_now = groups_next;
+      groups_next = ld.groups;
+      const int b = b2;
+      b2 = b0;
+      b0 = b1;
+      b1 = b;
+    }
+    last_values(b2 + HALF);
+  }
+
+#pragma unroll
+  for (int rb = 0; rb < 2; ++rb) {
+    const float l = l_run[rb] + __shfl_xor(l_run[rb], 32, kWave);
+    if (!row_ok[rb]) continue;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int64_t row = w.q0 + tok[rb];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = cb * 32 + 8 * g + 4 * hi;
+        if (c < dh) put4<T>(a, w.sp, row, head[rb], c, inv, o[rb][cb][4 * g], o[rb][cb][4 * g + 1], o[rb][cb][4 * g + 2], o[rb][cb][4 * g + 3]);
+      }
+    if (hi == 0) put_stats(a, w.sp, row, head[rb], ref[rb], l);
   }
 }
 
@@ -547,12 +849,35 @@ hipError_t launch_shape(const RowsAttn &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Few rows per sequence on average: the key kernel.
-bool few_rows(int total_q, int n_seqs, int group) { return (int64_t)total_q * group <= (int64_t)n_seqs * 32; }
+template <int DHP, bool PAGED>
+hipError_t launch_wide(const RowsAttn &a, hipStream_t s) {
+  constexpr int smem = 6 * Tile<bf16_t, DHP, 4, 1>::TILE_B;
+  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, PAGED>, smem>(); e != hipSuccess) return e;
+  RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
+  p.slots = (int)((int64_t)a.total_q * p.group / 256) + a.n_seqs;
+  attn_rows_wide_kernel<DHP, PAGED><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, smem, s>>>(p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
+  attn_rows_join_kernel<bf16_t><<<dim3((unsigned)(((int64_t)a.total_q * a.n_heads + 3) / 4)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// Which kernel: few rows per sequence on average: the key kernel; bf16 with a workgroup of 256 rows for every CU: the wide
+// one; else tiles for 128 rows.
+enum Shape { KEYS, TILES, WIDE };
+Shape pick_shape(int dt, int total_q, int n_seqs, int group, int kv_heads) {
+  const int64_t rows = (int64_t)total_q * group;
+  if (rows <= (int64_t)n_seqs * 32) return KEYS;
+  return dt == DT_BF16 && rows / 256 * kv_heads >= 256 ? WIDE : TILES;
+}
 
 template <typename T, int DHP, bool PAGED>
 hipError_t launch_rows_of(const RowsAttn &a, hipStream_t s) {
-  return few_rows(a.total_q, a.n_seqs, a.n_heads / a.kv_heads) ? launch_shape<T, DHP, PAGED, 1, 4>(a, s) : launch_shape<T, DHP, PAGED, 4, 1>(a, s);
+  const Shape shape = pick_shape(a.dt, a.total_q, a.n_seqs, a.n_heads / a.kv_heads, a.kv_heads);
+  if (shape == KEYS) return launch_shape<T, DHP, PAGED, 1, 4>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    if (shape == WIDE) return launch_wide<DHP, PAGED>(a, s);
+  }
+  return launch_shape<T, DHP, PAGED, 4, 1>(a, s);
 }
 template <typename T, bool PAGED>
 hipError_t launch_dim(const RowsAttn &a, hipStream_t s) {
@@ -565,12 +890,12 @@ hipError_t launch_dim(const RowsAttn &a, hipStream_t s) {
 
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
   const int group = n_heads / kv_heads;
-  const bool few = few_rows(total_q, n_seqs, group);
-  const int rows = few ? 32 : 128;
+  const Shape shape = pick_shape(dt, total_q, n_seqs, group, kv_heads);
+  const int rows = shape == KEYS ? 32 : shape == WIDE ? 256 : 128;
   // workgroups without chunks; chunks fill the chip a few times over, none shorter than four tiles' worth of keys
   const int64_t wgs = ((int64_t)total_q * group / rows + n_seqs) * kv_heads;
   const int64_t want = 1024;
-  int64_t splits = (want + wgs - 1) / wgs;
+  int64_t splits = shape == WIDE ? 1 : (want + wgs - 1) / wgs;
   const int64_t cap = max_kv / 512 > 1 ? max_kv / 512 : 1;
   if (splits > cap) splits = cap;
   if (splits > 256) splits = 256;
