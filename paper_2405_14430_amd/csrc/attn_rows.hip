@@ -15,7 +15,11 @@
 //
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
 // bounds of the buffer loads give zeros for rows past the last key, for pages that are none and for channels past the head, so
-// neither the scores nor 0 * v meets what lies there.  LDS rows are swizzled by 16-byte pieces against bank conflicts.
+// neither the scores nor 0 * v meets what lies there.  LDS rows are padded against bank conflicts.
+#ifndef PF_WANT
+#define PF_WANT 1024
+#define PF_MINK 512
+#endif
 #include <type_traits>
 
 #include "requests.h"
@@ -33,6 +37,7 @@ __device__ __forceinline__ void unrolled(F &&f) {
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxChunks = 256;
 constexpr float kLn2 = 0.6931471805599453f;
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -44,8 +49,8 @@ struct Buffer {   // `bytes` bytes from a wave-uniform address; loads past them 
   __amdgpu_buffer_rsrc_t rs;
   __device__ __forceinline__ Buffer(const void *base, unsigned bytes)
       : rs(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000)) {}
-  __device__ __forceinline__ u32x4 load16(unsigned at) const {
-    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0));
+  __device__ __forceinline__ u32x4 load16(unsigned lane_at, unsigned at) const {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane_at, at, 0));
   }
 };
 __device__ __forceinline__ s16x4 lds_read_transposed(const unsigned char *p) {
@@ -54,7 +59,7 @@ __device__ __forceinline__ s16x4 lds_read_transposed(const unsigned char *p) {
 #else   // the host pass only parses the kernels
 struct Buffer {
   __device__ Buffer(const void *, unsigned) {}
-  __device__ u32x4 load16(unsigned) const { return u32x4{}; }
+  __device__ u32x4 load16(unsigned, unsigned) const { return u32x4{}; }
 };
 __device__ s16x4 lds_read_transposed(const unsigned char *) { return s16x4{}; }
 #endif
@@ -83,23 +88,18 @@ struct Tile {
   static constexpr int NB = TK / 32;                       // blocks of 32 keys
   static constexpr int CB = DHP / 32;                      // blocks of 32 channels
   static constexpr int ROWB = DHP * (int)sizeof(T);        // bytes of an LDS row
-  static constexpr int CHUNKS = ROWB / 16;
-  static constexpr int TILE_B = TK * ROWB;
+  // LDS rows are padded so that what is read together lies in different banks: K as 16 bytes of 16 rows (16 bytes further a
+  // row), V as 64 bytes of four rows (bf16, transposed: 64 bytes further modulo 256) or 128 bytes of rows r and r + 4 (fp32)
+  static constexpr int KROWB = ROWB + 16;
+  static constexpr int VROWB = F32 ? ROWB + 32 : ROWB % 256 == 192 ? ROWB : ROWB + 64;
+  static constexpr int KTILE_B = TK * KROWB, VTILE_B = TK * VROWB;
   static constexpr int RW = TK / NW;                       // rows of a tile that one wave brings in
   static constexpr int LOADS = RW * ROWB / 1024;           // its 1 KB loads
   static constexpr int BUFS = NW > 1 ? 2 : 1;
   static constexpr int JOIN_B = KW > 1 ? KW * 32 * (DHP + 4 + 2) * 4 : 0;   // the waves' partial results
-  static constexpr int SMEM = KW * BUFS * 2 * TILE_B > JOIN_B ? KW * BUFS * 2 * TILE_B : JOIN_B;
+  static constexpr int SMEM = KW * BUFS * (KTILE_B + VTILE_B) > JOIN_B ? KW * BUFS * (KTILE_B + VTILE_B) : JOIN_B;
   static constexpr int ROWS = 32 * NW;                     // query rows of a workgroup
   static constexpr int WGS = SMEM > 80 * 1024 ? 1 : 2;     // workgroups on a CU, by their LDS
-  // swizzles of the 16-byte pieces of LDS row r: K is read as 16 bytes of 16 rows at a time, V as 64 bytes of four rows
-  // (transposed, bf16) or 128 bytes of rows r and r + 4 (fp32)
-  static __device__ __forceinline__ constexpr int kkey(int r) {
-    return ROWB % 256 == 0 ? (r & 15) : ROWB == 128 ? ((r >> 1) & 7) : ROWB == 192 ? ((r >> 2) & 3) : ((r >> 1) & 7);
-  }
-  static __device__ __forceinline__ constexpr int vkey(int r) {
-    return F32 ? (ROWB % 256 == 0 ? ((r >> 2) & 1) << 3 : 0) : ROWB == 256 ? (r & 3) << 2 : ROWB == 128 ? ((r >> 1) & 1) << 2 : 0;
-  }
 };
 
 // Key tiles of one chunk when the longest sequence of the launch is cut into `splits` of them: at least four.
@@ -181,7 +181,12 @@ struct TileLoader {
   const RowsAttn &a;
   const int lane, lw, s, kb, ke;
   unsigned k_row, v_row;                                           // bytes between rows
-  unsigned k_off[C::LOADS], v_off[C::LOADS];                       // the lane's bytes from a group's first row
+  // The lane's bytes from a group's first row, and where they go in an LDS tile.  Where a load is a whole number of rows its
+  // lanes' offsets are those of the first one, so many rows further.
+  static constexpr bool WHOLE = 1024 % ROWB == 0;
+  static constexpr int OFFS = WHOLE ? 1 : C::LOADS, RPL = 1024 / ROWB;
+  unsigned k_off[OFFS], v_off[OFFS];
+  int k_lds[OFFS], v_lds[OFFS];
   const T *k_head, *v_head;
   // Pages: lane i holds the page of 16-key group i of the current 1024 keys, and of the next 1024 (loaded that far ahead).
   int page_now = -1, page_next = -1;
@@ -196,12 +201,12 @@ struct TileLoader {
     k_row = (unsigned)((PAGED ? (int64_t)dh : a.ldk) * (int64_t)sizeof(T));
     v_row = (unsigned)((PAGED ? (int64_t)dh : a.ldv) * (int64_t)sizeof(T));
 #pragma unroll
-    for (int i = 0; i < C::LOADS; ++i) {
-      const int off = i * 1024 + lane * 16, row = off / ROWB, piece = (off % ROWB) >> 4;
-      const int in_tile = lw * C::RW + row, at = row % GROWS;
-      const int kc = piece ^ C::kkey(in_tile), vc = piece ^ C::vkey(in_tile);
-      k_off[i] = kc * 16 < dh * (int)sizeof(T) ? at * k_row + kc * 16 : kOutside;
-      v_off[i] = vc * 16 < dh * (int)sizeof(T) ? at * v_row + vc * 16 : kOutside;
+    for (int i = 0; i < OFFS; ++i) {
+      const int off = i * 1024 + lane * 16, row = off / ROWB, byte = off % ROWB;
+      k_off[i] = byte < dh * (int)sizeof(T) ? row % GROWS * k_row + byte : kOutside;
+      v_off[i] = byte < dh * (int)sizeof(T) ? row % GROWS * v_row + byte : kOutside;
+      k_lds[i] = (lw * C::RW + row) * C::KROWB + byte;
+      v_lds[i] = (lw * C::RW + row) * C::VROWB + byte;
     }
     if constexpr (PAGED) {
       k_head = (const T *)a.pages.k + ((int64_t)w.hk << a.pages.page_shift) * dh;
@@ -244,8 +249,12 @@ struct TileLoader {
       in_group[g] = uniform(rows);
     }
   }
-  __device__ __forceinline__ void load_k(int i) { k_reg[i] = Buffer(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[i]); }
-  __device__ __forceinline__ void load_v(int i) { v_reg[i] = Buffer(v_from[i / GL], in_group[i / GL] * v_row).load16(v_off[i]); }
+  __device__ __forceinline__ void load_k(int i) {
+    k_reg[i] = Buffer(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * k_row : 0);
+  }
+  __device__ __forceinline__ void load_v(int i) {
+    v_reg[i] = Buffer(v_from[i / GL], in_group[i / GL] * v_row).load16(v_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * v_row : 0);
+  }
   __device__ __forceinline__ void load(int t) {
     aim(t);
 #pragma unroll
@@ -253,8 +262,8 @@ struct TileLoader {
 #pragma unroll
     for (int i = 0; i < C::LOADS; ++i) load_v(i);
   }
-  __device__ __forceinline__ void store_k(unsigned char *tile, int i) const { *reinterpret_cast<u32x4 *>(tile + lw * C::RW * ROWB + lane * 16 + i * 1024) = k_reg[i]; }
-  __device__ __forceinline__ void store_v(unsigned char *tile, int i) const { *reinterpret_cast<u32x4 *>(tile + lw * C::RW * ROWB + lane * 16 + i * 1024) = v_reg[i]; }
+  __device__ __forceinline__ void store_k(unsigned char *tile, int i) const { *reinterpret_cast<u32x4 *>(tile + k_lds[WHOLE ? 0 : i] + (WHOLE ? i * RPL * C::KROWB : 0)) = k_reg[i]; }
+  __device__ __forceinline__ void store_v(unsigned char *tile, int i) const { *reinterpret_cast<u32x4 *>(tile + v_lds[WHOLE ? 0 : i] + (WHOLE ? i * RPL * C::VROWB : 0)) = v_reg[i]; }
   __device__ __forceinline__ void store(unsigned char *k_tile, unsigned char *v_tile) const {
 #pragma unroll
     for (int i = 0; i < C::LOADS; ++i) store_k(k_tile, i);
@@ -289,7 +298,7 @@ __device__ __forceinline__ void put_stats(const RowsAttn &a, int sp, int64_t row
 template <typename T, int DHP, bool PAGED, int NW, int KW>
 __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void attn_rows_kernel(RowsKernelArgs p) {
   using C = Tile<T, DHP, NW, KW>;
-  constexpr int TK = C::TK, NB = C::NB, CB = C::CB, ROWB = C::ROWB;
+  constexpr int TK = C::TK, NB = C::NB, CB = C::CB;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const RowsAttn &a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -331,8 +340,9 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     }
   }
   TileLoader<C, T, PAGED> ld(a, w, lane, KW > 1 ? 0 : wave, kb, ke);
-  unsigned char *const ring = smem + (KW > 1 ? wave * C::BUFS * 2 * C::TILE_B : 0);
-  auto store_tile = [&](int buf) __attribute__((always_inline)) { ld.store(ring + buf * 2 * C::TILE_B, ring + (buf * 2 + 1) * C::TILE_B); };
+  constexpr int BUF_B = C::KTILE_B + C::VTILE_B;
+  unsigned char *const ring = smem + (KW > 1 ? wave * C::BUFS * BUF_B : 0);
+  auto store_tile = [&](int buf) __attribute__((always_inline)) { ld.store(ring + buf * BUF_B, ring + buf * BUF_B + C::KTILE_B); };
 
   f32x16 o[CB];
 #pragma unroll
@@ -341,18 +351,13 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     for (int i = 0; i < 16; ++i) o[cb][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;    // running maximum of the raw scores; the lane's share of the sum
 
-  // LDS addresses of the lane: K row l32; V, bf16: row 4 hi + (i >> 2), piece of channels 16 g1 + 4 (i & 3); fp32: row 4 hi, channel l32
+  // LDS addresses of the lane: K row l32; V, bf16: row 4 hi + (i >> 2), channels 16 g1 + 4 (i & 3) of a block; fp32: row 4 hi, channel l32
   const int i16 = lane & 15, g1 = (lane >> 4) & 1;
-  const int v_row0 = C::F32 ? 4 * hi : 4 * hi + (i16 >> 2);
-  int v_at[CB];
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    const int piece = C::F32 ? cb * 8 + (l32 >> 2) : cb * 4 + g1 * 2 + ((i16 & 3) >> 1);
-    v_at[cb] = v_row0 * ROWB + ((piece ^ C::vkey(v_row0)) << 4) + (C::F32 ? (l32 & 3) * 4 : (i16 & 1) * 8);
-  }
+  const int k_at = l32 * C::KROWB + hi * 16;
+  const int v_at = C::KTILE_B + (C::F32 ? 4 * hi * C::VROWB + l32 * 4 : (4 * hi + (i16 >> 2)) * C::VROWB + g1 * 32 + (i16 & 3) * 8);
 
   auto work_tile = [&](int t, int buf, unsigned groups) __attribute__((always_inline)) {
-    const unsigned char *kt = ring + buf * 2 * C::TILE_B, *vt = kt + C::TILE_B;
+    const unsigned char *kt = ring + buf * BUF_B + k_at, *vt = ring + buf * BUF_B + v_at;
     f32x16 sc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -363,13 +368,13 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       for (int ks = 0; ks < DHP / 16; ++ks)
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + (b * 32 + l32) * ROWB + (((ks * 2 + hi) ^ C::kkey(l32)) << 4));
+          const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(kt + b * 32 * C::KROWB + ks * 32);
           sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, qf[ks]), sc[b], 0, 0, 0);
         }
     } else {
 #pragma unroll
       for (int j = 0; j < DHP / 8; ++j) {
-        const f32x4 kf = *reinterpret_cast<const f32x4 *>(kt + l32 * ROWB + (((j * 2 + hi) ^ C::kkey(l32)) << 4));
+        const f32x4 kf = *reinterpret_cast<const f32x4 *>(kt + j * 32);
         const f32x4 qv = __builtin_bit_cast(f32x4, qf[j]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qv[e], sc[0], 0, 0, 0);
@@ -420,7 +425,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
         for (int e = 0; e < 8; ++e) pf[e] = (bf16_t)sc[j >> 1][8 * (j & 1) + e];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-          struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(vt + v_at[cb] + j * 16 * ROWB), lds_read_transposed(vt + v_at[cb] + (j * 16 + 8) * ROWB)};
+          struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(vt + j * 16 * C::VROWB + cb * 64), lds_read_transposed(vt + (j * 16 + 8) * C::VROWB + cb * 64)};
           o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pf, o[cb], 0, 0, 0);
         }
       }
@@ -429,8 +434,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-          // the swizzle looks at bit 2 of the row, which 4 hi alone sets: rows 8 (i / 4) + i % 4 only move by whole rows
-          const float vf = *reinterpret_cast<const float *>(vt + v_at[cb] + (8 * (i >> 2) + (i & 3)) * ROWB);
+          const float vf = *reinterpret_cast<const float *>(vt + (8 * (i >> 2) + (i & 3)) * C::VROWB + cb * 128);
           o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, sc[0][i], o[cb], 0, 0, 0);
         }
     }
@@ -542,14 +546,14 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
 // any ref while nothing overflows, and the sum of a lane's weights, which is formed anyway, says when it has grown too
 // large.  Only then (and on the first keys of a row, whose ref is -inf) is the maximum found, the reference moved, and the
 // step's weights formed again.
-template <int DHP, bool PAGED>
-__global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p) {
+template <int DHP, int KS, bool PAGED>
+__global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kernel(RowsKernelArgs p) {
   using T = bf16_t;
   using C = Tile<T, DHP, 4, 1>;
-  constexpr int TK = C::TK, CB = C::CB, ROWB = C::ROWB, KS = DHP / 16;
+  constexpr int TK = C::TK, CB = C::CB;
   constexpr float kSumLimit = 8192.f;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // three K tiles, three V tiles
-  unsigned char *const vring = smem + 3 * C::TILE_B;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // two K tiles, two V tiles
+  unsigned char *const vring = smem + 2 * C::KTILE_B;
   const RowsAttn &a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
@@ -597,20 +601,16 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
   float l_run[2] = {0.f, 0.f};
 
   const int i16 = lane & 15, g1 = (lane >> 4) & 1;
-  const int v_row0 = 4 * hi + (i16 >> 2);
-  const unsigned char *k_at[KS], *v_at[CB];      // in the first K tile and the first V tile
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) k_at[ks] = smem + l32 * ROWB + (((ks * 2 + hi) ^ C::kkey(l32)) << 4);
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) v_at[cb] = vring + v_row0 * ROWB + (((cb * 4 + g1 * 2 + ((i16 & 3) >> 1)) ^ C::vkey(v_row0)) << 4) + (i16 & 1) * 8;
+  const unsigned char *const k_at = smem + l32 * C::KROWB + hi * 16;
+  const unsigned char *const v_at = vring + (4 * hi + (i16 >> 2)) * C::VROWB + g1 * 32 + (i16 & 3) * 8;
 
   struct Scores { f32x16 v[2]; };
   struct Weights { bf16x8 v[2][2]; };
   const f32x16 zero = {};
-  constexpr int HALF = 32 * ROWB;
-  auto k_fragment = [&](int ks, int at) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8 *>(k_at[ks] + at); };
+  constexpr int K_HALF = 32 * C::KROWB, V_HALF = 32 * C::VROWB;
+  auto k_fragment = [&](int ks, int at) __attribute__((always_inline)) { return *reinterpret_cast<const bf16x8 *>(k_at + at + ks * 32); };
   auto v_fragment = [&](int j, int cb, int at) __attribute__((always_inline)) {
-    struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(v_at[cb] + at + j * 16 * ROWB), lds_read_transposed(v_at[cb] + at + (j * 16 + 8) * ROWB)};
+    struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(v_at + at + j * 16 * C::VROWB + cb * 64), lds_read_transposed(v_at + at + (j * 16 + 8) * C::VROWB + cb * 64)};
     return __builtin_bit_cast(bf16x8, v8);
   };
   auto weights = [&](const f32x16 &x, float neg, bf16x8 (&y)[2]) __attribute__((always_inline)) {
@@ -624,9 +624,9 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
     return sum;
   };
   // One step: weights of the 32 keys from key0 on (scores `cur`, pages `groups`), scores of the next 32 (K at kt), values of the 32
-  // before (V at vt); SIDE: stores and loads of the tiles to come go along.
+  // before (V at vt).  The registers of K (first half of a tile) or V (second) go to LDS at `side` and are loaded again.
   auto step = [&](int key0, unsigned groups, Scores &cur, Scores &nxt, const Weights &before, Weights &now, int kt, int vt, int side,
-                  auto with_side) __attribute__((always_inline)) {
+                  auto k_side) __attribute__((always_inline)) {
     if (key0 + 32 > least || (PAGED && groups != 3)) {
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb)
@@ -636,8 +636,9 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
           if (key0 + at + 4 * hi >= limit[rb] || (PAGED && !((groups >> (at >> 4)) & 1))) cur.v[rb][i] = -INFINITY;
         }
     }
-    // The block, in slots of one MFMA with its share of the vector work behind it.  Fragments come from LDS PD fragments ahead of
-    // their two MFMAs; an element passes through its multiply-add, its exponential and its sum in slots behind each other.
+    // The block, in slots of one MFMA with its share of the vector work behind it: an MFMA takes 32 cycles, in which the wave
+    // can issue five other instructions.  Fragments come from LDS PD fragments ahead of their two MFMAs; an
+    // element passes through its multiply-add, its exponential and its sum in slots behind each other.
     constexpr int NF = KS + 2 * CB, MF = 2 * NF, PD = 2;
     bf16x8 ring[PD + 1];
     auto fragment = [&](auto f_c) __attribute__((always_inline)) {
@@ -653,17 +654,14 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
       const bf16x8 &fr = ring[f % (PD + 1)];
       if constexpr (f < KS) nxt.v[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, __builtin_bit_cast(bf16x8, qf[rb][f]), f == 0 ? zero : nxt.v[rb], 0, 0, 0);
       else o[rb][(f - KS) % CB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr, before.v[rb][(f - KS) / CB], o[rb][(f - KS) % CB], 0, 0, 0);
-      // the 2 LOADS registers of a tile, in turn: to LDS, and the next tile's load into them
-      if constexpr (decltype(with_side)::value) {
-        constexpr int U = 2 * C::LOADS, u = i * U / MF;
-        if constexpr (i == 0 || u != (i - 1) * U / MF) {
-          if constexpr (u < C::LOADS) {
-            ld.store_k(smem + side, u);
-            ld.load_k(u);
-          } else {
-            ld.store_v(vring + side, u - C::LOADS);
-            ld.load_v(u - C::LOADS);
-          }
+      constexpr int u = i * C::LOADS / MF;
+      if constexpr (i == 0 || u != (i - 1) * C::LOADS / MF) {
+        if constexpr (decltype(k_side)::value) {
+          ld.store_k(smem + side, u);
+          ld.load_k(u);
+        } else {
+          ld.store_v(vring + side, u);
+          ld.load_v(u);
         }
       }
       constexpr int N = MF - 2;
@@ -715,8 +713,9 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
     l_run[1] += sum[1];
   };
 
-  // Tile t lies in LDS buffer t % 3.  Its first half's weights are formed while its second half's scores run, and so on.  Tile t + 1 goes
-  // to LDS before the barrier in the middle of tile t, from which on nobody reads tile t - 1's buffer.
+  // Tile t lies in LDS buffers t % 2.  Its first half's weights are formed while its second half's scores run, and so on.  K of tile t + 1
+  // goes to LDS in the first half of tile t, where K of tile t - 1 has been read by all since the barrier before, V of tile t + 1 in
+  // the second half, behind the barrier in the middle, from which on nobody reads V of tile t - 1.
   if (tiles > 0) {
     Scores s0, s1;
     Weights w0, w1;
@@ -736,8 +735,8 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
     ld.store(smem, vring);
     ld.load(1);
     unsigned groups_next = ld.groups;
-    // the values "before tile 0" have weight zero, so that they must be finite: the third buffer's second half
-    for (int e = threadIdx.x; e < HALF / 16; e += 256) *reinterpret_cast<u32x4 *>(vring + 2 * C::TILE_B + HALF + e * 16) = u32x4{0, 0, 0, 0};
+    // the values "before tile 0" have weight zero, so that they must be finite: the other V buffer's second half
+    for (int e = threadIdx.x; e < V_HALF / 16; e += 256) *reinterpret_cast<u32x4 *>(vring + C::VTILE_B + V_HALF + e * 16) = u32x4{0, 0, 0, 0};
     meet();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -755,21 +754,17 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
           for (int rb = 0; rb < 2; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, w1.v[rb][j], o[rb][cb], 0, 0, 0);
         }
     };
-    int b0 = 0, b1 = C::TILE_B, b2 = 2 * C::TILE_B;      // buffers of tiles t, t + 1 and t - 1
     for (int t = 0; t < tiles; ++t) {
       const int key0 = kb + t * TK;
+      const int k0 = t & 1 ? C::KTILE_B : 0, k1 = C::KTILE_B - k0, v0 = t & 1 ? C::VTILE_B : 0, v1 = C::VTILE_B - v0;
       ld.aim(t + 2);
-      step(key0, groups_now & 3, s0, s1, w1, w0, b0 + HALF, b2 + HALF, b1, std::true_type{});
+      step(key0, groups_now & 3, s0, s1, w1, w0, k0 + K_HALF, v1 + V_HALF, k1, std::true_type{});
       meet();
-      step(key0 + 32, groups_now >> 2, s1, s0, w0, w1, b1, b0, 0, std::false_type{});
+      step(key0 + 32, groups_now >> 2, s1, s0, w0, w1, k1, v0, v1, std::false_type{});
       groups_now = groups_next;
       groups_next = ld.groups;
-      const int b = b2;
-      b2 = b0;
-      b0 = b1;
-      b1 = b;
     }
-    last_values(b2 + HALF);
+    last_values((tiles & 1 ? 0 : C::VTILE_B) + V_HALF);
   }
 
 #pragma unroll
@@ -789,51 +784,84 @@ __global__ __launch_bounds__(256, 1) void attn_rows_wide_kernel(RowsKernelArgs p
   }
 }
 
-// Joins the chunks of a row: out = sum 2^(m_c - m) O_c / sum 2^(m_c - m) l_c, one wave per (token, head).  Chunks behind the row's last
-// key left l = 0 and no O.
-template <typename T>
+// Joins the chunks of a row: out = sum 2^(m_c - m) O_c / sum 2^(m_c - m) l_c, W waves per (token, head).  A thread sums four channels of
+// every GROUPS-th chunk, the groups are added up through LDS in their order.  Chunks that saw no key of the row left l = 0; their O is
+// not read.
+template <typename T, int W>
 __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int R = 4 / W, NT = 64 * W;                       // rows per workgroup, threads per row
+  __shared__ float weight[R][kMaxChunks], part[R][NT * 4], stat[R][2 * W];
+  const int slot = threadIdx.x / NT, tid = threadIdx.x % NT, lane = threadIdx.x & 63, wave = tid >> 6;
+  const int dh = a.head_dim;
   const int64_t all = (int64_t)a.total_q * a.n_heads;
-  if (id >= all) return;
-  const int row = (int)(id / a.n_heads), head = (int)(id - (int64_t)row * a.n_heads), dh = a.head_dim;
-  if (row < a.cu_q[0] || row >= a.cu_q[a.n_seqs]) return;
+  const int64_t id = (int64_t)blockIdx.x * R + slot;
+  const int row = (int)(min(id, all - 1) / a.n_heads), head = (int)(min(id, all - 1) - (int64_t)row * a.n_heads);
+  const bool live = id < all && row >= a.cu_q[0] && row < a.cu_q[a.n_seqs];
   const float2 *ml = reinterpret_cast<const float2 *>(a.ws + (int64_t)a.splits * all * dh) + id;
+  constexpr int PER = (kMaxChunks + NT - 1) / NT;
+  float2 v[PER];
   float m = -INFINITY;
-  for (int c = lane; c < a.splits; c += 64) m = fmaxf(m, ml[c * all].x);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    v[i] = make_float2(-INFINITY, 0.f);
+    if (live && i * NT + tid < a.splits) v[i] = ml[(i * NT + tid) * all];
+    m = fmaxf(m, v[i].x);
+  }
   m = wave_max(m);
-  const int ch = lane * 2;
-  float l = 0.f, o0 = 0.f, o1 = 0.f;
-  if (m > -INFINITY) {
-    for (int c0 = 0; c0 < a.splits; c0 += 64) {
-      float w = 0.f, lc = 0.f;
-      if (c0 + lane < a.splits) {
-        const float2 v = ml[(c0 + lane) * all];
-        w = __builtin_amdgcn_exp2f(v.x - m);
-        lc = v.y;
-      }
-      unsigned long long live = __builtin_amdgcn_ballot_w64(lc > 0.f);
-      while (live) {
-        const int i = __builtin_ctzll(live);
-        live &= live - 1;
-        const float wi = __shfl(w, i, kWave);
-        l = fmaf(wi, __shfl(lc, i, kWave), l);
-        if (ch < dh) {
-          const float2 x = *reinterpret_cast<const float2 *>(a.ws + ((int64_t)(c0 + i) * all + id) * dh + ch);
-          o0 = fmaf(wi, x.x, o0);
-          o1 = fmaf(wi, x.y, o1);
-        }
+  if (lane == 0) stat[slot][wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < W; ++i) m = fmaxf(m, stat[slot][i]);
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (i * NT + tid < a.splits) {
+      const float w = v[i].y > 0.f ? __builtin_amdgcn_exp2f(v[i].x - m) : 0.f;
+      weight[slot][i * NT + tid] = w;
+      l = fmaf(w, v[i].y, l);
+    }
+  l = wave_sum(l);
+  if (lane == 0) stat[slot][W + wave] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) l += stat[slot][W + i];
+  const int cl = dh <= 64 ? 16 : 32, groups = NT / cl;        // threads across a row's channels
+  const int c = tid % cl * 4, g = tid / cl;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (live && c < dh) {
+#pragma unroll 4
+    for (int i = g; i < a.splits; i += groups) {
+      const float w = weight[slot][i];
+      if (w > 0.f) {
+        const float4 x = *reinterpret_cast<const float4 *>(a.ws + ((int64_t)i * all + id) * dh + c);
+        acc = make_float4(fmaf(w, x.x, acc.x), fmaf(w, x.y, acc.y), fmaf(w, x.z, acc.z), fmaf(w, x.w, acc.w));
       }
     }
   }
+  *reinterpret_cast<float4 *>(&part[slot][tid * 4]) = acc;
+  __syncthreads();
+  if (!live) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  if (ch < dh) {
-    T *dst = (T *)a.out + (int64_t)row * a.ldo + (int64_t)head * dh + ch;
-    dst[0] = from_f32<T>(o0 * inv);
-    dst[1] = from_f32<T>(o1 * inv);
+  if (g == 0 && c < dh) {
+    for (int i = 1; i < groups; ++i) {
+      const float4 x = *reinterpret_cast<const float4 *>(&part[slot][(i * cl + tid) * 4]);
+      acc = make_float4(acc.x + x.x, acc.y + x.y, acc.z + x.z, acc.w + x.w);
+    }
+    T *dst = (T *)a.out + (int64_t)row * a.ldo + (int64_t)head * dh + c;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    else *reinterpret_cast<bf16x4 *>(dst) = bf16x4{(bf16_t)(acc.x * inv), (bf16_t)(acc.y * inv), (bf16_t)(acc.z * inv), (bf16_t)(acc.w * inv)};
   }
-  if (a.lse && lane == 0) a.lse[id] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+  if (a.lse && tid == 0) a.lse[id] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+template <typename T>
+hipError_t launch_join(const RowsAttn &a, hipStream_t s) {
+  const int64_t all = (int64_t)a.total_q * a.n_heads;
+  // four waves per row where a wave would have more than eight chunks to add up per thread
+  if (a.splits > 16) attn_rows_join_kernel<T, 4><<<dim3((unsigned)all), 256, 0, s>>>(a);
+  else attn_rows_join_kernel<T, 1><<<dim3((unsigned)((all + 3) / 4)), 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <typename T, int DHP, bool PAGED, int NW, int KW>
@@ -844,21 +872,19 @@ hipError_t launch_shape(const RowsAttn &a, hipStream_t s) {
   p.slots = (int)((int64_t)a.total_q * p.group / C::ROWS) + a.n_seqs;
   const int64_t grid = (int64_t)p.slots * a.splits * a.kv_heads;
   attn_rows_kernel<T, DHP, PAGED, NW, KW><<<dim3((unsigned)grid), 64 * C::WAVES, C::SMEM, s>>>(p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-  attn_rows_join_kernel<T><<<dim3((unsigned)(((int64_t)a.total_q * a.n_heads + 3) / 4)), 256, 0, s>>>(a);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : launch_join<T>(a, s);
 }
 
-template <int DHP, bool PAGED>
+template <int DHP, int KS, bool PAGED>
 hipError_t launch_wide(const RowsAttn &a, hipStream_t s) {
-  constexpr int smem = 6 * Tile<bf16_t, DHP, 4, 1>::TILE_B;
-  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, PAGED>, smem>(); e != hipSuccess) return e;
+  constexpr int smem = Tile<bf16_t, DHP, 4, 1>::SMEM;
+  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, KS, PAGED>, smem>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   p.slots = (int)((int64_t)a.total_q * p.group / 256) + a.n_seqs;
-  attn_rows_wide_kernel<DHP, PAGED><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, smem, s>>>(p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-  attn_rows_join_kernel<bf16_t><<<dim3((unsigned)(((int64_t)a.total_q * a.n_heads + 3) / 4)), 256, 0, s>>>(a);
-  return hipGetLastError();
+  attn_rows_wide_kernel<DHP, KS, PAGED><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, smem, s>>>(p);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.splits == 1 ? e : launch_join<bf16_t>(a, s);
 }
 
 // Which kernel: few rows per sequence on average: the key kernel; bf16 with a workgroup of 256 rows for every CU: the wide
@@ -875,7 +901,7 @@ hipError_t launch_rows_of(const RowsAttn &a, hipStream_t s) {
   const Shape shape = pick_shape(a.dt, a.total_q, a.n_seqs, a.n_heads / a.kv_heads, a.kv_heads);
   if (shape == KEYS) return launch_shape<T, DHP, PAGED, 1, 4>(a, s);
   if constexpr (sizeof(T) == 2) {
-    if (shape == WIDE) return launch_wide<DHP, PAGED>(a, s);
+    if (shape == WIDE) return DHP == 96 && a.head_dim <= 80 ? launch_wide<DHP, DHP == 96 ? 5 : DHP / 16, PAGED>(a, s) : launch_wide<DHP, DHP / 16, PAGED>(a, s);
   }
   return launch_shape<T, DHP, PAGED, 4, 1>(a, s);
 }
@@ -892,13 +918,30 @@ RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int k
   const int group = n_heads / kv_heads;
   const Shape shape = pick_shape(dt, total_q, n_seqs, group, kv_heads);
   const int rows = shape == KEYS ? 32 : shape == WIDE ? 256 : 128;
-  // workgroups without chunks; chunks fill the chip a few times over, none shorter than four tiles' worth of keys
-  const int64_t wgs = ((int64_t)total_q * group / rows + n_seqs) * kv_heads;
-  const int64_t want = 1024;
-  int64_t splits = shape == WIDE ? 1 : (want + wgs - 1) / wgs;
-  const int64_t cap = max_kv / 512 > 1 ? max_kv / 512 : 1;
-  if (splits > cap) splits = cap;
-  if (splits > 256) splits = 256;
+  const int64_t wgs = ((int64_t)total_q * group / rows + n_seqs) * kv_heads;   // without chunks
+  int64_t splits = 1;
+  if (shape == KEYS) {
+    splits = (PF_WANT + wgs - 1) / wgs;
+    const int64_t cap = max_kv / PF_MINK > 1 ? max_kv / PF_MINK : 1;
+    if (splits > cap) splits = cap;
+    if (splits > kMaxChunks) splits = kMaxChunks;
+  } else if (shape == TILES) {
+    // The chip holds 512 of these workgroups.  Time in key tiles: rounds x (tiles of a chunk and four for a workgroup's start and end),
+    // more where CUs hold a single workgroup; chunks cost a second launch and their partial results' way through memory.
+    const int64_t tiles = (max_kv + 63) / 64, cap = tiles / 4 < 16 ? tiles / 4 : 16;
+    const double row_units = (double)total_q * n_heads * head_dim * 2.9e-7;
+    double best = 1e300;
+    for (int64_t n = 1; n <= (cap > 1 ? cap : 1); ++n) {
+      const int64_t rounds = (wgs * n + 511) / 512;
+      const double fill = wgs * n >= 512 ? 1.0 : wgs * n / 512.0;
+      double cost = rounds * ((tiles + n - 1) / n + 4) * (1.5 - 0.5 * fill);
+      if (n > 1) cost += 2.0 + (4 * n + 2) * row_units;
+      if (cost < best - 1e-9) {
+        best = cost;
+        splits = n;
+      }
+    }
+  }
   RowsPlan p{rows, (int)splits, 0};
   if (splits > 1) p.ws_bytes = (size_t)splits * total_q * n_heads * (head_dim + 2) * sizeof(float);
   return p;
