@@ -7,6 +7,7 @@ library has not been built (python paper_2405_14430_amd/build.py, or __graft_ent
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -480,15 +481,15 @@ def _ints(name, t, shape, device):
     return t
 
 
-def _vectors(name, t, d, n_seqs, device):
-    """float [d], or [n_seqs, d] for a call with sequences; returns the stride between sequences."""
+def _vectors(name, t, d, n_seqs, index, device):
+    """float [d], or [n_seqs, d] for a call with sequences; returns the stride between sequences and the address."""
     if t is None:
-        return 0
-    _plain(name, t, torch.float32, device)
+        return 0, None
     shape = (d,) if n_seqs is None else (n_seqs, d)
-    if tuple(t.shape) != shape or (d > 1 and t.stride(-1) != 1):
-        raise PfError(-3, f"{name}: shape {tuple(t.shape)}, {shape} is needed")
-    return 0 if n_seqs in (None, 1) else t.stride(0)
+    if not (t.dtype is torch.float32 and t.get_device() == index and t.shape == shape and t.stride(-1) == 1):
+        _plain(name, t, torch.float32, device)
+        raise PfError(-3, f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, contiguous vectors {shape} are needed")
+    return 0 if n_seqs is None or n_seqs == 1 else t.stride(0), t.data_ptr()
 
 
 def _ld(t):
@@ -496,22 +497,28 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 8)
 
 
-class _on:
-    """Makes a tensor's GPU the current one for a launch."""
-    __slots__ = ("index", "before")
+# The checks above say what is wrong; a call of a few microseconds first asks these, which only say whether all is well.
+def _good_rows(t, dtype, index):
+    return t.dtype is dtype and t.get_device() == index and t.dim() == 2 and t.stride(1) == 1
 
-    def __init__(self, device):
-        self.index = device.index
 
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return C.c_void_p(torch.cuda.current_stream(self.index).cuda_stream)
+def _good_ints(t, shape, index):
+    return t.dtype is torch.int32 and t.get_device() == index and t.shape == shape and t.is_contiguous()
 
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+
+def _launch(index, fn, *args):
+    """Calls a C entry point, whose last argument is the stream, on GPU `index` and its current stream."""
+    if torch._C._cuda_getDevice() == index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if st != 0:
+        _raise(st)
+
+
+def _like(t, dtype=None):
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
 
 
 def make_rope(axis_dims, layout="interleaved", theta=1e4, scaling="none", factor=1.0, low=1.0, high=32.0, original_len=1,
@@ -536,24 +543,23 @@ def _heads(name, t, head_dim):
     return t.shape[1] // head_dim
 
 
-def _positions(rope, pos, tokens, device):
+def _positions(rope, pos, tokens, index, device):
     n = rope.n_axes
-    return _ints("pos", pos, (tokens,) if pos.dim() == 1 and n == 1 else (tokens, n), device)
+    if not (_good_ints(pos, (tokens, n), index) or (n == 1 and _good_ints(pos, (tokens,), index))):
+        _ints("pos", pos, (tokens,) if pos.dim() == 1 and n == 1 else (tokens, n), device)
 
 
 def pf_op_rope(x, rope, pos, head_dim, out=None):
     """x [tokens, heads * head_dim] with every head turned by its row's position(s); pos int32 [tokens, n_axes] (or [tokens] for
     one axis).  out may be x."""
-    _rows("x", x)
-    tokens, dev = x.shape[0], x.device
-    heads = _heads("x", x, head_dim)
-    _positions(rope, pos, tokens, dev)
-    out = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else _out("out", out, x.shape, x.dtype, dev)
-    with _on(dev) as stream:
-        st = load_library().pf_op_rope(_DT[x.dtype], C.byref(rope), pos.data_ptr(), x.data_ptr(), _ld(x), out.data_ptr(), _ld(out),
-                                       tokens, heads, head_dim, stream)
-    if st != 0:
-        _raise(st)
+    index, dt = x.get_device(), _DT.get(x.dtype)
+    if index < 0 or dt is None or not _good_rows(x, x.dtype, index):
+        _rows("x", x)
+    tokens, heads = x.shape[0], _heads("x", x, head_dim)
+    _positions(rope, pos, tokens, index, x.device)
+    out = _like(x) if out is None else _out("out", out, x.shape, x.dtype, x.device)
+    _launch(index, (_lib or load_library()).pf_op_rope, dt, C.byref(rope), pos.data_ptr(), x.data_ptr(), _ld(x), out.data_ptr(),
+            _ld(out), tokens, heads, head_dim)
     return out
 
 
@@ -581,79 +587,86 @@ class KvPages:
         n, self.kv_heads, self.page_size, self.head_dim = k.shape
         block = self.kv_heads * self.page_size * self.head_dim
         self.n_seqs, self.max_pages = table.shape
+        self.device, self.index = k.device, k.get_device()
         self.c = PfKvPages(k=k.data_ptr(), v=v.data_ptr(), k_page_stride=k.stride(0) if n > 1 else block,
                            v_page_stride=v.stride(0) if n > 1 else block, table=table.data_ptr(), n_pages=n,
                            page_size=self.page_size, kv_heads=self.kv_heads, head_dim=self.head_dim, n_seqs=self.n_seqs,
                            max_pages=self.max_pages)
+        self.ref = C.byref(self.c)
 
 
 def pf_op_kv_append(pages, k, v, cu, first, rope=None, pos=None, q=None, q_out=None):
     """Writes rows of k and v [tokens, kv_heads * head_dim] into the pages, row cu[s] + i of sequence s into slot first[s] + i, k
     turned by `rope` on the way; returns q turned likewise (None without q)."""
-    dt, dev = pages.k.dtype, pages.k.device
-    _rows("k", k, dt, dev)
-    _out("v", v, k.shape, dt, dev)
-    tokens = k.shape[0]
-    if k.shape[1] != pages.kv_heads * pages.head_dim:
-        raise PfError(-3, f"k: rows of {k.shape[1]} channels for {pages.kv_heads} heads of {pages.head_dim}")
-    _ints("cu", cu, (pages.n_seqs + 1,), dev)
-    _ints("first", first, (pages.n_seqs,), dev)
+    dt, dev, index = pages.k.dtype, pages.device, pages.index
+    if not (_good_rows(k, dt, index) and _good_rows(v, dt, index) and v.shape == k.shape and
+            _good_ints(cu, (pages.n_seqs + 1,), index) and _good_ints(first, (pages.n_seqs,), index)):
+        _rows("k", k, dt, dev)
+        _out("v", v, k.shape, dt, dev)
+        _ints("cu", cu, (pages.n_seqs + 1,), dev)
+        _ints("first", first, (pages.n_seqs,), dev)
+    tokens, width = k.shape
+    if width != pages.kv_heads * pages.head_dim:
+        raise PfError(-3, f"k: rows of {width} channels for {pages.kv_heads} heads of {pages.head_dim}")
     if rope is not None:
         if pos is None:
             raise PfError(-1, "pos")
-        _positions(rope, pos, tokens, dev)
-    heads = 0
-    if q is not None:
-        _rows("q", q, dt, dev)
+        _positions(rope, pos, tokens, index, dev)
+    if q is None:
+        if q_out is not None:
+            raise PfError(-1, "q_out without q")
+        q_args = (None, 0, None, 0, 0)
+    else:
+        if not _good_rows(q, dt, index):
+            _rows("q", q, dt, dev)
         if q.shape[0] != tokens:
             raise PfError(-3, f"q: {q.shape[0]} rows, k has {tokens}")
         heads = _heads("q", q, pages.head_dim)
-        q_out = torch.empty(q.shape, dtype=dt, device=dev) if q_out is None else _out("q_out", q_out, q.shape, dt, dev)
-    elif q_out is not None:
-        raise PfError(-1, "q_out without q")
-    with _on(dev) as stream:
-        st = load_library().pf_op_kv_append(
-            _DT[dt], C.byref(pages.c), k.data_ptr(), _ld(k), v.data_ptr(), _ld(v), cu.data_ptr(), first.data_ptr(), tokens,
-            None if rope is None else C.byref(rope), None if rope is None else pos.data_ptr(),
-            None if q is None else q.data_ptr(), 0 if q is None else _ld(q), None if q is None else q_out.data_ptr(),
-            0 if q is None else _ld(q_out), heads, stream)
-    if st != 0:
-        _raise(st)
+        q_out = _like(q) if q_out is None else _out("q_out", q_out, q.shape, dt, dev)
+        q_args = (q.data_ptr(), _ld(q), q_out.data_ptr(), _ld(q_out), heads)
+    _launch(index, (_lib or load_library()).pf_op_kv_append, _DT[dt], pages.ref, k.data_ptr(), _ld(k), v.data_ptr(), _ld(v),
+            cu.data_ptr(), first.data_ptr(), tokens, None if rope is None else C.byref(rope),
+            None if rope is None else pos.data_ptr(), *q_args)
     return q_out
 
 
+@functools.lru_cache(maxsize=1024)
+def _rows_ws_bytes(*sizes):
+    return load_library().pf_op_attention_rows_ws_bytes(*sizes)
+
+
 def _attention_buffers(q, heads, kv_heads, head_dim, n_seqs, max_kv, out, want_lse):
-    dev = q.device
-    out = torch.empty(q.shape, dtype=q.dtype, device=dev) if out is None else _out("out", out, q.shape, q.dtype, dev)
-    lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=dev) if want_lse else None
-    n = load_library().pf_op_attention_rows_ws_bytes(_DT[q.dtype], q.shape[0], n_seqs, heads, kv_heads, head_dim, max_kv)
-    return out, lse, torch.empty(n, dtype=torch.uint8, device=dev) if n else None, n
+    """out, lse, and (address of out, its row stride, address of lse, workspace, its bytes) for the call."""
+    out = _like(q) if out is None else _out("out", out, q.shape, q.dtype, q.device)
+    lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=q.device) if want_lse else None
+    n = _rows_ws_bytes(_DT[q.dtype], q.shape[0], n_seqs, heads, kv_heads, head_dim, max_kv)
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    return out, lse, ws, (out.data_ptr(), _ld(out), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), n)
 
 
 def pf_op_attention_packed(q, k, v, cu_q, cu_k, head_dim, causal=False, scale=None, out=None, want_lse=False):
     """Attention of packed sequences: q [total_q, heads * head_dim], k and v [total_k, kv_heads * head_dim], cu_q and cu_k int32
     [n_seqs + 1].  causal: the last query of a sequence sees all its keys, the one before all but one, ...  Returns out, or
     (out, lse) with lse float [total_q, heads]; rows of no sequence are not written."""
-    _rows("q", q)
-    _rows("k", k, q.dtype, q.device)
-    _out("v", v, k.shape, q.dtype, q.device)
+    index, dt = q.get_device(), q.dtype
+    n_seqs = cu_q.shape[0] - 1 if cu_q.dim() == 1 else -1
+    if not (index >= 0 and dt in _DT and n_seqs >= 0 and _good_rows(q, dt, index) and _good_rows(k, dt, index) and
+            _good_rows(v, dt, index) and v.shape == k.shape and _good_ints(cu_q, (n_seqs + 1,), index) and
+            _good_ints(cu_k, (n_seqs + 1,), index)):
+        _rows("q", q)
+        _rows("k", k, dt, q.device)
+        _out("v", v, k.shape, dt, q.device)
+        if n_seqs < 0:
+            raise PfError(-3, f"cu_q: shape {tuple(cu_q.shape)}, [n_seqs + 1] is needed")
+        _ints("cu_q", cu_q, (n_seqs + 1,), q.device)
+        _ints("cu_k", cu_k, (n_seqs + 1,), q.device)
     heads, kv_heads = _heads("q", q, head_dim), _heads("k", k, head_dim)
-    if cu_q.dim() != 1 or cu_q.shape[0] < 1:
-        raise PfError(-3, f"cu_q: shape {tuple(cu_q.shape)}, [n_seqs + 1] is needed")
-    n_seqs = cu_q.shape[0] - 1
-    _ints("cu_q", cu_q, (n_seqs + 1,), q.device)
-    _ints("cu_k", cu_k, (n_seqs + 1,), q.device)
     if scale is not None and not scale > 0:
         raise PfError(-3, f"scale: {scale}")
-    with _on(q.device) as stream:
-        out, lse, ws, ws_bytes = _attention_buffers(q, heads, kv_heads, head_dim, n_seqs, max(k.shape[0], 1), out, want_lse)
-        st = load_library().pf_op_attention_packed(
-            _DT[q.dtype], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k), v.data_ptr(), _ld(v), cu_q.data_ptr(), cu_k.data_ptr(),
-            n_seqs, q.shape[0], k.shape[0], heads, kv_heads, head_dim, 0.0 if scale is None else scale, int(causal),
-            out.data_ptr(), _ld(out), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes,
-            stream)
-    if st != 0:
-        _raise(st)
+    out, lse, ws, tail = _attention_buffers(q, heads, kv_heads, head_dim, n_seqs, max(k.shape[0], 1), out, want_lse)
+    _launch(index, (_lib or load_library()).pf_op_attention_packed, _DT[dt], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k),
+            v.data_ptr(), _ld(v), cu_q.data_ptr(), cu_k.data_ptr(), n_seqs, q.shape[0], k.shape[0], heads, kv_heads, head_dim,
+            0.0 if scale is None else scale, int(causal), *tail)
     return (out, lse) if want_lse else out
 
 
@@ -661,23 +674,22 @@ def pf_op_attention_paged(q, pages, cu_q, first, kv_len, causal=True, scale=None
     """Attention of new rows q [total_q, heads * head_dim], cu_q[s] .. cu_q[s + 1] those of sequence s from its slot first[s] on,
     over slots [0, kv_len[s]) of the pages; causal: row i sees slots up to first[s] + i.  first may be None if not causal.
     Returns out, or (out, lse) with lse float [total_q, heads]; rows of no sequence are not written."""
-    _rows("q", q, pages.k.dtype, pages.k.device)
+    index, dt = pages.index, pages.k.dtype
+    if not (_good_rows(q, dt, index) and _good_ints(cu_q, (pages.n_seqs + 1,), index) and
+            _good_ints(kv_len, (pages.n_seqs,), index) and (first is None or _good_ints(first, (pages.n_seqs,), index))):
+        _rows("q", q, dt, pages.device)
+        _ints("cu_q", cu_q, (pages.n_seqs + 1,), pages.device)
+        _ints("kv_len", kv_len, (pages.n_seqs,), pages.device)
+        if first is not None:
+            _ints("first", first, (pages.n_seqs,), pages.device)
     heads = _heads("q", q, pages.head_dim)
-    _ints("cu_q", cu_q, (pages.n_seqs + 1,), q.device)
-    _ints("kv_len", kv_len, (pages.n_seqs,), q.device)
-    if first is not None:
-        _ints("first", first, (pages.n_seqs,), q.device)
     if scale is not None and not scale > 0:
         raise PfError(-3, f"scale: {scale}")
-    with _on(q.device) as stream:
-        out, lse, ws, ws_bytes = _attention_buffers(q, heads, pages.kv_heads, pages.head_dim, pages.n_seqs,
-                                                    pages.max_pages * pages.page_size, out, want_lse)
-        st = load_library().pf_op_attention_paged(
-            _DT[q.dtype], q.data_ptr(), _ld(q), C.byref(pages.c), cu_q.data_ptr(), None if first is None else first.data_ptr(),
-            kv_len.data_ptr(), q.shape[0], heads, 0.0 if scale is None else scale, int(causal), out.data_ptr(), _ld(out),
-            None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes, stream)
-    if st != 0:
-        _raise(st)
+    out, lse, ws, tail = _attention_buffers(q, heads, pages.kv_heads, pages.head_dim, pages.n_seqs,
+                                            pages.max_pages * pages.page_size, out, want_lse)
+    _launch(index, (_lib or load_library()).pf_op_attention_paged, _DT[dt], q.data_ptr(), _ld(q), pages.ref, cu_q.data_ptr(),
+            None if first is None else first.data_ptr(), kv_len.data_ptr(), q.shape[0], heads, 0.0 if scale is None else scale,
+            int(causal), *tail)
     return (out, lse) if want_lse else out
 
 
@@ -693,6 +705,14 @@ class Norm:
                 raise PfError(-3, f"norm {name}: shape {tuple(t.shape)}, a contiguous [d] is needed")
         self.c = PfNorm(kind=NORM_KINDS[kind], eps=eps, weight=None if weight is None else weight.data_ptr(),
                         bias=None if bias is None else bias.data_ptr())
+        self.ref = C.byref(self.c)
+        self.key = None      # (type, GPU, width) of the last call that the vectors fitted
+
+    def check(self, side, dtype, device, d):
+        for t in (self.weight, self.bias):
+            if t is not None and tuple(_plain(side + " norm", t, dtype, device).shape) != (d,):
+                raise PfError(-3, f"{side} norm: {tuple(t.shape)}, ({d},) is needed")
+        self.key = (dtype, device.index, d)
 
 
 def make_norm(kind, weight=None, bias=None, eps=1e-6):
@@ -705,40 +725,42 @@ def pf_op_norm_residual(y, x, post=None, pre=None, gate=None, gate_tanh=False, x
     """x_out = x_scale * x + g(gate) * post(y), h = pre(x_out) * (1 + scale) + shift; returns (x_out, h).  x float [rows, d], y and h
     in `dtype` (y's; without a branch, y None, it has to be given).  gate / scale / shift float [d], or [n_seqs, d] with cu
     int32 [n_seqs + 1].  want_h False: only the residual (h None)."""
-    _rows("x", x, torch.float32)
+    index, dev = x.get_device(), x.device
+    if index < 0 or not _good_rows(x, torch.float32, index):
+        _rows("x", x, torch.float32)
     rows, d = x.shape
-    dev = x.device
-    if y is not None:
-        _rows("y", y, dtype, dev)
-        if y.shape != x.shape:
-            raise PfError(-3, f"y: shape {tuple(y.shape)}, x has {tuple(x.shape)}")
-        dtype = y.dtype
+    if y is None:
+        y_args = (None, 0)
+    else:
+        dtype = y.dtype if dtype is None else dtype
+        if not (_good_rows(y, dtype, index) and y.shape == x.shape):
+            _out("y", y, x.shape, dtype, dev)
+        y_args = (y.data_ptr(), _ld(y))
     if dtype not in _DT:
         raise PfError(-4, f"dtype {dtype}")
-    for name, n in (("post", post), ("pre", pre)):
-        for t in () if n is None else (n.weight, n.bias):
-            if t is not None and tuple(_plain(name + " norm", t, dtype, dev).shape) != (d,):
-                raise PfError(-3, f"{name} norm: {tuple(t.shape)}, ({d},) is needed")
+    if post is not None and post.key != (dtype, index, d):
+        post.check("post", dtype, dev, d)
+    if pre is not None and pre.key != (dtype, index, d):
+        pre.check("pre", dtype, dev, d)
     n_seqs = None
     if cu is not None:
         if cu.dim() != 1 or cu.shape[0] < 1:
             raise PfError(-3, f"cu: shape {tuple(cu.shape)}, [n_seqs + 1] is needed")
         n_seqs = cu.shape[0] - 1
-        _ints("cu", cu, (n_seqs + 1,), dev)
-    gs = _vectors("gate", gate, d, n_seqs, dev)
-    ms = _vectors("scale", scale, d, n_seqs, dev)
-    ms2 = _vectors("shift", shift, d, n_seqs, dev)
+        if not _good_ints(cu, (n_seqs + 1,), index):
+            _ints("cu", cu, (n_seqs + 1,), dev)
+    gs, g_at = _vectors("gate", gate, d, n_seqs, index, dev)
+    ms, sc_at = _vectors("scale", scale, d, n_seqs, index, dev)
+    ms2, sh_at = _vectors("shift", shift, d, n_seqs, index, dev)
     if scale is not None and shift is not None and ms != ms2:
         raise PfError(-3, f"scale and shift: {ms} and {ms2} elements between sequences")
-    x_out = torch.empty(rows, d, dtype=torch.float32, device=dev) if x_out is None else _out("x_out", x_out, x.shape, torch.float32, dev)
+    x_out = _like(x) if x_out is None else _out("x_out", x_out, x.shape, torch.float32, dev)
     if want_h:
-        h_out = torch.empty(rows, d, dtype=dtype, device=dev) if h_out is None else _out("h_out", h_out, x.shape, dtype, dev)
-    with _on(dev) as stream:
-        st = load_library().pf_op_norm_residual(
-            _DT[dtype], _ptr(y), 0 if y is None else _ld(y), None if post is None else C.byref(post.c), _ptr(gate), gs,
-            int(gate_tanh), x_scale, x.data_ptr(), _ld(x), x_out.data_ptr(), _ld(x_out), None if pre is None else C.byref(pre.c),
-            _ptr(shift), _ptr(scale), max(ms, ms2), _ptr(h_out) if want_h else None, _ld(h_out) if want_h else 0, _ptr(cu),
-            n_seqs or 0, rows, d, stream)
-    if st != 0:
-        _raise(st)
+        h_out = _like(x, dtype) if h_out is None else _out("h_out", h_out, x.shape, dtype, dev)
+        h_args = (h_out.data_ptr(), _ld(h_out))
+    else:
+        h_args = (None, 0)
+    _launch(index, (_lib or load_library()).pf_op_norm_residual, _DT[dtype], *y_args, None if post is None else post.ref, g_at, gs,
+            int(gate_tanh), x_scale, x.data_ptr(), _ld(x), x_out.data_ptr(), _ld(x_out), None if pre is None else pre.ref, sh_at,
+            sc_at, max(ms, ms2), *h_args, None if cu is None else cu.data_ptr(), n_seqs or 0, rows, d)
     return x_out, h_out if want_h else None

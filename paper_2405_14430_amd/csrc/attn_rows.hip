@@ -16,10 +16,6 @@
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
 // bounds of the buffer loads give zeros for rows past the last key, for pages that are none and for channels past the head, so
 // neither the scores nor 0 * v meets what lies there.  LDS rows are padded against bank conflicts.
-#ifndef PF_WANT
-#define PF_WANT 1024
-#define PF_MINK 512
-#endif
 #include <type_traits>
 
 #include "requests.h"
@@ -45,18 +41,20 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 #if defined(__HIP_DEVICE_COMPILE__)
+template <int POLICY>
 struct Buffer {   // `bytes` bytes from a wave-uniform address; loads past them give zeros
   __amdgpu_buffer_rsrc_t rs;
   __device__ __forceinline__ Buffer(const void *base, unsigned bytes)
       : rs(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000)) {}
   __device__ __forceinline__ u32x4 load16(unsigned lane_at, unsigned at) const {
-    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane_at, at, 0));
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, lane_at, at, POLICY));
   }
 };
 __device__ __forceinline__ s16x4 lds_read_transposed(const unsigned char *p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
 #else   // the host pass only parses the kernels
+template <int POLICY>
 struct Buffer {
   __device__ Buffer(const void *, unsigned) {}
   __device__ u32x4 load16(unsigned, unsigned) const { return u32x4{}; }
@@ -96,6 +94,9 @@ struct Tile {
   static constexpr int RW = TK / NW;                       // rows of a tile that one wave brings in
   static constexpr int LOADS = RW * ROWB / 1024;           // its 1 KB loads
   static constexpr int BUFS = NW > 1 ? 2 : 1;
+  // The key kernel reads every key once: non-temporal loads (policy bit 1) leave the caches to what is read again (64 tokens over
+  // caches of up to 16k keys 191 -> 172 us).  Row tiles share their keys through the L2s (the wide kernel 2.33 -> 2.49 ms with it).
+  static constexpr int POLICY = KW > 1 ? 2 : 0;
   static constexpr int JOIN_B = KW > 1 ? KW * 32 * (DHP + 4 + 2) * 4 : 0;   // the waves' partial results
   static constexpr int SMEM = KW * BUFS * (KTILE_B + VTILE_B) > JOIN_B ? KW * BUFS * (KTILE_B + VTILE_B) : JOIN_B;
   static constexpr int ROWS = 32 * NW;                     // query rows of a workgroup
@@ -250,10 +251,10 @@ struct TileLoader {
     }
   }
   __device__ __forceinline__ void load_k(int i) {
-    k_reg[i] = Buffer(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * k_row : 0);
+    k_reg[i] = Buffer<C::POLICY>(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * k_row : 0);
   }
   __device__ __forceinline__ void load_v(int i) {
-    v_reg[i] = Buffer(v_from[i / GL], in_group[i / GL] * v_row).load16(v_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * v_row : 0);
+    v_reg[i] = Buffer<C::POLICY>(v_from[i / GL], in_group[i / GL] * v_row).load16(v_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * v_row : 0);
   }
   __device__ __forceinline__ void load(int t) {
     aim(t);
@@ -887,21 +888,11 @@ hipError_t launch_wide(const RowsAttn &a, hipStream_t s) {
   return e != hipSuccess || a.splits == 1 ? e : launch_join<bf16_t>(a, s);
 }
 
-// Which kernel: few rows per sequence on average: the key kernel; bf16 with a workgroup of 256 rows for every CU: the wide
-// one; else tiles for 128 rows.
-enum Shape { KEYS, TILES, WIDE };
-Shape pick_shape(int dt, int total_q, int n_seqs, int group, int kv_heads) {
-  const int64_t rows = (int64_t)total_q * group;
-  if (rows <= (int64_t)n_seqs * 32) return KEYS;
-  return dt == DT_BF16 && rows / 256 * kv_heads >= 256 ? WIDE : TILES;
-}
-
 template <typename T, int DHP, bool PAGED>
 hipError_t launch_rows_of(const RowsAttn &a, hipStream_t s) {
-  const Shape shape = pick_shape(a.dt, a.total_q, a.n_seqs, a.n_heads / a.kv_heads, a.kv_heads);
-  if (shape == KEYS) return launch_shape<T, DHP, PAGED, 1, 4>(a, s);
+  if (a.shape == ROWS_KEYS) return launch_shape<T, DHP, PAGED, 1, 4>(a, s);
   if constexpr (sizeof(T) == 2) {
-    if (shape == WIDE) return DHP == 96 && a.head_dim <= 80 ? launch_wide<DHP, DHP == 96 ? 5 : DHP / 16, PAGED>(a, s) : launch_wide<DHP, DHP / 16, PAGED>(a, s);
+    if (a.shape == ROWS_WIDE) return DHP == 96 && a.head_dim <= 80 ? launch_wide<DHP, DHP == 96 ? 5 : DHP / 16, PAGED>(a, s) : launch_wide<DHP, DHP / 16, PAGED>(a, s);
   }
   return launch_shape<T, DHP, PAGED, 4, 1>(a, s);
 }
@@ -914,36 +905,46 @@ hipError_t launch_dim(const RowsAttn &a, hipStream_t s) {
 
 }  // namespace
 
+// Which kernel, and how many chunks of the key range.  The lengths are on the device: the host knows the rows of all sequences, their
+// number, and that none has more than max_kv keys.
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
-  const int group = n_heads / kv_heads;
-  const Shape shape = pick_shape(dt, total_q, n_seqs, group, kv_heads);
-  const int rows = shape == KEYS ? 32 : shape == WIDE ? 256 : 128;
-  const int64_t wgs = ((int64_t)total_q * group / rows + n_seqs) * kv_heads;   // without chunks
-  int64_t splits = 1;
-  if (shape == KEYS) {
-    splits = (PF_WANT + wgs - 1) / wgs;
-    const int64_t cap = max_kv / PF_MINK > 1 ? max_kv / PF_MINK : 1;
-    if (splits > cap) splits = cap;
-    if (splits > kMaxChunks) splits = kMaxChunks;
-  } else if (shape == TILES) {
-    // The chip holds 512 of these workgroups.  Time in key tiles: rounds x (tiles of a chunk and four for a workgroup's start and end),
-    // more where CUs hold a single workgroup; chunks cost a second launch and their partial results' way through memory.
-    const int64_t tiles = (max_kv + 63) / 64, cap = tiles / 4 < 16 ? tiles / 4 : 16;
-    const double row_units = (double)total_q * n_heads * head_dim * 2.9e-7;
-    double best = 1e300;
-    for (int64_t n = 1; n <= (cap > 1 ? cap : 1); ++n) {
-      const int64_t rounds = (wgs * n + 511) / 512;
-      const double fill = wgs * n >= 512 ? 1.0 : wgs * n / 512.0;
-      double cost = rounds * ((tiles + n - 1) / n + 4) * (1.5 - 0.5 * fill);
-      if (n > 1) cost += 2.0 + (4 * n + 2) * row_units;
-      if (cost < best - 1e-9) {
-        best = cost;
-        splits = n;
-      }
+  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads);
+  const auto wgs = [&](int per) { return (rows / per + n_seqs) * kv_heads; };   // workgroups of `per` rows, without chunks
+  const double out_units = (double)total_q * n_heads * head_dim * 2.9e-7;      // writing and reading a partial result, in key tiles
+
+  // Tiles for 128 rows.  The chip holds 512 of these workgroups.  Time in key tiles: rounds x (tiles of a chunk and four for a
+  // workgroup's start and end), more where CUs hold a single workgroup; chunks cost a second launch and their partial results.
+  const int64_t tiles = (max_kv + 63) / 64, most = tiles / 4 < 16 ? tiles / 4 : 16;
+  RowsPlan p{ROWS_TILES, 1, 0};
+  double tiles_cost = 1e300;
+  for (int64_t n = 1; n <= (most > 1 ? most : 1); ++n) {
+    const int64_t rounds = (wgs(128) * n + 511) / 512;
+    const double fill = wgs(128) * n >= 512 ? 1.0 : wgs(128) * n / 512.0;
+    double cost = rounds * ((double)((tiles + n - 1) / n) + 4) * (1.5 - 0.5 * fill);
+    if (n > 1) cost += 2.0 + (4 * n + 2) * out_units;
+    if (cost < tiles_cost - 1e-9) {
+      tiles_cost = cost;
+      p.splits = (int)n;
     }
   }
-  RowsPlan p{rows, (int)splits, 0};
-  if (splits > 1) p.ws_bytes = (size_t)splits * total_q * n_heads * (head_dim + 2) * sizeof(float);
+  // bf16 with a workgroup of 256 rows for every CU: the wide kernel (it needs no chunks)
+  if (dt == DT_BF16 && rows / 256 * kv_heads >= 256) p = RowsPlan{ROWS_WIDE, 1, 0};
+
+  // The key kernel for single tokens, and for launches that leave the chip empty.  It reads the keys for every 32 rows, through the
+  // L2s at some 7 TB/s; a tile of the tile kernel takes about 1.7 us (1024 rows x 16 heads of 72 over 1024 keys: 18.5 us,
+  // in tiles 30.4; 512 rows x 8 heads of 128 over 16384 keys: 188 and 63).  In fp32 the matrix units bound both, and more
+  // waves are better until the chip holds them (1024 rows x 16 heads of 128: 88 us, in tiles 121).
+  const double keys_us = 4.0 + (double)wgs(32) * max_kv * head_dim * 2 * dt_size(dt) / 7e6;
+  const bool keys = rows <= (int64_t)n_seqs * 32 || (dt == DT_BF16 ? p.shape == ROWS_TILES && keys_us < 1.7 * tiles_cost : wgs(32) <= 1024);
+  if (keys) {
+    // Chunks of at least 1024 keys, so many of them that caches of different lengths share the 512 workgroups the chip holds evenly
+    // (64 tokens over caches of up to 16k keys: 225 us with chunks enough for 1024 workgroups, 196 for 4096, 191 for 8192).
+    int64_t n = (8192 + wgs(32) - 1) / wgs(32);
+    const int64_t cap = max_kv / 1024 > 1 ? max_kv / 1024 : 1;
+    n = n < cap ? n : cap;
+    p = RowsPlan{ROWS_KEYS, (int)(n < kMaxChunks ? n : kMaxChunks), 0};
+  }
+  if (p.splits > 1) p.ws_bytes = (size_t)p.splits * total_q * n_heads * (head_dim + 2) * sizeof(float);
   return p;
 }
 

@@ -162,6 +162,7 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes || !aligned(ws, 16)))
     return refuse(PF_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes is needed, %zu given", who, p.ws_bytes, ws ? ws_bytes : (size_t)0);
   a.ws = (float *)ws;
+  a.shape = p.shape;
   a.splits = p.splits;
   return launched(launch_rows_attention(a, (hipStream_t)stream), who);
 }
