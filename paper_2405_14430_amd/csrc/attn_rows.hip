@@ -879,11 +879,14 @@ hipError_t launch_shape(const RowsAttn &a, hipStream_t s) {
 
 template <int DHP, int KS, bool PAGED>
 hipError_t launch_wide(const RowsAttn &a, hipStream_t s) {
-  constexpr int smem = Tile<bf16_t, DHP, 4, 1>::SMEM;
-  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, KS, PAGED>, smem>(); e != hipSuccess) return e;
+  constexpr int smem = Tile<bf16_t, DHP, 4, 1>::SMEM, alone = smem > 82 * 1024 ? smem : 82 * 1024;
+  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, KS, PAGED>, alone>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   p.slots = (int)((int64_t)a.total_q * p.group / 256) + a.n_seqs;
-  attn_rows_wide_kernel<DHP, KS, PAGED><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, smem, s>>>(p);
+  // Two workgroups of head size 64 fit a CU, and the dispatcher puts them there while other CUs are idle: where there are no more
+  // than CUs, each asks for more than half a CU's LDS (4 x 512 rows x 24 heads over 4250 keys: 132 -> 95 us).
+  const bool few = (int64_t)a.total_q * p.group / 256 * a.kv_heads * a.splits <= 256;
+  attn_rows_wide_kernel<DHP, KS, PAGED><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, few ? alone : smem, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_join<bf16_t>(a, s);
 }
@@ -905,38 +908,46 @@ hipError_t launch_dim(const RowsAttn &a, hipStream_t s) {
 
 }  // namespace
 
-// Which kernel, and how many chunks of the key range.  The lengths are on the device: the host knows the rows of all sequences, their
-// number, and that none has more than max_kv keys.
+// Which kernel, and how many chunks of the key range, by the estimated time in microseconds.  The lengths are on the device: the host
+// knows the rows of all sequences, their number, and that none has more than max_kv keys; a causal mask and shorter
+// sequences make all the estimates too long alike.
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
-  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads);
-  const auto wgs = [&](int per) { return (rows / per + n_seqs) * kv_heads; };   // workgroups of `per` rows, without chunks
-  const double out_units = (double)total_q * n_heads * head_dim * 2.9e-7;      // writing and reading a partial result, in key tiles
+  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads), tiles = (max_kv + 63) / 64;
+  // workgroups with work, without chunks
+  const auto wgs = [&](int per) { return ((rows + per - 1) / per > n_seqs ? (rows + per - 1) / per : n_seqs) * kv_heads; };
+  const auto rounds = [](int64_t n, int fit) { return n <= 2 * fit ? (double)((n + fit - 1) / fit) : (double)n / fit + 0.5; };
+  // the second launch, and the partial results on their way through memory (4 TB/s)
+  const double row_us = (double)total_q * n_heads * head_dim * 4.9e-7;
+  const auto join_us = [&](int64_t n) { return n > 1 ? 4.0 + (4 * n + 2) * row_us : 0.0; };
+  const int dim = head_dim <= 64 ? 0 : head_dim <= 96 ? 1 : 2;
 
-  // Tiles for 128 rows.  The chip holds 512 of these workgroups.  Time in key tiles: rounds x (tiles of a chunk and four for a
-  // workgroup's start and end), more where CUs hold a single workgroup; chunks cost a second launch and their partial results.
-  const int64_t tiles = (max_kv + 63) / 64, most = tiles / 4 < 16 ? tiles / 4 : 16;
   RowsPlan p{ROWS_TILES, 1, 0};
-  double tiles_cost = 1e300;
-  for (int64_t n = 1; n <= (most > 1 ? most : 1); ++n) {
-    const int64_t rounds = (wgs(128) * n + 511) / 512;
-    const double fill = wgs(128) * n >= 512 ? 1.0 : wgs(128) * n / 512.0;
-    double cost = rounds * ((double)((tiles + n - 1) / n) + 4) * (1.5 - 0.5 * fill);
-    if (n > 1) cost += 2.0 + (4 * n + 2) * out_units;
-    if (cost < tiles_cost - 1e-9) {
-      tiles_cost = cost;
-      p.splits = (int)n;
+  double best = 1e300;
+  const auto offer = [&](int shape, int64_t n, double us) {
+    if (us < best - 1e-9) {
+      best = us;
+      p = RowsPlan{shape, (int)n, 0};
     }
+  };
+  // chunks of four tiles or more, and none for launches that fill the chip twice without
+  const int64_t most = tiles < 8 ? 1 : tiles / 4 < 16 ? tiles / 4 : 16;
+  for (int64_t n = 1; n <= most; ++n) {
+    const double steps = (double)((tiles + n - 1) / n);
+    // 128 rows: two workgroups fit a CU; a tile of 64 keys takes this long where a CU has one, and where it has two (head sizes 64, 96, 128)
+    constexpr double kOne[] = {0.9, 1.4, 1.5}, kTwo[] = {1.3, 1.9, 2.3};
+    const int64_t w = wgs(128) * n;
+    if (w - wgs(128) < 1024) offer(ROWS_TILES, n, rounds(w, 512) * (steps + 4) * (w <= 256 ? kOne[dim] : kTwo[dim]) + join_us(n));
+    // 256 rows, one on a CU (2048 rows x 16 heads of 72 over 2048 keys: 44 us against 59)
+    constexpr double kWide[] = {1.0, 1.2, 1.7};
+    if (dt == DT_BF16 && wgs(256) * (n - 1) < 512) offer(ROWS_WIDE, n, rounds(wgs(256) * n, 256) * (steps * kWide[dim] + 8) + join_us(n));
   }
-  // bf16 with a workgroup of 256 rows for every CU: the wide kernel (it needs no chunks)
-  if (dt == DT_BF16 && rows / 256 * kv_heads >= 256) p = RowsPlan{ROWS_WIDE, 1, 0};
 
   // The key kernel for single tokens, and for launches that leave the chip empty.  It reads the keys for every 32 rows, through the
-  // L2s at some 7 TB/s; a tile of the tile kernel takes about 1.7 us (1024 rows x 16 heads of 72 over 1024 keys: 18.5 us,
-  // in tiles 30.4; 512 rows x 8 heads of 128 over 16384 keys: 188 and 63).  In fp32 the matrix units bound both, and more
-  // waves are better until the chip holds them (1024 rows x 16 heads of 128: 88 us, in tiles 121).
-  const double keys_us = 4.0 + (double)wgs(32) * max_kv * head_dim * 2 * dt_size(dt) / 7e6;
-  const bool keys = rows <= (int64_t)n_seqs * 32 || (dt == DT_BF16 ? p.shape == ROWS_TILES && keys_us < 1.7 * tiles_cost : wgs(32) <= 1024);
-  if (keys) {
+  // L2s at some 8 TB/s (1024 rows x 16 heads of 72 over 1024 keys: 18 us, in tiles 30; 512 rows x 8 heads of 128 over 16384
+  // keys: 188 and 63).  In fp32 the matrix units bound all kernels, and more waves are better until the chip holds them (1024
+  // rows x 16 heads of 128 over as many keys: 88 us, in tiles 121).
+  const double keys_us = 4.0 + (double)wgs(32) * max_kv * head_dim * 2 * dt_size(dt) / 8e6;
+  if (rows <= (int64_t)n_seqs * 32 || (dt == DT_BF16 ? keys_us < best : wgs(32) <= 1024)) {
     // Chunks of at least 1024 keys, so many of them that caches of different lengths share the 512 workgroups the chip holds evenly
     // (64 tokens over caches of up to 16k keys: 225 us with chunks enough for 1024 workgroups, 196 for 4096, 191 for 8192).
     int64_t n = (8192 + wgs(32) - 1) / wgs(32);
