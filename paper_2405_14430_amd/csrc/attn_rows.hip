@@ -831,13 +831,19 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
   const int c = tid % cl * 4, g = tid / cl;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   if (live && c < dh) {
-#pragma unroll 4
-    for (int i = g; i < a.splits; i += groups) {
-      const float w = weight[slot][i];
-      if (w > 0.f) {
-        const float4 x = *reinterpret_cast<const float4 *>(a.ws + ((int64_t)i * all + id) * dh + c);
-        acc = make_float4(fmaf(w, x.x, acc.x), fmaf(w, x.y, acc.y), fmaf(w, x.z, acc.z), fmaf(w, x.w, acc.w));
+    // eight chunks' loads at a time, whether they count or not (a chunk that does not may hold anything)
+    for (int i0 = g; i0 < a.splits; i0 += 8 * groups) {
+      float4 x[8];
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = min(i0 + j * groups, a.splits - 1);
+        x[j] = *reinterpret_cast<const float4 *>(a.ws + ((int64_t)i * all + id) * dh + c);
+        w[j] = i0 + j * groups < a.splits ? weight[slot][i] : 0.f;
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (w[j] > 0.f) acc = make_float4(fmaf(w[j], x[j].x, acc.x), fmaf(w[j], x[j].y, acc.y), fmaf(w[j], x[j].z, acc.z), fmaf(w[j], x[j].w, acc.w));
     }
   }
   *reinterpret_cast<float4 *>(&part[slot][tid * 4]) = acc;

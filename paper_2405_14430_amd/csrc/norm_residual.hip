@@ -71,25 +71,42 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
   constexpr int STEP = W * 64 * 4;
   const float inv_d = 1.0f / (float)d;
 
-  float x[NV][4];
+  // The vectors of the two norms, the gate and the modulation do not depend on the row's sums: with few groups per lane they are
+  // loaded in front of the first one, so that a launch of few rows waits for memory once and not once per sum.
+  constexpr bool EARLY = NV <= 2;
+  struct Vectors {
+    float wy[NV][4], by[NV][4], g[NV][4], wx[NV][4], bx[NV][4], sc[NV][4], sh[NV][4];
+  } vec;
+  const float *gp = a.gate ? a.gate + seg * a.gate_stride : nullptr;
+  const float *scp = a.scale ? a.scale + seg * a.mod_stride : nullptr, *shp = a.shift ? a.shift + seg * a.mod_stride : nullptr;
+  auto get = [&](auto *p, float (&o)[4], int c, float none) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = none;
+    if (p && c < d) load4(p + c, o);
+  };
+  const T *wyp = (const T *)a.post.weight, *byp = (const T *)a.post.bias, *wxp = (const T *)a.pre.weight, *bxp = (const T *)a.pre.bias;
+
+  float x[NV][4], y[NV][4];
   const float *xp = a.x + row * a.ldx;
+  const T *yp = a.y ? (const T *)a.y + row * a.ldy : nullptr;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c = c0 + v * STEP;
+  for (int v = 0; v < NV; ++v) get(xp, x[v], c0 + v * STEP, 0.f);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[v][i] = 0.f;
-    if (c < d) load4(xp + c, x[v]);
-  }
-  if (a.y) {
-    float y[NV][4];
-    const T *yp = (const T *)a.y + row * a.ldy;
+  for (int v = 0; v < NV; ++v) get(yp, y[v], c0 + v * STEP, 0.f);
+  if constexpr (EARLY) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = c0 + v * STEP;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[v][i] = 0.f;
-      if (c < d) load4(yp + c, y[v]);
+      get(wyp, vec.wy[v], c, 1.f);
+      get(byp, vec.by[v], c, 0.f);
+      get(gp, vec.g[v], c, 1.f);
+      get(wxp, vec.wx[v], c, 1.f);
+      get(bxp, vec.bx[v], c, 0.f);
+      get(scp, vec.sc[v], c, 0.f);
+      get(shp, vec.sh[v], c, 0.f);
     }
+  }
+  if (a.y) {
     if (a.post.kind != PF_NORM_NONE) {
       float mean = 0.f;
       if (a.post.kind == kLayer) {
@@ -111,32 +128,23 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
       const float r = 1.0f / sqrtf(row_sum<W>(t, wr, lane, part[1][slot]) * inv_d + a.post.eps);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int c = c0 + v * STEP;
-        if (c < d) {
-          float w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-          if (a.post.weight) load4((const T *)a.post.weight + c, w);
-          if (a.post.bias) load4((const T *)a.post.bias + c, b);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[v][i] = fmaf(y[v][i] * r, w[i], b[i]);
+        if constexpr (!EARLY) {
+          get(wyp, vec.wy[v], c0 + v * STEP, 1.f);
+          get(byp, vec.by[v], c0 + v * STEP, 0.f);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[v][i] = fmaf(y[v][i] * r, vec.wy[v][i], vec.by[v][i]);
       }
     }
-    const float *gp = a.gate ? a.gate + seg * a.gate_stride : nullptr;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = c0 + v * STEP;
-      if (c < d) {
-        float g[4] = {1.f, 1.f, 1.f, 1.f};
-        if (gp) {
-          load4(gp + c, g);
-          if (a.gate_tanh) {
+      if constexpr (!EARLY) get(gp, vec.g[v], c0 + v * STEP, 1.f);
+      if (gp && a.gate_tanh) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) g[i] = tanhf(g[i]);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[v][i] = fmaf(g[i], y[v][i], a.x_scale * x[v][i]);
+        for (int i = 0; i < 4; ++i) vec.g[v][i] = tanhf(vec.g[v][i]);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[v][i] = fmaf(vec.g[v][i], y[v][i], a.x_scale * x[v][i]);
     }
   } else {
 #pragma unroll
@@ -157,7 +165,8 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
     if (a.pre.kind == kLayer) {
       float t = 0.f;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) t += (x[v][0] + x[v][1]) + (x[v][2] + x[v][3]);
+      for (int v = 0; v < NV; ++v)
+        if (c0 + v * STEP < d) t += (x[v][0] + x[v][1]) + (x[v][2] + x[v][3]);
       mean = row_sum<W>(t, wr, lane, part[2][slot]) * inv_d;
     }
     float t = 0.f;
@@ -174,25 +183,21 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
   }
   if (!live) return;
   T *hp = (T *)a.h + row * a.ldh;
-  const float *sc = a.scale ? a.scale + seg * a.mod_stride : nullptr, *sh = a.shift ? a.shift + seg * a.mod_stride : nullptr;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * STEP;
+    if constexpr (!EARLY) {
+      get(wxp, vec.wx[v], c, 1.f);
+      get(bxp, vec.bx[v], c, 0.f);
+      get(scp, vec.sc[v], c, 0.f);
+      get(shp, vec.sh[v], c, 0.f);
+    }
     if (c < d) {
-      float w[4] = {1.f, 1.f, 1.f, 1.f}, b[4] = {0.f, 0.f, 0.f, 0.f}, o[4];
-      if (a.pre.weight) load4((const T *)a.pre.weight + c, w);
-      if (a.pre.bias) load4((const T *)a.pre.bias + c, b);
+      float o[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = fmaf(x[v][i] * r, w[i], b[i]);
-      if (sc) {
-        load4(sc + c, w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = fmaf(o[i], w[i], o[i]);
-      }
-      if (sh) {
-        load4(sh + c, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += b[i];
+      for (int i = 0; i < 4; ++i) {
+        o[i] = fmaf(x[v][i] * r, vec.wx[v][i], vec.bx[v][i]);
+        o[i] = fmaf(o[i], vec.sc[v][i], o[i]) + vec.sh[v][i];
       }
       store4(hp + c, o);
     }
