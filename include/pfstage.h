@@ -404,7 +404,8 @@ int pf_gemm_read_ahead(int M, int N, int K);
  * does not read: the calls can be captured into a graph and replayed with other contents.  Every value read from them is
  * bounded before it is used, so wrong ones give wrong rows and no access outside the arrays.
  * The conventions above hold here too: nothing is allocated, nothing synchronises, errors of arguments are found before
- * anything is launched.  Calls with no rows or no sequences do nothing and may pass NULL pointers.  Outputs may not overlap inputs
+ * anything is launched.   Calls with no rows or no sequences do nothing and may pass NULL pointers; a call
+ * takes at most 2^24 rows (attention: as many workgroups of 32 rows).  Outputs may not overlap inputs
  * except where it is said.  pf_last_error(NULL) says what was wrong.
  * ---------------------------------------------------------------------------------------------- */
 
@@ -488,7 +489,8 @@ pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, in
  * of n_q sees the keys j <= i + n_k - n_q, so the last query sees all.  A row that sees no key gives zeros.
  * lse != NULL: float [total_q, n_heads] receives log sum_j exp(scale * q . k_j) (-inf for a row that sees none), with which parts of a
  * sequence can be joined.  Scores, softmax and sums are in 32 bits; for bf16 the weights are rounded to bf16 for the second product.
- * Values of keys past the end of a sequence are not read; values that only the causal mask hides take part with weight zero.
+ * Keys and values past the end of a sequence are not read, and what the causal mask hides from a row does not reach it, infinities
+ * and NaN included.
  * ws: pf_op_attention_rows_ws_bytes(.., max_kv = total_k) bytes (may be NULL if that is 0); calls that may run at the same
  * time need one each.
  */
@@ -498,6 +500,10 @@ pf_status pf_op_attention_packed(int dtype, const void *q, int64_t ldq, const vo
                                  const int32_t *cu_q, const int32_t *cu_k, int n_seqs, int total_q, int total_k, int n_heads,
                                  int kv_heads, int head_dim, float scale, int causal, void *out, int64_t ldo, float *lse, void *ws,
                                  size_t ws_bytes, void *stream);
+/* Host-only: the kernel that an attention launch of these sizes runs (a kernel trace shows it with its types in front), and the
+ * number of chunks of the key range it is cut into; "" where the sizes are refused.  Per-thread storage, valid until the next call. */
+const char *pf_attention_rows_kernel_name(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv,
+                                          int *chunks);
 
 /*
  * The same over keys in pages: the rows cu_q[s] .. cu_q[s + 1] are new tokens (a patch, part of a prompt, one token) of sequence

@@ -58,7 +58,7 @@ EXPORTS = ["pf_stage_kv_bytes", "pf_stage_workspace_bytes", "pf_stage_create", "
            "pf_op_ln_modulate", "pf_op_gemm", "pf_op_kv_scatter", "pf_op_attention_ws_bytes", "pf_op_attention", "pf_attention_kernel_name", "pf_probe_mfma_loop",
            "pf_gemm_tile_count", "pf_gemm_tile_map", "pf_gemm_read_ahead", "pf_op_gemm_tile", "pf_static_scratch_bytes", "pf_op_attention_static", "pf_gemm_kernel_name", "pf_gemm_qkv_kernel_name", "pf_op_axpy", "pf_kv_view_image", "pf_op_axpby",
            "pf_rope_init", "pf_op_rope", "pf_op_kv_append", "pf_op_attention_rows_ws_bytes", "pf_op_attention_packed",
-           "pf_op_attention_paged", "pf_op_norm_residual"]
+           "pf_op_attention_paged", "pf_op_norm_residual", "pf_attention_rows_kernel_name"]
 
 PF_ROPE_MAX_AXES, PF_ROPE_MAX_PAIRS = 3, 64
 ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
@@ -178,6 +178,8 @@ def load_library():
                                     vp, i64, i32, vp]
     lib.pf_op_attention_rows_ws_bytes.restype = sz
     lib.pf_op_attention_rows_ws_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i64]
+    lib.pf_attention_rows_kernel_name.restype = C.c_char_p
+    lib.pf_attention_rows_kernel_name.argtypes = [i32, i32, i32, i32, i32, i32, i64, C.POINTER(i32)]
     lib.pf_op_attention_packed.restype = i32
     lib.pf_op_attention_packed.argtypes = [i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i32, i32, i32, i32, f32, i32, vp,
                                            i64, vp, vp, sz, vp]

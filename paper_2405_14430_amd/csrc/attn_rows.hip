@@ -131,6 +131,7 @@ struct Work {
   int k0, k_end;          // packed: row of key 0; keys that some row of the tile sees lie before k_end
   int kb, ke;             // the chunk's
   int64_t first;          // slot of query 0
+  int zone;               // keys from here to ke are hidden from some row of the tile (ke: none are)
 };
 template <bool PAGED, int ROWS, int UNIT>
 __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Work &w) {
@@ -165,6 +166,8 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
     w.kb = (int)min((int64_t)w.k_end, w.sp * c);
     w.ke = (int)min((int64_t)w.k_end, (w.sp + 1) * c);
   }
+  w.zone = w.ke;
+  if (a.causal && w.first + w.r_first / G + 1 < w.ke) w.zone = w.first + w.r_first / G + 1 < 0 ? 0 : (int)(w.first + w.r_first / G + 1);
   return true;
 }
 
@@ -250,6 +253,60 @@ struct TileLoader {
       in_group[g] = uniform(rows);
     }
   }
+  // Values that the mask hides from some rows of the tile have weight 0 there, and 0 times an infinity or a NaN is none: for tiles with
+  // such keys the V registers are cleared of them before they go to LDS, and the keys noted in `hidden` (one bit a
+  // key; nearly always none).  `at`: the tile's place in `hidden`.
+  __device__ __forceinline__ void clear_v(unsigned *hidden, int at) {
+#pragma unroll
+    for (int i = 0; i < C::LOADS; ++i) {
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        unsigned u = v_reg[i][e];
+        if constexpr (sizeof(T) == 2) {
+          if ((u & 0x7f80u) == 0x7f80u) { u &= 0xffff0000u; bad = true; }
+          if ((u & 0x7f800000u) == 0x7f800000u) { u &= 0xffffu; bad = true; }
+        } else {
+          if ((u & 0x7f800000u) == 0x7f800000u) { u = 0; bad = true; }
+        }
+        v_reg[i][e] = u;
+      }
+      const int row = lw * C::RW + (i * 1024 + lane * 16) / ROWB;
+      if (bad) atomicOr(hidden + at * (TK / 32) + (row >> 5), 1u << (row & 31));
+    }
+  }
+  // The row of V of a key before ke, nullptr where its page is none.
+  __device__ __forceinline__ const T *value_row(int key) const {
+    if constexpr (PAGED) {
+      const int pg = a.pages.table[(int64_t)s * a.pages.max_pages + (key >> a.pages.page_shift)];
+      if (pg < 0 || pg >= a.pages.n_pages) return nullptr;
+      return v_head + pg * a.pages.v_stride + (int64_t)(key & ((1 << a.pages.page_shift) - 1)) * a.head_dim;
+    } else {
+      return v_head + key * a.ldv;
+    }
+  }
+  // What the noted keys bring to the rows that do see them: their infinities and NaN, whatever the weight.  o: the lane's row, channels
+  // cb * 32 + 8 g + 4 hi .. + 3 in o[cb][4 g ..].
+  template <int CB>
+  __device__ __forceinline__ void add_hidden(const unsigned *hidden, int n_tiles, int first_tile, int limit, int hi, f32x16 (&o)[CB]) const {
+    for (int w = 0; w < n_tiles * (TK / 32); ++w) {
+      unsigned bits = __builtin_amdgcn_readfirstlane(hidden[w]);
+      while (bits) {
+        const int key = kb + first_tile * TK + w * 32 + __builtin_ctz(bits);
+        bits &= bits - 1;
+        const T *vr = key < ke ? value_row(key) : nullptr;
+        if (!vr || key >= limit) continue;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int c = cb * 32 + 8 * (i >> 2) + 4 * hi + (i & 3);
+            const float v = c < a.head_dim ? to_f32(vr[c]) : 0.f;
+            if (!(fabsf(v) <= 3.4028235e38f)) o[cb][i] += v;
+          }
+      }
+    }
+  }
   __device__ __forceinline__ void load_k(int i) {
     k_reg[i] = Buffer<C::POLICY>(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * k_row : 0);
   }
@@ -290,9 +347,9 @@ __device__ __forceinline__ void put_stats(const RowsAttn &a, int sp, int64_t row
   const int64_t at = row * a.n_heads + head;
   if (a.splits > 1) {
     float *dst = a.ws + (int64_t)a.splits * a.total_q * a.n_heads * a.head_dim + ((int64_t)sp * a.total_q * a.n_heads + at) * 2;
-    *reinterpret_cast<float2 *>(dst) = make_float2(l > 0.f ? m : -INFINITY, l);
+    *reinterpret_cast<float2 *>(dst) = make_float2(l != 0.f ? m : -INFINITY, l);
   } else if (a.lse) {
-    a.lse[at] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+    a.lse[at] = l != 0.f ? m * kLn2 + logf(l) : -INFINITY;
   }
 }
 
@@ -343,7 +400,21 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   TileLoader<C, T, PAGED> ld(a, w, lane, KW > 1 ? 0 : wave, kb, ke);
   constexpr int BUF_B = C::KTILE_B + C::VTILE_B;
   unsigned char *const ring = smem + (KW > 1 ? wave * C::BUFS * BUF_B : 0);
-  auto store_tile = [&](int buf) __attribute__((always_inline)) { ld.store(ring + buf * BUF_B, ring + buf * BUF_B + C::KTILE_B); };
+  // keys with infinities or NaN among those that some row does not see: the zone spans fewer keys than the tile has rows
+  constexpr int ZONE = (C::ROWS + TK - 2) / TK + 1;              // tiles it can touch
+  __shared__ unsigned hidden_all[KW][ZONE * (TK / 32)];
+  unsigned *const hidden = hidden_all[KW > 1 ? wave : 0];
+  const bool zoned = w.zone < ke;
+  const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
+  if (zoned) {
+    if ((KW > 1 ? lane : (int)threadIdx.x) < ZONE * (TK / 32)) hidden[KW > 1 ? lane : threadIdx.x] = 0;
+    if constexpr (NW > 1) __syncthreads();
+  }
+  auto store_tile = [&](int t) __attribute__((always_inline)) {
+    if (zoned && t >= zone_tile) ld.clear_v(hidden, t - zone_tile);
+    const int buf = t & (C::BUFS - 1);
+    ld.store(ring + buf * BUF_B, ring + buf * BUF_B + C::KTILE_B);
+  };
 
   f32x16 o[CB];
 #pragma unroll
@@ -456,7 +527,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       const unsigned now = groups;
       if (t + 1 < tiles) {
         groups = ld.groups;
-        store_tile((t + 1) & 1);
+        store_tile(t + 1);
         if (t + 2 < tiles) ld.load(t + 2);
       }
       work_tile(t, t & 1, now);
@@ -465,10 +536,14 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     // a wave's LDS operations are carried out in order: its own tile needs no barrier
     for (int t = 0; t < tiles; ++t) {
       const unsigned now = ld.groups;
-      store_tile(0);
+      store_tile(t);
       if (t + 1 < tiles) ld.load(t + 1);
       work_tile(t, 0, now);
     }
+  }
+  if (zoned) {
+    if constexpr (NW > 1) __syncthreads();
+    ld.template add_hidden<CB>(hidden, ZONE, zone_tile, row_ok ? limit : 0, hi, o);
   }
   float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
 
@@ -504,7 +579,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     m_run = m_all;
     // the lane's channels: 4 hi + 8 (wave + 4 i) .. + 3
     if (row_ok) {
-      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+      const float inv = l_tot != 0.f ? 1.f / l_tot : 0.f;
 #pragma unroll
       for (int i = 0; i < (DHP / 8 + KW - 1) / KW; ++i) {
         const int c = 4 * hi + 8 * (wave + KW * i);
@@ -524,7 +599,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     }
     if (wave != 0) return;
   } else if (row_ok) {
-    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    const float inv = l_tot != 0.f ? 1.f / l_tot : 0.f;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -717,6 +792,18 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
   // Tile t lies in LDS buffers t % 2.  Its first half's weights are formed while its second half's scores run, and so on.  K of tile t + 1
   // goes to LDS in the first half of tile t, where K of tile t - 1 has been read by all since the barrier before, V of tile t + 1 in
   // the second half, behind the barrier in the middle, from which on nobody reads V of tile t - 1.
+  // keys with infinities or NaN among those that some row does not see (fewer than 256)
+  constexpr int ZONE = 5;                                         // tiles they can touch
+  __shared__ unsigned hidden[ZONE * 2];
+  const bool zoned = w.zone < ke;
+  const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
+  if (zoned) {
+    if (threadIdx.x < ZONE * 2) hidden[threadIdx.x] = 0;
+    __syncthreads();
+  }
+  auto clear = [&](int t) __attribute__((always_inline)) {
+    if (zoned && t >= zone_tile && t < tiles) ld.clear_v(hidden, t - zone_tile);
+  };
   if (tiles > 0) {
     Scores s0, s1;
     Weights w0, w1;
@@ -733,6 +820,7 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
     };
     ld.load(0);
     unsigned groups_now = ld.groups;
+    clear(0);
     ld.store(smem, vring);
     ld.load(1);
     unsigned groups_next = ld.groups;
@@ -761,18 +849,24 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
       ld.aim(t + 2);
       step(key0, groups_now & 3, s0, s1, w1, w0, k0 + K_HALF, v1 + V_HALF, k1, std::true_type{});
       meet();
+      clear(t + 1);
       step(key0 + 32, groups_now >> 2, s1, s0, w0, w1, k1, v0, v1, std::false_type{});
       groups_now = groups_next;
       groups_next = ld.groups;
     }
     last_values((tiles & 1 ? 0 : C::VTILE_B) + V_HALF);
+    if (zoned) {
+      __syncthreads();
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) ld.template add_hidden<CB>(hidden, ZONE, zone_tile, row_ok[rb] ? limit[rb] : 0, hi, o[rb]);
+    }
   }
 
 #pragma unroll
   for (int rb = 0; rb < 2; ++rb) {
     const float l = l_run[rb] + __shfl_xor(l_run[rb], 32, kWave);
     if (!row_ok[rb]) continue;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
     const int64_t row = w.q0 + tok[rb];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -817,7 +911,7 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
 #pragma unroll
   for (int i = 0; i < PER; ++i)
     if (i * NT + tid < a.splits) {
-      const float w = v[i].y > 0.f ? __builtin_amdgcn_exp2f(v[i].x - m) : 0.f;
+      const float w = v[i].y != 0.f ? __builtin_amdgcn_exp2f(v[i].x - m) : 0.f;
       weight[slot][i * NT + tid] = w;
       l = fmaf(w, v[i].y, l);
     }
@@ -843,13 +937,13 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (w[j] > 0.f) acc = make_float4(fmaf(w[j], x[j].x, acc.x), fmaf(w[j], x[j].y, acc.y), fmaf(w[j], x[j].z, acc.z), fmaf(w[j], x[j].w, acc.w));
+        if (w[j] != 0.f) acc = make_float4(fmaf(w[j], x[j].x, acc.x), fmaf(w[j], x[j].y, acc.y), fmaf(w[j], x[j].z, acc.z), fmaf(w[j], x[j].w, acc.w));
     }
   }
   *reinterpret_cast<float4 *>(&part[slot][tid * 4]) = acc;
   __syncthreads();
   if (!live) return;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
   if (g == 0 && c < dh) {
     for (int i = 1; i < groups; ++i) {
       const float4 x = *reinterpret_cast<const float4 *>(&part[slot][(i * cl + tid) * 4]);
@@ -859,7 +953,7 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
     if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
     else *reinterpret_cast<bf16x4 *>(dst) = bf16x4{(bf16_t)(acc.x * inv), (bf16_t)(acc.y * inv), (bf16_t)(acc.z * inv), (bf16_t)(acc.w * inv)};
   }
-  if (a.lse && tid == 0) a.lse[id] = l > 0.f ? m * kLn2 + logf(l) : -INFINITY;
+  if (a.lse && tid == 0) a.lse[id] = l != 0.f ? m * kLn2 + logf(l) : -INFINITY;
 }
 
 template <typename T>

@@ -9,6 +9,8 @@ using namespace pf;
 
 namespace {
 
+constexpr int kMaxRows = 1 << 24;   // rows of one call of the row-wise operators: a launch has less than 2^32 threads
+
 bool dt_ok(int dt) { return dt == PF_F32 || dt == PF_BF16; }
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 bool row_stride_ok(int64_t ld, int64_t width, int dt) { return ld >= width && ld % (16 / (int64_t)dt_size(dt)) == 0; }
@@ -113,6 +115,7 @@ pf_status pf_op_rope(int dtype, const pf_rope *rope, const int32_t *pos, const v
   const int64_t d = (int64_t)n_heads * head_dim;
   if (!row_stride_ok(ldx, d, dtype) || !row_stride_ok(ldo, d, dtype) || !aligned(x, 16) || !aligned(out, 16) || !aligned(pos, 4))
     return refuse(PF_ERR_SHAPE, "pf_op_rope: row strides %lld, %lld for rows of %lld, or alignment", (long long)ldx, (long long)ldo, (long long)d);
+  if (tokens > kMaxRows) return refuse(PF_ERR_SHAPE, "pf_op_rope: %d tokens are more than %d", tokens, kMaxRows);
   if (x == out && ldx != ldo) return refuse(PF_ERR_SHAPE, "pf_op_rope: in place with two row strides");
   if (const char *w = rope_wrong(*rope, head_dim)) return refuse(PF_ERR_CONFIG, "%s", w);
   RopeRows a{};
@@ -136,6 +139,7 @@ pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, in
       (n_heads && (!row_stride_ok(ldq, dq, dtype) || !row_stride_ok(ldqo, dq, dtype) || !aligned(q, 16) || !aligned(q_out, 16))))
     return refuse(PF_ERR_SHAPE, "pf_op_kv_append: row strides %lld, %lld for rows of %lld (q %lld, %lld for %lld), or alignment", (long long)ldk,
                   (long long)ldv, (long long)d, (long long)ldq, (long long)ldqo, (long long)dq);
+  if (tokens > kMaxRows) return refuse(PF_ERR_SHAPE, "pf_op_kv_append: %d tokens are more than %d", tokens, kMaxRows);
   if (n_heads && q == q_out && ldq != ldqo) return refuse(PF_ERR_SHAPE, "pf_op_kv_append: in place with two row strides");
   if (rope)
     if (const char *w = rope_wrong(*rope, pages->head_dim)) return refuse(PF_ERR_CONFIG, "%s", w);
@@ -152,6 +156,18 @@ size_t pf_op_attention_rows_ws_bytes(int dtype, int total_q, int n_seqs, int n_h
   return rows_attention_plan(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv).ws_bytes;
 }
 
+const char *pf_attention_rows_kernel_name(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv,
+                                          int *chunks) {
+  static thread_local char name[64];
+  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1) return "";
+  const RowsPlan p = rows_attention_plan(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
+  if (chunks) *chunks = p.splits;
+  const int dim = head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128;
+  if (p.shape == ROWS_WIDE) snprintf(name, sizeof(name), "attn_rows_wide_kernel<%d,%d>", dim, head_dim <= 80 && dim == 96 ? 5 : dim / 16);
+  else snprintf(name, sizeof(name), "attn_rows_kernel<%s,%d,%s>", dtype == PF_BF16 ? "bf16" : "float", dim, p.shape == ROWS_KEYS ? "1,4" : "4,1");
+  return name;
+}
+
 static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws_bytes, void *stream, const char *who) {
   const int64_t d = (int64_t)a.n_heads * a.head_dim;
   if (!row_stride_ok(a.ldq, d, a.dt) || !row_stride_ok(a.ldo, d, a.dt) || !aligned(a.q, 16) || !aligned(a.out, 16) || (a.lse && !aligned(a.lse, 4)))
@@ -162,6 +178,9 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes || !aligned(ws, 16)))
     return refuse(PF_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes is needed, %zu given", who, p.ws_bytes, ws ? ws_bytes : (size_t)0);
   a.ws = (float *)ws;
+  // a launch has less than 2^32 threads
+  if (((int64_t)a.total_q * (a.n_heads / a.kv_heads) / 32 + a.n_seqs) * a.kv_heads * p.splits >= (1 << 24))
+    return refuse(PF_ERR_SHAPE, "%s: %d rows of %d heads in %d sequences are too many for one launch", who, a.total_q, a.n_heads, a.n_seqs);
   a.shape = p.shape;
   a.splits = p.splits;
   return launched(launch_rows_attention(a, (hipStream_t)stream), who);
@@ -220,6 +239,7 @@ pf_status pf_op_norm_residual(int dtype, const void *y, int64_t ldy, const pf_no
   if (rows == 0 || (cu && n_seqs == 0)) return PF_OK;
   if (!x || (!x_out && !h)) return refuse(PF_ERR_NULL, "%s: x, or both outputs", who);
   const size_t al = dtype == PF_BF16 ? 8 : 16;
+  if (rows > kMaxRows) return refuse(PF_ERR_SHAPE, "%s: %d rows are more than %d", who, rows, kMaxRows);
   if (d < 8 || d % 8 || d > 8192) return refuse(PF_ERR_SHAPE, "%s: d = %d", who, d);
   if (ldx < d || ldx % 4 || !aligned(x, 16) || (y && (ldy < d || ldy % 4 || !aligned(y, al))) ||
       (x_out && (ldxo < d || ldxo % 4 || !aligned(x_out, 16))) || (h && (ldh < d || ldh % 4 || !aligned(h, al))) ||
