@@ -171,6 +171,18 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
   return true;
 }
 
+// (token, head) row `at` of a workgroup's tile.
+struct LaneRow {
+  bool ok;
+  int tok, head;
+  __device__ __forceinline__ LaneRow(const Work &w, int G, int at) {
+    const int r = w.r_first + at;
+    ok = r < w.n * G;
+    tok = ok ? r / G : 0;
+    head = w.hk * G + (ok ? r - tok * G : 0);
+  }
+};
+
 // Brings a wave's RW rows (from row LW on) of K and V tiles of TK keys from memory into registers, and from there into LDS.  The rows
 // of a load lie in one group of 16 keys, so in one page.
 template <typename C, typename T, bool PAGED>
@@ -275,38 +287,6 @@ struct TileLoader {
       if (bad) atomicOr(hidden + at * (TK / 32) + (row >> 5), 1u << (row & 31));
     }
   }
-  // The row of V of a key before ke, nullptr where its page is none.
-  __device__ __forceinline__ const T *value_row(int key) const {
-    if constexpr (PAGED) {
-      const int pg = a.pages.table[(int64_t)s * a.pages.max_pages + (key >> a.pages.page_shift)];
-      if (pg < 0 || pg >= a.pages.n_pages) return nullptr;
-      return v_head + pg * a.pages.v_stride + (int64_t)(key & ((1 << a.pages.page_shift) - 1)) * a.head_dim;
-    } else {
-      return v_head + key * a.ldv;
-    }
-  }
-  // What the noted keys bring to the rows that do see them: their infinities and NaN, whatever the weight.  o: the lane's row, channels
-  // cb * 32 + 8 g + 4 hi .. + 3 in o[cb][4 g ..].
-  template <int CB>
-  __device__ __forceinline__ void add_hidden(const unsigned *hidden, int n_tiles, int first_tile, int limit, int hi, f32x16 (&o)[CB]) const {
-    for (int w = 0; w < n_tiles * (TK / 32); ++w) {
-      unsigned bits = __builtin_amdgcn_readfirstlane(hidden[w]);
-      while (bits) {
-        const int key = kb + first_tile * TK + w * 32 + __builtin_ctz(bits);
-        bits &= bits - 1;
-        const T *vr = key < ke ? value_row(key) : nullptr;
-        if (!vr || key >= limit) continue;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int c = cb * 32 + 8 * (i >> 2) + 4 * hi + (i & 3);
-            const float v = c < a.head_dim ? to_f32(vr[c]) : 0.f;
-            if (!(fabsf(v) <= 3.4028235e38f)) o[cb][i] += v;
-          }
-      }
-    }
-  }
   __device__ __forceinline__ void load_k(int i) {
     k_reg[i] = Buffer<C::POLICY>(k_from[i / GL], in_group[i / GL] * k_row).load16(k_off[WHOLE ? 0 : i], WHOLE ? i % GL * RPL * k_row : 0);
   }
@@ -353,6 +333,40 @@ __device__ __forceinline__ void put_stats(const RowsAttn &a, int sp, int64_t row
   }
 }
 
+// What the keys noted in `hidden` (n words, from key0 on; keys at ke and behind are none) bring to the rows that do see them: their
+// infinities and NaN, whatever the weight, added to the rows that the workgroup has stored.  Nearly always there are none.
+template <typename T, bool PAGED, int ROWS, int THREADS>
+__device__ __forceinline__ void add_hidden(const RowsKernelArgs &p, const Work &w, const unsigned *hidden, int n, int key0, int ke) {
+  const RowsAttn &a = p.a;
+  unsigned any = 0;
+  for (int i = 0; i < n; ++i) any |= hidden[i];
+  if (__builtin_amdgcn_readfirstlane(any) == 0) return;
+  __threadfence_block();
+  __syncthreads();                        // every row is stored
+  const int dh = a.head_dim;
+  for (int i = 0; i < n; ++i)
+    for (unsigned bits = hidden[i]; bits; bits &= bits - 1) {
+      const int key = key0 + i * 32 + __builtin_ctz(bits);
+      if (key >= ke) break;
+      const T *v;
+      if constexpr (PAGED) {
+        const int pg = a.pages.table[(int64_t)w.s * a.pages.max_pages + (key >> a.pages.page_shift)];
+        if (pg < 0 || pg >= a.pages.n_pages) continue;
+        v = (const T *)a.pages.v + pg * a.pages.v_stride + (((int64_t)w.hk << a.pages.page_shift) + (key & ((1 << a.pages.page_shift) - 1))) * dh;
+      } else {
+        v = (const T *)a.v + (int64_t)(w.k0 + key) * a.ldv + (int64_t)w.hk * dh;
+      }
+      for (int e = threadIdx.x; e < ROWS * dh; e += THREADS) {
+        const int r = w.r_first + e / dh, c = e % dh, tok = r / p.group;
+        const float x = to_f32(v[c]);
+        if (r >= w.n * p.group || key > w.first + tok || fabsf(x) <= 3.4028235e38f) continue;
+        const int64_t row = w.q0 + tok, head = w.hk * p.group + r - tok * p.group;
+        if (a.splits > 1) a.ws[(((int64_t)w.sp * a.total_q + row) * a.n_heads + head) * dh + c] += x;
+        else ((T *)a.out)[row * a.ldo + head * dh + c] = from_f32<T>(to_f32(((T *)a.out)[row * a.ldo + head * dh + c]) + x);
+      }
+    }
+}
+
 template <typename T, int DHP, bool PAGED, int NW, int KW>
 __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void attn_rows_kernel(RowsKernelArgs p) {
   using C = Tile<T, DHP, NW, KW>;
@@ -375,12 +389,9 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   const int tiles = (ke - kb + TK - 1) / TK;
 
   // ---- the lane's row
-  const int r = w.r_first + (KW > 1 ? 0 : wave) * 32 + l32;
-  const bool row_ok = r < w.n * G;
-  const int tok = row_ok ? r / G : 0;
-  const int head = w.hk * G + (row_ok ? r - tok * G : 0);
+  const LaneRow row(w, G, (KW > 1 ? 0 : wave) * 32 + l32);
   int limit = ke;                    // keys before this one are seen
-  if (row_ok && a.causal && w.first + tok + 1 < limit) limit = w.first + tok + 1 < 0 ? 0 : (int)(w.first + tok + 1);
+  if (row.ok && a.causal && w.first + row.tok + 1 < limit) limit = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
   int least = limit;                 // of all rows of the wave: tiles below it need no mask
   for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
   least = __builtin_amdgcn_readfirstlane(least);
@@ -389,12 +400,12 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   constexpr int NQ = C::F32 ? DHP / 8 : DHP / 16;
   u32x4 qf[NQ];
   {
-    const T *qp = (const T *)a.q + (int64_t)(w.q0 + tok) * a.ldq + (int64_t)head * dh;
+    const T *qp = (const T *)a.q + (int64_t)(w.q0 + row.tok) * a.ldq + (int64_t)row.head * dh;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int c = C::F32 ? i * 8 + hi * 4 : i * 16 + hi * 8;
       qf[i] = u32x4{0, 0, 0, 0};
-      if (row_ok && c < dh) qf[i] = *reinterpret_cast<const u32x4 *>(qp + c);
+      if (row.ok && c < dh) qf[i] = *reinterpret_cast<const u32x4 *>(qp + c);
     }
   }
   TileLoader<C, T, PAGED> ld(a, w, lane, KW > 1 ? 0 : wave, kb, ke);
@@ -406,7 +417,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   unsigned *const hidden = hidden_all[KW > 1 ? wave : 0];
   const bool zoned = w.zone < ke;
   const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
-  if (zoned) {
+  if (KW > 1 || zoned) {
     if ((KW > 1 ? lane : (int)threadIdx.x) < ZONE * (TK / 32)) hidden[KW > 1 ? lane : threadIdx.x] = 0;
     if constexpr (NW > 1) __syncthreads();
   }
@@ -541,10 +552,6 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       work_tile(t, 0, now);
     }
   }
-  if (zoned) {
-    if constexpr (NW > 1) __syncthreads();
-    ld.template add_hidden<CB>(hidden, ZONE, zone_tile, row_ok ? limit : 0, hi, o);
-  }
   float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
 
   if constexpr (KW > 1) {
@@ -578,7 +585,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
     }
     m_run = m_all;
     // the lane's channels: 4 hi + 8 (wave + 4 i) .. + 3
-    if (row_ok) {
+    if (row.ok) {
       const float inv = l_tot != 0.f ? 1.f / l_tot : 0.f;
 #pragma unroll
       for (int i = 0; i < (DHP / 8 + KW - 1) / KW; ++i) {
@@ -593,22 +600,35 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
             acc[2] = fmaf(wt[v], x.z, acc[2]);
             acc[3] = fmaf(wt[v], x.w, acc[3]);
           }
-          put4<T>(a, w.sp, w.q0 + tok, head, c, inv, acc[0], acc[1], acc[2], acc[3]);
+          put4<T>(a, w.sp, w.q0 + row.tok, row.head, c, inv, acc[0], acc[1], acc[2], acc[3]);
         }
       }
     }
-    if (wave != 0) return;
-  } else if (row_ok) {
+  } else if (row.ok) {
     const float inv = l_tot != 0.f ? 1.f / l_tot : 0.f;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int c = cb * 32 + 8 * g + 4 * hi;
-        if (c < dh) put4<T>(a, w.sp, w.q0 + tok, head, c, inv, o[cb][4 * g], o[cb][4 * g + 1], o[cb][4 * g + 2], o[cb][4 * g + 3]);
+        if (c < dh) put4<T>(a, w.sp, w.q0 + row.tok, row.head, c, inv, o[cb][4 * g], o[cb][4 * g + 1], o[cb][4 * g + 2], o[cb][4 * g + 3]);
       }
   }
-  if (row_ok && hi == 0) put_stats(a, w.sp, w.q0 + tok, head, m_run * p.sl2, l_tot);
+  if (row.ok && hi == 0 && (KW == 1 || wave == 0)) put_stats(a, w.sp, w.q0 + row.tok, row.head, m_run * p.sl2, l_tot);
+  if (w.zone < w.ke) {
+    if constexpr (KW > 1) {
+      // wave v's share of the keys, as above
+      const int q = ((w.ke - w.kb + KW - 1) / KW + TK - 1) / TK * TK;
+#pragma unroll 1
+      for (int v = 0; v < KW; ++v) {
+        const int b = min(w.ke, w.kb + v * q), e = min(w.ke, b + q);
+        if (w.zone < e) add_hidden<T, PAGED, C::ROWS, 64 * C::WAVES>(p, w, hidden_all[v], ZONE * (TK / 32), b + (w.zone > b ? (w.zone - b) / TK : 0) * TK, e);
+      }
+    } else {
+      __syncthreads();
+      add_hidden<T, PAGED, C::ROWS, 64 * C::WAVES>(p, w, hidden, ZONE * (TK / 32), kb + zone_tile * TK, ke);
+    }
+  }
 }
 
 // The tile kernel for launches with many rows (bf16): four waves of 64 rows, one workgroup per CU.
@@ -640,25 +660,21 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
   const int tiles = (ke - kb + TK - 1) / TK;
 
   // ---- the lane's two rows
-  int tok[2], head[2], limit[2];
-  bool row_ok[2];
+  int limit[2];
   int least = ke;
   u32x4 qf[2][KS];
 #pragma unroll
   for (int rb = 0; rb < 2; ++rb) {
-    const int r = w.r_first + wave * 64 + rb * 32 + l32;
-    row_ok[rb] = r < w.n * G;
-    tok[rb] = row_ok[rb] ? r / G : 0;
-    head[rb] = w.hk * G + (row_ok[rb] ? r - tok[rb] * G : 0);
+    const LaneRow row(w, G, wave * 64 + rb * 32 + l32);
     limit[rb] = ke;
-    if (row_ok[rb] && a.causal && w.first + tok[rb] + 1 < ke) limit[rb] = w.first + tok[rb] + 1 < 0 ? 0 : (int)(w.first + tok[rb] + 1);
+    if (row.ok && a.causal && w.first + row.tok + 1 < ke) limit[rb] = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
     least = min(least, limit[rb]);
-    const T *qp = (const T *)a.q + (int64_t)(w.q0 + tok[rb]) * a.ldq + (int64_t)head[rb] * dh;
+    const T *qp = (const T *)a.q + (int64_t)(w.q0 + row.tok) * a.ldq + (int64_t)row.head * dh;
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
       const int c = i * 16 + hi * 8;
       qf[rb][i] = u32x4{0, 0, 0, 0};
-      if (row_ok[rb] && c < dh) qf[rb][i] = *reinterpret_cast<const u32x4 *>(qp + c);
+      if (row.ok && c < dh) qf[rb][i] = *reinterpret_cast<const u32x4 *>(qp + c);
     }
   }
   for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
@@ -825,7 +841,8 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
     ld.load(1);
     unsigned groups_next = ld.groups;
     // the values "before tile 0" have weight zero, so that they must be finite: the other V buffer's second half
-    for (int e = threadIdx.x; e < V_HALF / 16; e += 256) *reinterpret_cast<u32x4 *>(vring + C::VTILE_B + V_HALF + e * 16) = u32x4{0, 0, 0, 0};
+    static_assert(V_HALF % 1024 == 0, "whole kilobytes, one a wave and turn");
+    for (int i = wave; i < V_HALF / 1024; i += 4) *reinterpret_cast<u32x4 *>(vring + C::VTILE_B + V_HALF + i * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
     meet();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -855,27 +872,28 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
       groups_next = ld.groups;
     }
     last_values((tiles & 1 ? 0 : C::VTILE_B) + V_HALF);
-    if (zoned) {
-      __syncthreads();
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) ld.template add_hidden<CB>(hidden, ZONE, zone_tile, row_ok[rb] ? limit[rb] : 0, hi, o[rb]);
-    }
   }
 
+  int lane_again = l32;                          // the rows are worked out anew here, not kept in registers through the loop
+  asm volatile("" : "+v"(lane_again));
 #pragma unroll
   for (int rb = 0; rb < 2; ++rb) {
     const float l = l_run[rb] + __shfl_xor(l_run[rb], 32, kWave);
-    if (!row_ok[rb]) continue;
+    const LaneRow row(w, G, wave * 64 + rb * 32 + lane_again);
+    if (!row.ok) continue;
     const float inv = l != 0.f ? 1.f / l : 0.f;
-    const int64_t row = w.q0 + tok[rb];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int c = cb * 32 + 8 * g + 4 * hi;
-        if (c < dh) put4<T>(a, w.sp, row, head[rb], c, inv, o[rb][cb][4 * g], o[rb][cb][4 * g + 1], o[rb][cb][4 * g + 2], o[rb][cb][4 * g + 3]);
+        if (c < dh) put4<T>(a, w.sp, w.q0 + row.tok, row.head, c, inv, o[rb][cb][4 * g], o[rb][cb][4 * g + 1], o[rb][cb][4 * g + 2], o[rb][cb][4 * g + 3]);
       }
-    if (hi == 0) put_stats(a, w.sp, row, head[rb], ref[rb], l);
+    if (hi == 0) put_stats(a, w.sp, w.q0 + row.tok, row.head, ref[rb], l);
+  }
+  if (zoned) {
+    __syncthreads();
+    add_hidden<T, PAGED, 256, 256>(p, w, hidden, ZONE * 2, kb + zone_tile * TK, ke);
   }
 }
 
