@@ -404,7 +404,7 @@ int pf_gemm_read_ahead(int M, int N, int K);
  * does not read: the calls can be captured into a graph and replayed with other contents.  Every value read from them is
  * bounded before it is used, so wrong ones give wrong rows and no access outside the arrays.
  * The conventions above hold here too: nothing is allocated, nothing synchronises, errors of arguments are found before
- * anything is launched.   Calls with no rows or no sequences do nothing and may pass NULL pointers; a call
+ * anything is launched.  Calls with no rows or no sequences do nothing and may pass NULL pointers; a call
  * takes at most 2^24 rows (attention: as many workgroups of 32 rows).  Outputs may not overlap inputs
  * except where it is said.  pf_last_error(NULL) says what was wrong.
  * ---------------------------------------------------------------------------------------------- */
@@ -500,8 +500,8 @@ pf_status pf_op_attention_packed(int dtype, const void *q, int64_t ldq, const vo
                                  const int32_t *cu_q, const int32_t *cu_k, int n_seqs, int total_q, int total_k, int n_heads,
                                  int kv_heads, int head_dim, float scale, int causal, void *out, int64_t ldo, float *lse, void *ws,
                                  size_t ws_bytes, void *stream);
-/* Host-only: the kernel that an attention launch of these sizes runs (a kernel trace shows it with its types in front), and the
- * number of chunks of the key range it is cut into; "" where the sizes are refused.  Per-thread storage, valid until the next call. */
+/* Host-only: the kernel that an attention launch of these sizes runs (a kernel trace shows it with the flags for pages and mask in
+ * between), and the number of chunks of the key range it is cut into; "" where the sizes are refused.  Per-thread storage, valid until the next call. */
 const char *pf_attention_rows_kernel_name(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv,
                                           int *chunks);
 

@@ -133,7 +133,7 @@ struct Work {
   int64_t first;          // slot of query 0
   int zone;               // keys from here to ke are hidden from some row of the tile (ke: none are)
 };
-template <bool PAGED, int ROWS, int UNIT>
+template <bool PAGED, bool CAUSAL, int ROWS, int UNIT>
 __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Work &w) {
   const RowsAttn &a = p.a;
   const int G = p.group;
@@ -149,10 +149,10 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
   w.r_first = (slot - (w.q0 * G / ROWS + w.s)) * ROWS;
   if (w.r_first < 0 || w.r_first >= w.n * G) return false;
   const int kn = sequence_keys<PAGED>(a, w.s, w.k0);
-  w.first = !a.causal ? 0 : PAGED ? a.first[w.s] : kn - w.n;
+  w.first = !CAUSAL ? 0 : PAGED ? a.first[w.s] : kn - w.n;
   const int t_last = (w.r_first + ROWS < w.n * G ? w.r_first + ROWS - 1 : w.n * G - 1) / G;
   w.k_end = kn;
-  if (a.causal && w.first + t_last + 1 < w.k_end) w.k_end = w.first + t_last + 1 < 0 ? 0 : (int)(w.first + t_last + 1);
+  if (CAUSAL && w.first + t_last + 1 < w.k_end) w.k_end = w.first + t_last + 1 < 0 ? 0 : (int)(w.first + t_last + 1);
   w.kb = 0;
   w.ke = w.k_end;
   if (a.splits > 1) {
@@ -167,7 +167,7 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
     w.ke = (int)min((int64_t)w.k_end, (w.sp + 1) * c);
   }
   w.zone = w.ke;
-  if (a.causal && w.first + w.r_first / G + 1 < w.ke) w.zone = w.first + w.r_first / G + 1 < 0 ? 0 : (int)(w.first + w.r_first / G + 1);
+  if (CAUSAL && w.first + w.r_first / G + 1 < w.ke) w.zone = w.first + w.r_first / G + 1 < 0 ? 0 : (int)(w.first + w.r_first / G + 1);
   return true;
 }
 
@@ -367,7 +367,7 @@ __device__ __forceinline__ void add_hidden(const RowsKernelArgs &p, const Work &
     }
 }
 
-template <typename T, int DHP, bool PAGED, int NW, int KW>
+template <typename T, int DHP, bool PAGED, bool CAUSAL, int NW, int KW>
 __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void attn_rows_kernel(RowsKernelArgs p) {
   using C = Tile<T, DHP, NW, KW>;
   constexpr int TK = C::TK, NB = C::NB, CB = C::CB;
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   const int l32 = lane & 31, hi = lane >> 5;
   const int dh = a.head_dim, G = p.group;
   Work w;
-  if (!find_work<PAGED, C::ROWS, 64 * KW>(p, lane, w)) return;   // chunks: whole tiles for all waves
+  if (!find_work<PAGED, CAUSAL, C::ROWS, 64 * KW>(p, lane, w)) return;   // chunks: whole tiles for all waves
   int kb = w.kb, ke = w.ke;
   if constexpr (KW > 1) {            // the wave's quarter
     const int q = ((ke - kb + KW - 1) / KW + TK - 1) / TK * TK;
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   // ---- the lane's row
   const LaneRow row(w, G, (KW > 1 ? 0 : wave) * 32 + l32);
   int limit = ke;                    // keys before this one are seen
-  if (row.ok && a.causal && w.first + row.tok + 1 < limit) limit = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
+  if (CAUSAL && row.ok && w.first + row.tok + 1 < limit) limit = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
   int least = limit;                 // of all rows of the wave: tiles below it need no mask
   for (int o = 32; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
   least = __builtin_amdgcn_readfirstlane(least);
@@ -415,9 +415,9 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   constexpr int ZONE = (C::ROWS + TK - 2) / TK + 1;              // tiles it can touch
   __shared__ unsigned hidden_all[KW][ZONE * (TK / 32)];
   unsigned *const hidden = hidden_all[KW > 1 ? wave : 0];
-  const bool zoned = w.zone < ke;
+  const bool zoned = CAUSAL && w.zone < ke;
   const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
-  if (KW > 1 || zoned) {
+  if ((CAUSAL && KW > 1) || zoned) {
     if ((KW > 1 ? lane : (int)threadIdx.x) < ZONE * (TK / 32)) hidden[KW > 1 ? lane : threadIdx.x] = 0;
     if constexpr (NW > 1) __syncthreads();
   }
@@ -615,7 +615,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
       }
   }
   if (row.ok && hi == 0 && (KW == 1 || wave == 0)) put_stats(a, w.sp, w.q0 + row.tok, row.head, m_run * p.sl2, l_tot);
-  if (w.zone < w.ke) {
+  if (CAUSAL && w.zone < w.ke) {
     if constexpr (KW > 1) {
       // wave v's share of the keys, as above
       const int q = ((w.ke - w.kb + KW - 1) / KW + TK - 1) / TK * TK;
@@ -642,7 +642,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
 // any ref while nothing overflows, and the sum of a lane's weights, which is formed anyway, says when it has grown too
 // large.  Only then (and on the first keys of a row, whose ref is -inf) is the maximum found, the reference moved, and the
 // step's weights formed again.
-template <int DHP, int KS, bool PAGED>
+template <int DHP, int KS, bool PAGED, bool CAUSAL>
 __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kernel(RowsKernelArgs p) {
   using T = bf16_t;
   using C = Tile<T, DHP, 4, 1>;
@@ -655,7 +655,7 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
   const int l32 = lane & 31, hi = lane >> 5;
   const int dh = a.head_dim, G = p.group;
   Work w;
-  if (!find_work<PAGED, 256, 64>(p, lane, w)) return;
+  if (!find_work<PAGED, CAUSAL, 256, 64>(p, lane, w)) return;
   const int kb = __builtin_amdgcn_readfirstlane(w.kb), ke = __builtin_amdgcn_readfirstlane(w.ke);
   const int tiles = (ke - kb + TK - 1) / TK;
 
@@ -667,7 +667,7 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
   for (int rb = 0; rb < 2; ++rb) {
     const LaneRow row(w, G, wave * 64 + rb * 32 + l32);
     limit[rb] = ke;
-    if (row.ok && a.causal && w.first + row.tok + 1 < ke) limit[rb] = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
+    if (CAUSAL && row.ok && w.first + row.tok + 1 < ke) limit[rb] = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
     least = min(least, limit[rb]);
     const T *qp = (const T *)a.q + (int64_t)(w.q0 + row.tok) * a.ldq + (int64_t)row.head * dh;
 #pragma unroll
@@ -811,7 +811,7 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
   // keys with infinities or NaN among those that some row does not see (fewer than 256)
   constexpr int ZONE = 5;                                         // tiles they can touch
   __shared__ unsigned hidden[ZONE * 2];
-  const bool zoned = w.zone < ke;
+  const bool zoned = CAUSAL && w.zone < ke;
   const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
   if (zoned) {
     if (threadIdx.x < ZONE * 2) hidden[threadIdx.x] = 0;
@@ -983,45 +983,56 @@ hipError_t launch_join(const RowsAttn &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int DHP, bool PAGED, int NW, int KW>
+template <typename T, int DHP, bool PAGED, bool CAUSAL, int NW, int KW>
 hipError_t launch_shape(const RowsAttn &a, hipStream_t s) {
   using C = Tile<T, DHP, NW, KW>;
-  if (hipError_t e = allow_dynamic_lds<&attn_rows_kernel<T, DHP, PAGED, NW, KW>, C::SMEM>(); e != hipSuccess) return e;
+  if (hipError_t e = allow_dynamic_lds<&attn_rows_kernel<T, DHP, PAGED, CAUSAL, NW, KW>, C::SMEM>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   p.slots = (int)((int64_t)a.total_q * p.group / C::ROWS) + a.n_seqs;
   const int64_t grid = (int64_t)p.slots * a.splits * a.kv_heads;
-  attn_rows_kernel<T, DHP, PAGED, NW, KW><<<dim3((unsigned)grid), 64 * C::WAVES, C::SMEM, s>>>(p);
+  attn_rows_kernel<T, DHP, PAGED, CAUSAL, NW, KW><<<dim3((unsigned)grid), 64 * C::WAVES, C::SMEM, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_join<T>(a, s);
 }
 
-template <int DHP, int KS, bool PAGED>
+template <int DHP, int KS, bool PAGED, bool CAUSAL>
 hipError_t launch_wide(const RowsAttn &a, hipStream_t s) {
   constexpr int smem = Tile<bf16_t, DHP, 4, 1>::SMEM, alone = smem > 82 * 1024 ? smem : 82 * 1024;
-  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, KS, PAGED>, alone>(); e != hipSuccess) return e;
+  if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, KS, PAGED, CAUSAL>, alone>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   p.slots = (int)((int64_t)a.total_q * p.group / 256) + a.n_seqs;
   // Two workgroups of head size 64 fit a CU, and the dispatcher puts them there while other CUs are idle: where there are no more
   // than CUs, each asks for more than half a CU's LDS (4 x 512 rows x 24 heads over 4250 keys: 132 -> 95 us).
   const bool few = (int64_t)a.total_q * p.group / 256 * a.kv_heads * a.splits <= 256;
-  attn_rows_wide_kernel<DHP, KS, PAGED><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, few ? alone : smem, s>>>(p);
+  attn_rows_wide_kernel<DHP, KS, PAGED, CAUSAL><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, few ? alone : smem, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_join<bf16_t>(a, s);
 }
 
-template <typename T, int DHP, bool PAGED>
+template <typename T, int DHP, bool PAGED, bool CAUSAL>
 hipError_t launch_rows_of(const RowsAttn &a, hipStream_t s) {
-  if (a.shape == ROWS_KEYS) return launch_shape<T, DHP, PAGED, 1, 4>(a, s);
+  if (a.shape == ROWS_KEYS) return launch_shape<T, DHP, PAGED, CAUSAL, 1, 4>(a, s);
   if constexpr (sizeof(T) == 2) {
-    if (a.shape == ROWS_WIDE) return DHP == 96 && a.head_dim <= 80 ? launch_wide<DHP, DHP == 96 ? 5 : DHP / 16, PAGED>(a, s) : launch_wide<DHP, DHP / 16, PAGED>(a, s);
+    if (a.shape == ROWS_WIDE) {
+      // head sizes up to 80: five steps of 16 channels for the scores, of the six that a row of 96 has
+      if constexpr (DHP == 96) {
+        if (a.head_dim <= 80) return launch_wide<DHP, 5, PAGED, CAUSAL>(a, s);
+      }
+      return launch_wide<DHP, DHP / 16, PAGED, CAUSAL>(a, s);
+    }
   }
-  return launch_shape<T, DHP, PAGED, 4, 1>(a, s);
+  return launch_shape<T, DHP, PAGED, CAUSAL, 4, 1>(a, s);
 }
-template <typename T, bool PAGED>
+template <typename T, bool PAGED, bool CAUSAL>
 hipError_t launch_dim(const RowsAttn &a, hipStream_t s) {
-  if (a.head_dim <= 64) return launch_rows_of<T, 64, PAGED>(a, s);
-  if (a.head_dim <= 96) return launch_rows_of<T, 96, PAGED>(a, s);
-  return launch_rows_of<T, 128, PAGED>(a, s);
+  if (a.head_dim <= 64) return launch_rows_of<T, 64, PAGED, CAUSAL>(a, s);
+  if (a.head_dim <= 96) return launch_rows_of<T, 96, PAGED, CAUSAL>(a, s);
+  return launch_rows_of<T, 128, PAGED, CAUSAL>(a, s);
+}
+template <typename T>
+hipError_t launch_type(const RowsAttn &a, hipStream_t s) {
+  if (a.pages.table) return a.causal ? launch_dim<T, true, true>(a, s) : launch_dim<T, true, false>(a, s);
+  return a.causal ? launch_dim<T, false, true>(a, s) : launch_dim<T, false, false>(a, s);
 }
 
 }  // namespace
@@ -1078,9 +1089,7 @@ RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int k
 }
 
 hipError_t launch_rows_attention(const RowsAttn &a, hipStream_t s) {
-  const bool paged = a.pages.table != nullptr;
-  if (a.dt == DT_BF16) return paged ? launch_dim<bf16_t, true>(a, s) : launch_dim<bf16_t, false>(a, s);
-  return paged ? launch_dim<float, true>(a, s) : launch_dim<float, false>(a, s);
+  return a.dt == DT_BF16 ? launch_type<bf16_t>(a, s) : launch_type<float>(a, s);
 }
 
 }  // namespace pf
