@@ -557,11 +557,15 @@ def pf_op_rope(x, rope, pos, head_dim, out=None):
     index, dt = x.get_device(), _DT.get(x.dtype)
     if index < 0 or dt is None or not _good_rows(x, x.dtype, index):
         _rows("x", x)
-    tokens, heads = x.shape[0], _heads("x", x, head_dim)
+    tokens, width = x.shape
+    heads = _heads("x", x, head_dim)
     _positions(rope, pos, tokens, index, x.device)
-    out = _like(x) if out is None else _out("out", out, x.shape, x.dtype, x.device)
-    _launch(index, (_lib or load_library()).pf_op_rope, dt, C.byref(rope), pos.data_ptr(), x.data_ptr(), _ld(x), out.data_ptr(),
-            _ld(out), tokens, heads, head_dim)
+    if out is None:
+        out, ldo = _like(x), width
+    else:
+        ldo = _ld(_out("out", out, x.shape, x.dtype, x.device))
+    _launch(index, (_lib or load_library()).pf_op_rope, dt, C.byref(rope), pos.data_ptr(), x.data_ptr(), _ld(x), out.data_ptr(), ldo,
+            tokens, heads, head_dim)
     return out
 
 
@@ -624,8 +628,11 @@ def pf_op_kv_append(pages, k, v, cu, first, rope=None, pos=None, q=None, q_out=N
         if q.shape[0] != tokens:
             raise PfError(-3, f"q: {q.shape[0]} rows, k has {tokens}")
         heads = _heads("q", q, pages.head_dim)
-        q_out = _like(q) if q_out is None else _out("q_out", q_out, q.shape, dt, dev)
-        q_args = (q.data_ptr(), _ld(q), q_out.data_ptr(), _ld(q_out), heads)
+        if q_out is None:
+            q_out, ldo = _like(q), heads * pages.head_dim
+        else:
+            ldo = _ld(_out("q_out", q_out, q.shape, dt, dev))
+        q_args = (q.data_ptr(), _ld(q), q_out.data_ptr(), ldo, heads)
     _launch(index, (_lib or load_library()).pf_op_kv_append, _DT[dt], pages.ref, k.data_ptr(), _ld(k), v.data_ptr(), _ld(v),
             cu.data_ptr(), first.data_ptr(), tokens, None if rope is None else C.byref(rope),
             None if rope is None else pos.data_ptr(), *q_args)
@@ -639,11 +646,14 @@ def _rows_ws_bytes(*sizes):
 
 def _attention_buffers(q, heads, kv_heads, head_dim, n_seqs, max_kv, out, want_lse):
     """out, lse, and (address of out, its row stride, address of lse, workspace, its bytes) for the call."""
-    out = _like(q) if out is None else _out("out", out, q.shape, q.dtype, q.device)
+    if out is None:
+        out, ldo = _like(q), heads * head_dim
+    else:
+        ldo = _ld(_out("out", out, q.shape, q.dtype, q.device))
     lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=q.device) if want_lse else None
     n = _rows_ws_bytes(_DT[q.dtype], q.shape[0], n_seqs, heads, kv_heads, head_dim, max_kv)
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    return out, lse, ws, (out.data_ptr(), _ld(out), None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), n)
+    return out, lse, ws, (out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), n)
 
 
 def pf_op_attention_packed(q, k, v, cu_q, cu_k, head_dim, causal=False, scale=None, out=None, want_lse=False):
@@ -756,13 +766,18 @@ def pf_op_norm_residual(y, x, post=None, pre=None, gate=None, gate_tanh=False, x
     ms2, sh_at = _vectors("shift", shift, d, n_seqs, index, dev)
     if scale is not None and shift is not None and ms != ms2:
         raise PfError(-3, f"scale and shift: {ms} and {ms2} elements between sequences")
-    x_out = _like(x) if x_out is None else _out("x_out", x_out, x.shape, torch.float32, dev)
-    if want_h:
-        h_out = _like(x, dtype) if h_out is None else _out("h_out", h_out, x.shape, dtype, dev)
-        h_args = (h_out.data_ptr(), _ld(h_out))
+    if x_out is None:
+        x_out, ldxo = _like(x), d
     else:
+        ldxo = _ld(_out("x_out", x_out, x.shape, torch.float32, dev))
+    if not want_h:
         h_args = (None, 0)
+    elif h_out is None:
+        h_out = _like(x, dtype)
+        h_args = (h_out.data_ptr(), d)
+    else:
+        h_args = (h_out.data_ptr(), _ld(_out("h_out", h_out, x.shape, dtype, dev)))
     _launch(index, (_lib or load_library()).pf_op_norm_residual, _DT[dtype], *y_args, None if post is None else post.ref, g_at, gs,
-            int(gate_tanh), x_scale, x.data_ptr(), _ld(x), x_out.data_ptr(), _ld(x_out), None if pre is None else pre.ref, sh_at,
+            int(gate_tanh), x_scale, x.data_ptr(), _ld(x), x_out.data_ptr(), ldxo, None if pre is None else pre.ref, sh_at,
             sc_at, max(ms, ms2), *h_args, None if cu is None else cu.data_ptr(), n_seqs or 0, rows, d)
     return x_out, h_out if want_h else None

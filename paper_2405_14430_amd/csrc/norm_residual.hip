@@ -6,6 +6,8 @@
 // Bound by memory: y and x are read once, x' and h written once, a row lives in registers between its (up to four) sums.
 // A row belongs to one wave, or to 2, 4 or 8 that add their sums up through LDS: few rows need the waves, many rows do not.
 // The variance is the mean of (x - mean)^2 over the registers, a second sum and no difference of squares.  Sums in 32 bits.
+#include <type_traits>
+
 #include "requests.h"
 
 namespace pf {
@@ -13,15 +15,11 @@ namespace {
 
 constexpr int kLayer = PF_NORM_LAYER;
 
-template <typename T> __device__ __forceinline__ void load4(const T *p, float *o) {
-  if constexpr (sizeof(T) == 2) {
-    const bf16x4 v = *reinterpret_cast<const bf16x4 *>(p);
+template <typename T, bool ONCE = false> __device__ __forceinline__ void load4(const T *p, float *o) {
+  using V = std::conditional_t<sizeof(T) == 2, bf16x4, f32x4>;
+  const V v = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const V *>(p)) : *reinterpret_cast<const V *>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (float)v[i];
-  } else {
-    const float4 v = *reinterpret_cast<const float4 *>(p);
-    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
-  }
+  for (int i = 0; i < 4; ++i) o[i] = (float)v[i];
 }
 template <typename T> __device__ __forceinline__ void store4(T *p, const float *o) {
   if constexpr (sizeof(T) == 2) {
@@ -79,20 +77,25 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
   } vec;
   const float *gp = a.gate ? a.gate + seg * a.gate_stride : nullptr;
   const float *scp = a.scale ? a.scale + seg * a.mod_stride : nullptr, *shp = a.shift ? a.shift + seg * a.mod_stride : nullptr;
-  auto get = [&](auto *p, float (&o)[4], int c, float none) __attribute__((always_inline)) {
+  auto get_as = [&](auto once, auto *p, float (&o)[4], int c, float none) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = none;
-    if (p && c < d) load4(p + c, o);
+    if (p && c < d) load4<std::remove_const_t<std::remove_pointer_t<decltype(p)>>, decltype(once)::value>(p + c, o);
   };
+  auto get = [&](auto *p, float (&o)[4], int c, float none) __attribute__((always_inline)) { get_as(std::false_type{}, p, o, c, none); };
   const T *wyp = (const T *)a.post.weight, *byp = (const T *)a.post.bias, *wxp = (const T *)a.pre.weight, *bxp = (const T *)a.pre.bias;
 
   float x[NV][4], y[NV][4];
   const float *xp = a.x + row * a.ldx;
   const T *yp = a.y ? (const T *)a.y + row * a.ldy : nullptr;
+  auto rows = [&](auto once) __attribute__((always_inline)) {
 #pragma unroll
-  for (int v = 0; v < NV; ++v) get(xp, x[v], c0 + v * STEP, 0.f);
+    for (int v = 0; v < NV; ++v) get_as(once, xp, x[v], c0 + v * STEP, 0.f);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) get(yp, y[v], c0 + v * STEP, 0.f);
+    for (int v = 0; v < NV; ++v) get_as(once, yp, y[v], c0 + v * STEP, 0.f);
+  };
+  if (a.once) rows(std::true_type{});
+  else rows(std::false_type{});
   if constexpr (EARLY) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -223,8 +226,11 @@ hipError_t launch_w(const NormResidual &a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_norm_residual(const NormResidual &a, hipStream_t s) {
-  if (a.rows <= 0) return hipSuccess;
+hipError_t launch_norm_residual(const NormResidual &args, hipStream_t s) {
+  if (args.rows <= 0) return hipSuccess;
+  NormResidual a = args;
+  const int64_t el = (int64_t)dt_size(a.dt);
+  a.once = (int64_t)a.rows * a.d * (4 + (a.y ? el : 0) + (a.x_out ? 4 : 0) + (a.h ? el : 0)) > kReadOnceBytes;
   // Waves per row: enough that a lane holds at most eight groups of four channels, and twice or four times as many while
   // the launch has fewer than 4096 waves and a wave still has two groups per lane.
   int w = 1;

@@ -47,6 +47,12 @@ inline Pages pages_of(const pf_kv_pages &p) {
   return Pages{p.k, p.v, p.k_page_stride, p.v_page_stride, p.table, p.n_pages, __builtin_ctz((unsigned)p.page_size), p.max_pages};
 }
 
+// Calls that move more bytes than the 256 MiB cache in front of the memory holds read their rows with non-temporal loads, which do not
+// push out what is being written; smaller ones find rows there that the kernel before has left, and lose by it (append of 16384 rows
+// of 32 + 2 x 8 heads of 128, bf16, 400 MB: 81 -> 66 us, 8192 rows 34 -> 37; norm of 8192 rows of 4096, bf16, 403 MB:
+// 120 -> 109, 16384 rows of 1152, 226 MB: 48 -> 55; the same rows again and again).
+constexpr int64_t kReadOnceBytes = 256ll << 20;
+
 struct RopeRows {
   int dt;
   const pf_rope *rope;   // nullptr: rows are copied (append only)
@@ -73,6 +79,7 @@ struct NormResidual {
   void *h; int64_t ldh;
   const int32_t *cu; int n_seqs;
   int rows, d;
+  bool once;               // x and y are read with non-temporal loads (set at the launch)
 };
 hipError_t launch_norm_residual(const NormResidual &a, hipStream_t s);
 

@@ -31,9 +31,13 @@ struct RowsK {
   int n_seqs;
 };
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 template <typename T, int V> struct Unit { T e[V]; };
-template <typename T, int V> __device__ __forceinline__ void load_unit(const T *p, Unit<T, V> &u) {
-  if constexpr (sizeof(T) * V == 16) *reinterpret_cast<uint4 *>(&u) = *reinterpret_cast<const uint4 *>(p);
+template <bool ONCE, typename T, int V> __device__ __forceinline__ void load_unit(const T *p, Unit<T, V> &u) {
+  if constexpr (sizeof(T) * V == 16) {
+    const u32x4 *from = reinterpret_cast<const u32x4 *>(p);
+    *reinterpret_cast<u32x4 *>(&u) = ONCE ? __builtin_nontemporal_load(from) : *from;
+  }
   else if constexpr (sizeof(T) * V == 8) *reinterpret_cast<uint2 *>(&u) = *reinterpret_cast<const uint2 *>(p);
   else u = *reinterpret_cast<const Unit<T, V> *>(p);
 }
@@ -44,7 +48,8 @@ template <typename T, int V> __device__ __forceinline__ void store_unit(T *p, co
 }
 
 // HALF: pairs half an axis apart (each axis' half a multiple of V), else neighbours (V even).  TOK tokens per workgroup.
-template <typename T, int V, bool HALF, bool APPEND, int TOK>
+// ONCE: rows are read with non-temporal loads (units of 16 bytes).
+template <typename T, int V, bool HALF, bool APPEND, int TOK, bool ONCE>
 __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
   __shared__ float2 cs[TOK][kMaxPairs];
   __shared__ int64_t k_at[TOK], v_at[TOK];
@@ -129,7 +134,7 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
     if (copy || (HALF && u >= rot_units)) {
       const int c = copy ? u * V : rk.rot + (u - rot_units) * V;
       Unit<T, V> x;
-      load_unit(src + c, x);
+      load_unit<ONCE>(src + c, x);
       store_unit(dst + c, x);
     } else if constexpr (HALF) {
       // pairs u * V .. + V - 1 lie in one axis: its first channel, and half its width
@@ -139,8 +144,8 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
       const int end = p < b1 ? b1 : p < b2 ? b2 : pairs;
       const int c = 2 * beg + (p - beg), hw = end - beg;
       Unit<T, V> x, y;
-      load_unit(src + c, x);
-      load_unit(src + c + hw, y);
+      load_unit<ONCE>(src + c, x);
+      load_unit<ONCE>(src + c + hw, y);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float2 w = cs[t][p + i];
@@ -153,7 +158,7 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
     } else {
       const int c = u * V;
       Unit<T, V> x;
-      load_unit(src + c, x);
+      load_unit<ONCE>(src + c, x);
 #pragma unroll
       for (int i = 0; i < V; i += 2) {
         if (c + i < rk.rot) {   // a unit may reach behind the channels that turn
@@ -168,17 +173,22 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
   }
 }
 
-template <typename T, int V, bool HALF, bool APPEND>
+template <typename T, int V, bool HALF, bool APPEND, bool ONCE>
 hipError_t launch_tok(const RopeK &rk, const RowsK &a, hipStream_t s) {
-  // four tokens per workgroup once that still leaves four workgroups per CU; a token's heads are split over workgroups where
-  // there are few tokens
-  if (a.tokens >= 4096) {
-    rope_rows_kernel<T, V, HALF, APPEND, 4><<<dim3((a.tokens + 3) / 4), 256, 0, s>>>(rk, a);
+  // Workgroups of several tokens where a token has less than 256 threads' work and there are tokens for 2048 of them or more (4
+  // tokens, 2, 1: 8192 tokens of 16 heads of 64, bf16, half layout, 64 units: 7.4, 8.3 and 9.0 us; append of 16384 of 16 + 2 x 16 heads
+  // of 64, 256 units: 34.4, 33.1, 34.1; 16384 of 32 + 2 x 8 heads of 128, 448 units: 81, 79, 74).  A token's heads are split over
+  // workgroups where there are few tokens.
+  const int turned = HALF ? (rk.rot / 2 + a.head_dim - rk.rot) / V : a.head_dim / V;
+  const int units = (a.n_heads + a.kv_heads) * turned + a.kv_heads * (a.head_dim / V);
+  if (a.tokens >= 4096 && units <= 128) {
+    rope_rows_kernel<T, V, HALF, APPEND, 4, ONCE><<<dim3((a.tokens + 3) / 4), 256, 0, s>>>(rk, a);
+  } else if (a.tokens >= 4096 && units <= 256) {
+    rope_rows_kernel<T, V, HALF, APPEND, 2, ONCE><<<dim3((a.tokens + 1) / 2), 256, 0, s>>>(rk, a);
   } else {
-    const int units = (a.n_heads + 2 * a.kv_heads) * (a.head_dim / V);
     int y = (units + 255) / 256;
     while (y > 1 && (int64_t)a.tokens * y > 4096) y = (y + 1) / 2;
-    rope_rows_kernel<T, V, HALF, APPEND, 1><<<dim3(a.tokens, y), 256, 0, s>>>(rk, a);
+    rope_rows_kernel<T, V, HALF, APPEND, 1, ONCE><<<dim3(a.tokens, y), 256, 0, s>>>(rk, a);
   }
   return hipGetLastError();
 }
@@ -186,11 +196,12 @@ hipError_t launch_tok(const RopeK &rk, const RowsK &a, hipStream_t s) {
 template <typename T, bool APPEND>
 hipError_t launch_layout(const RopeK &rk, const RowsK &a, bool half, int align, hipStream_t s) {
   constexpr int V16 = 16 / (int)sizeof(T);
-  if (!half) return launch_tok<T, V16, false, APPEND>(rk, a, s);
+  const bool once = (int64_t)a.tokens * 2 * (a.n_heads + 2 * a.kv_heads) * a.head_dim * (int64_t)sizeof(T) > kReadOnceBytes;
+  if (!half) return once ? launch_tok<T, V16, false, APPEND, true>(rk, a, s) : launch_tok<T, V16, false, APPEND, false>(rk, a, s);
   // pairs half an axis apart move in units that start on both halves' boundaries
-  if (align % V16 == 0) return launch_tok<T, V16, true, APPEND>(rk, a, s);
-  if (align % (V16 / 2) == 0) return launch_tok<T, V16 / 2, true, APPEND>(rk, a, s);
-  return launch_tok<T, 1, true, APPEND>(rk, a, s);
+  if (align % V16 == 0) return once ? launch_tok<T, V16, true, APPEND, true>(rk, a, s) : launch_tok<T, V16, true, APPEND, false>(rk, a, s);
+  if (align % (V16 / 2) == 0) return launch_tok<T, V16 / 2, true, APPEND, false>(rk, a, s);
+  return launch_tok<T, 1, true, APPEND, false>(rk, a, s);
 }
 
 }  // namespace

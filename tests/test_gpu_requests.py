@@ -544,3 +544,96 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+# ---- offsets that do not fit 32 bits -----------------------------------------------------------------------------------------
+def spread(x, stride):
+    """x's rows `stride` elements apart; what lies between them is not initialised."""
+    out = torch.empty(x.shape[0], stride, dtype=x.dtype, device="cuda")[:, :x.shape[1]]
+    assert (x.shape[0] - 1) * stride > 2 ** 31
+    return out.copy_(x)
+
+
+def test_rows_far_apart():
+    """Rows whose offsets pass 2^31 elements: what packed rows give, bit for bit."""
+    n, heads, kv_heads, dh = 515, 4, 2, 64
+    far = 2 ** 22
+    q = dev(n, heads * dh, seed=1)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")[:, None]
+    rope = make_rope((dh,), theta=1e4, layout="half")
+    out = spread(torch.zeros_like(q), far)
+    assert torch.equal(pf_op_rope(spread(q, far), rope, pos, dh, out=out), pf_op_rope(q, rope, pos, dh))
+
+    keys = 2100                                # as far apart as keys may be
+    k, v = dev(keys, kv_heads * dh, seed=2), dev(keys, kv_heads * dh, seed=3)
+    lens_q, lens_k = cu([500, 15]), cu([900, 1200])
+    for causal in (False, True):
+        want = pf_op_attention_packed(q, k, v, lens_q, lens_k, dh, causal=causal)
+        out = spread(torch.zeros_like(q), far)
+        got = pf_op_attention_packed(spread(q, far), spread(k, 2 ** 20), spread(v, 2 ** 20), lens_q, lens_k, dh, causal=causal, out=out)
+        assert torch.equal(got, want), causal
+    del out, got
+
+    x, y = dev(n, 256, dtype=F32, seed=4), dev(n, 256, seed=5)
+    norm = make_norm("layer")
+    want = pf_op_norm_residual(y, x, pre=norm)
+    x_out, h_out = spread(torch.zeros_like(x), far), spread(torch.zeros_like(y), far)
+    got = pf_op_norm_residual(spread(y, far), spread(x, far), pre=norm, x_out=x_out, h_out=h_out)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_pages_far_apart():
+    """Pages whose offsets pass 2^31 elements, written and read."""
+    kv_heads, dh, page, n_pages = 2, 64, 16, 6
+    block = kv_heads * page * dh
+
+    def pool(far):
+        flat = torch.empty(n_pages, 2 ** 29 if far else block, dtype=BF16, device="cuda")
+        return flat[:, :block].unflatten(1, (kv_heads, page, dh)).fill_(0)
+
+    table = ints(5, 0, 4, 1, 3, 2).view(2, 3)
+    new, first = [40, 30], [3, 10]
+    q, k, v = dev(70, 4 * dh, seed=1), dev(70, kv_heads * dh, seed=2), dev(70, kv_heads * dh, seed=3)
+    results = []
+    for far in (False, True):
+        pages = KvPages(pool(far), pool(far), table)
+        pf_op_kv_append(pages, k, v, cu(new), ints(*first))
+        rows = pf_op_attention_paged(q, pages, cu(new), ints(*first), ints(43, 40), causal=True)
+        tokens = pf_op_attention_paged(q[:2], pages, cu([1, 1]), ints(42, 39), ints(43, 40))
+        results.append((pages.k.clone(), pages.v.clone(), rows, tokens))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+# ---- calls past the size from which rows are read only once ---------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_large_calls_equal_their_parts(layout, dtype):
+    """More than 256 MiB in one call: bit for bit what calls of a part of the rows give."""
+    heads, kv_heads, dh = 16, 16, 64
+    n = 2 ** 28 // (2 * heads * dh * (2 if dtype == BF16 else 4)) + 37
+    parts = [slice(i, min(i + 5000, n)) for i in range(0, n, 5000)]
+    q, rope = dev(n, heads * dh, dtype=dtype, seed=1), make_rope((dh,), layout=layout)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")[:, None]
+    got = pf_op_rope(q, rope, pos, dh)
+    assert torch.equal(got, torch.cat([pf_op_rope(q[p], rope, pos[p], dh) for p in parts]))
+
+    k, v = q.flip(0), q.roll(1, 0)
+    table = torch.randperm((n + 63) // 64, generator=torch.Generator().manual_seed(3)).int().cuda()[None]
+    caches = [KvPages(*(torch.zeros(table.shape[1], kv_heads, 64, dh, dtype=dtype, device="cuda") for _ in range(2)), table) for _ in range(2)]
+    assert torch.equal(pf_op_kv_append(caches[0], k, v, cu([n]), ints(0), rope=rope, pos=pos, q=q), got)
+    for p in parts:
+        pf_op_kv_append(caches[1], k[p], v[p], cu([p.stop - p.start]), ints(p.start), rope=rope, pos=pos[p])
+    assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v, caches[1].v)
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+def test_large_norm_equals_its_parts(dtype):
+    d = 1152
+    n = 2 ** 28 // (d * (12 if dtype == BF16 else 16)) + 37
+    parts = [slice(i, min(i + 5000, n)) for i in range(0, n, 5000)]
+    x, y = dev(n, d, dtype=F32, seed=1), dev(n, d, dtype=dtype, seed=2)
+    w, shift = dev(d, dtype=dtype, seed=3), dev(d, dtype=F32, seed=4)
+    run = lambda p: pf_op_norm_residual(y[p], x[p], post=make_norm("rms", w), pre=make_norm("layer"), shift=shift)
+    got = run(slice(0, n))
+    want = [run(p) for p in parts]
+    assert all(torch.equal(g, torch.cat([w[i] for w in want])) for i, g in enumerate(got))
