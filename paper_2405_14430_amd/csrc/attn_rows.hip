@@ -11,7 +11,14 @@
 //   key kernel  (KW = 4): four waves hold the same 32 rows and each walks a quarter of the keys in tiles of its own, without
 //                         a barrier; they are joined through LDS at the end.  For few rows per sequence, where the keys
 //                         are the work.
+//   wide kernel (bf16):   four waves of 64 rows, below.
 // The keys of a launch with few workgroups are cut into chunks, whose partial results a second launch joins.
+//
+// What bounds them, and what they measured.  Wide: the matrix cores and the power they take: six causal prompts (28223 rows
+// of 32 heads of 128 over 8 key heads) 2.35 ms, 1.20 PFLOP/s (a library product of 8192 cubed: 1.42); at head sizes up to 80 the vector
+// unit as much, one exponential per score: 22256 rows of 16 heads of 72 in six images 0.68 ms, 0.86 PFLOP/s.  Keys: memory: 64 tokens of 32
+// heads of 128 over caches of up to 16384 keys of 8 heads 174 us, 783 MB at 4.5 TB/s; one token over 131072 keys of two heads 30 us, 5 of
+// them the join's.  Tiles: the LDS (every MFMA takes a fragment from it) and, in fp32, the matrix cores.
 //
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
 // bounds of the buffer loads give zeros for rows past the last key, for pages that are none and for channels past the head, so

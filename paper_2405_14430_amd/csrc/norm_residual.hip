@@ -4,7 +4,9 @@
 // with RMS or Layer norms over a row and gate / scale / shift vectors per sequence.
 //
 // Bound by memory: y and x are read once, x' and h written once, a row lives in registers between its (up to four) sums.
-// A row belongs to one wave, or to 2, 4 or 8 that add their sums up through LDS: few rows need the waves, many rows do not.
+// 16384 fp32 rows of 1152 with both norms, gate and modulation, from memory: 58 us, 302 MB at 5.2 TB/s, a large device copy's rate
+// or better; 32 rows of 1536: 4.5 us between two calls of a graph, launch, one wait for memory and three sums behind each other.
+// A row belongs to one wave, or to 2, 4 or 8 that add their sums up through LDS (the rule and what it measured: at the launch).
 // The variance is the mean of (x - mean)^2 over the registers, a second sum and no difference of squares.  Sums in 32 bits.
 #include <type_traits>
 
@@ -69,8 +71,9 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
   constexpr int STEP = W * 64 * 4;
   const float inv_d = 1.0f / (float)d;
 
-  // The vectors of the two norms, the gate and the modulation do not depend on the row's sums: with few groups per lane they are
-  // loaded in front of the first one, so that a launch of few rows waits for memory once and not once per sum.
+  // The vectors of the two norms, the gate and the modulation do not depend on the row's sums: with up to two groups per lane they
+  // are loaded in front of the first one, so that a launch of few rows waits for memory once and not once per sum (32
+  // rows of 4096, bf16: 5.1 -> 4.8 us).  With three or four groups their registers leave too few waves (16384 rows of 1152: 44 -> 56).
   constexpr bool EARLY = NV <= 2;
   struct Vectors {
     float wy[NV][4], by[NV][4], g[NV][4], wx[NV][4], bx[NV][4], sc[NV][4], sh[NV][4];
@@ -220,8 +223,7 @@ hipError_t launch_w(const NormResidual &a, hipStream_t s) {
   if (nv <= 1) return launch_nw<T, 1, W>(a, s);
   if (nv <= 2) return launch_nw<T, 2, W>(a, s);
   if (nv <= 3) return launch_nw<T, 3, W>(a, s);
-  if (nv <= 5) return launch_nw<T, 5, W>(a, s);
-  return launch_nw<T, 8, W>(a, s);
+  return launch_nw<T, 4, W>(a, s);
 }
 
 }  // namespace
@@ -231,10 +233,13 @@ hipError_t launch_norm_residual(const NormResidual &args, hipStream_t s) {
   NormResidual a = args;
   const int64_t el = (int64_t)dt_size(a.dt);
   a.once = (int64_t)a.rows * a.d * (4 + (a.y ? el : 0) + (a.x_out ? 4 : 0) + (a.h ? el : 0)) > kReadOnceBytes;
-  // Waves per row: enough that a lane holds at most eight groups of four channels, and twice or four times as many while
-  // the launch has fewer than 4096 waves and a wave still has two groups per lane.
+  // Waves per row: so many that a lane holds at most four groups of four channels of each row it works on (16384 rows, bf16, in
+  // us: up to eight groups, up to four, up to two: 1536 channels 84, 60, 75; 4096: 227, 172, 202; 8192: 444, 337, 337; fp32: 1536: 74,
+  // 68, 72), and twice or four times as many while the launch has fewer than 4096 waves and a wave still has two groups per
+  // lane (32 rows of 1536, bf16: 4.5 us with four waves, 9.0 with one; 1024 rows of 4096: 13.2, up to 2048 waves 16.4, up to 8192
+  // 14.3; 4000 rows of 1152: 13.4 with two, 18.8 with four).
   int w = 1;
-  while (a.d > w * 2048) w *= 2;
+  while (a.d > w * 1024) w *= 2;
   while (w < 8 && (int64_t)a.rows * w < 4096 && a.d > w * 512) w *= 2;
   if (a.dt == DT_BF16)
     return w == 1 ? launch_w<bf16_t, 1>(a, s) : w == 2 ? launch_w<bf16_t, 2>(a, s) : w == 4 ? launch_w<bf16_t, 4>(a, s) : launch_w<bf16_t, 8>(a, s);
