@@ -17,12 +17,13 @@
 // What bounds them, and what they measured.  Wide: the matrix cores and the power they take: six causal prompts (28223 rows
 // of 32 heads of 128 over 8 key heads) 2.35 ms, 1.20 PFLOP/s (a library product of 8192 cubed: 1.42); at head sizes up to 80 the vector
 // unit as much, one exponential per score: 22256 rows of 16 heads of 72 in six images 0.68 ms, 0.86 PFLOP/s.  Keys: memory: 64 tokens of 32
-// heads of 128 over caches of up to 16384 keys of 8 heads 174 us, 783 MB at 4.5 TB/s; one token over 131072 keys of two heads 30 us, 5 of
+// heads of 128 over caches of up to 16384 keys of 8 heads 155 us, 783 MB at 5.0 TB/s; one token over 131072 keys of two heads 30 us, 5 of
 // them the join's.  Tiles: the LDS (every MFMA takes a fragment from it) and, in fp32, the matrix cores.
 //
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
 // bounds of the buffer loads give zeros for rows past the last key, for pages that are none and for channels past the head, so
 // neither the scores nor 0 * v meets what lies there.  LDS rows are padded against bank conflicts.
+#include <algorithm>
 #include <type_traits>
 
 #include "requests.h"
@@ -110,10 +111,10 @@ struct Tile {
   static constexpr int WGS = SMEM > 80 * 1024 ? 1 : 2;     // workgroups on a CU, by their LDS
 };
 
-// Key tiles of one chunk when the longest sequence of the launch is cut into `splits` of them: at least four.
-__device__ __forceinline__ int chunk_tiles(int longest_tiles, int splits) {
-  const int c = (longest_tiles + splits - 1) / splits;
-  return c < 4 ? 4 : c;
+// Units of UNIT keys in one chunk when the longest sequence of the launch is cut into `splits` of them: at least 256 keys.
+template <int UNIT> __device__ __forceinline__ int chunk_units(int longest, int splits) {
+  const int c = (longest + splits - 1) / splits;
+  return c < 256 / UNIT ? 256 / UNIT : c;
 }
 // Keys of sequence s, inside what there is.
 template <bool PAGED>
@@ -169,7 +170,7 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
       longest = max(longest, sequence_keys<PAGED>(a, i, unused));
     }
     for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, kWave));
-    const int64_t c = (int64_t)chunk_tiles((longest + UNIT - 1) / UNIT, a.splits) * UNIT;
+    const int64_t c = (int64_t)chunk_units<UNIT>((longest + UNIT - 1) / UNIT, a.splits) * UNIT;
     w.kb = (int)min((int64_t)w.k_end, w.sp * c);
     w.ke = (int)min((int64_t)w.k_end, (w.sp + 1) * c);
   }
@@ -906,7 +907,8 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
 
 // Joins the chunks of a row: out = sum 2^(m_c - m) O_c / sum 2^(m_c - m) l_c, W waves per (token, head).  A thread sums four channels of
 // every GROUPS-th chunk, the groups are added up through LDS in their order.  Chunks that saw no key of the row left l = 0; their O is
-// not read.
+// not read.  Four to five microseconds, launch included, of three memory latencies behind each other, for a token of 16 heads in 128
+// chunks as for 64 of 32 heads in 8.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
   constexpr int R = 4 / W, NT = 64 * W;                       // rows per workgroup, threads per row
@@ -984,7 +986,8 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
 template <typename T>
 hipError_t launch_join(const RowsAttn &a, hipStream_t s) {
   const int64_t all = (int64_t)a.total_q * a.n_heads;
-  // four waves per row where a wave would have more than eight chunks to add up per thread
+  // four waves per row where a wave would have more than eight chunks to add up per thread (128 chunks of a token of 16 heads: the call
+  // takes 30.9 us, with one wave 34.4; 16 chunks of 64 tokens of 32 heads: 176, with four waves 180)
   if (a.splits > 16) attn_rows_join_kernel<T, 4><<<dim3((unsigned)all), 256, 0, s>>>(a);
   else attn_rows_join_kernel<T, 1><<<dim3((unsigned)((all + 3) / 4)), 256, 0, s>>>(a);
   return hipGetLastError();
@@ -1084,11 +1087,16 @@ RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int k
   // rows x 16 heads of 128 over as many keys: 88 us, in tiles 121).
   const double keys_us = 4.0 + (double)wgs(32) * max_kv * head_dim * 2 * dt_size(dt) / 8e6;
   if (rows <= (int64_t)n_seqs * 32 || (dt == DT_BF16 ? keys_us < best : wgs(32) <= 1024)) {
-    // Chunks of at least 1024 keys, so many of them that caches of different lengths share the 512 workgroups the chip holds evenly
-    // (64 tokens over caches of up to 16k keys: 225 us with chunks enough for 1024 workgroups, 196 for 4096, 191 for 8192).
-    int64_t n = (8192 + wgs(32) - 1) / wgs(32);
-    const int64_t cap = max_kv / 1024 > 1 ? max_kv / 1024 : 1;
-    n = n < cap ? n : cap;
+    // Chunks down to 256 keys until every CU has a workgroup (one token of 8 key heads over 4096 keys: 16 chunks 13.5 us, 4 chunks
+    // 21.3; of 2 key heads over 131072 keys: 128 chunks 30.6 us, 64 chunks 34.0, 256 chunks 33.0).  Behind that, chunks of at least
+    // 2048 keys, whole rounds of the 512 workgroups that the chip holds, up to 8192: caches of different lengths
+    // share the chip evenly (64 tokens over up to 16384 keys of 8 key heads: 156 us, without chunks 211, with chunks of 1024 keys
+    // 177; where lengths are alike it costs little: 32 tokens over 8192 keys each 176, in two chunks 173).
+    const int64_t w = wgs(32), none = 1;
+    int64_t n = std::min((256 + w - 1) / w, std::max(max_kv / 256, none));
+    int64_t more = std::min((8192 + w - 1) / w, max_kv / 2048);
+    if (w < 512) more -= more % (512 / w);
+    n = std::max(n, more);
     p = RowsPlan{ROWS_KEYS, (int)(n < kMaxChunks ? n : kMaxChunks), 0};
   }
   if (p.splits > 1) p.ws_bytes = (size_t)p.splits * total_q * n_heads * (head_dim + 2) * sizeof(float);

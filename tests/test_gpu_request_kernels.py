@@ -36,9 +36,12 @@ KERNELS = [
     (BF16, 128, 4100, 1, 8, 8, 1000, "attn_rows_wide_kernel<128,8>", False),
     (BF16, 128, 777, 3, 14, 2, 2000, "attn_rows_wide_kernel<128,8>", True),
     (BF16, 64, 5, 3, 8, 2, 3000, "attn_rows_kernel<bf16,64,1,4>", True),
-    (BF16, 72, 60, 1, 6, 3, 900, "attn_rows_kernel<bf16,96,1,4>", False),
+    (BF16, 72, 60, 1, 6, 3, 900, "attn_rows_kernel<bf16,96,1,4>", True),
+    (BF16, 72, 60, 1, 6, 3, 500, "attn_rows_kernel<bf16,96,1,4>", False),
     (BF16, 128, 33, 3, 14, 2, 3000, "attn_rows_kernel<bf16,128,1,4>", True),
-    (F32, 64, 300, 1, 8, 8, 700, "attn_rows_kernel<float,64,1,4>", False),
+    (F32, 64, 300, 1, 8, 8, 700, "attn_rows_kernel<float,64,1,4>", True),
+    (F32, 64, 300, 1, 8, 8, 400, "attn_rows_kernel<float,64,1,4>", False),
+    (BF16, 128, 60, 3, 8, 2, 170, "attn_rows_kernel<bf16,128,1,4>", False),
     (F32, 96, 3, 3, 8, 1, 3000, "attn_rows_kernel<float,96,1,4>", True),
     (F32, 128, 70, 3, 8, 2, 2500, "attn_rows_kernel<float,128,1,4>", True),
 ]

@@ -429,7 +429,7 @@ class Block:
         self.rope_kw = dict(axes=(32, 32), layout="interleaved", theta=1e4)
         self.rope = make_rope((32, 32), layout="interleaved", theta=1e4)
 
-    def run(self, x, cu_rows, first, kv_len, pos, pages, gate, causal):
+    def run(self, x, cu_rows, first, kv_len, pos, pages, gate, causal, x_out=None):
         zero = torch.zeros(self.w_qkv.shape[0], dtype=self.dt, device="cuda")
         _, h = pf_op_norm_residual(None, x, pre=make_norm("rms", self.pre), dtype=self.dt)
         qkv = pf_op_gemm(h, self.w_qkv, zero)
@@ -437,7 +437,8 @@ class Block:
         q = pf_op_kv_append(pages, k, v, cu_rows, first, rope=self.rope, pos=pos, q=q)
         o = pf_op_attention_paged(q, pages, cu_rows, first, kv_len, causal=causal)
         y = pf_op_gemm(o, self.w_o, zero[:self.d])
-        x2, _ = pf_op_norm_residual(y, x, post=make_norm("rms", self.post), gate=gate, gate_tanh=True, cu=cu_rows, want_h=False)
+        x2, _ = pf_op_norm_residual(y, x, post=make_norm("rms", self.post), gate=gate, gate_tanh=True, cu=cu_rows, want_h=False,
+                                    x_out=x_out)
         return x2
 
     def plain(self, x, new, first, kv_len, pos, cache, gate, causal):
@@ -504,9 +505,11 @@ def test_a_captured_block_replays_with_other_lengths():
     for c in caches:
         c.k.zero_()
         c.v.zero_()
+    # (not from the graph's own memory, where another of its tensors may have lain before: rows of no sequence stay as they were)
+    out = torch.empty(3, blk.d, device="cuda")
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
-        out = blk.run(x, pages=caches[0], gate=gate, causal=True, **st)
+        blk.run(x, pages=caches[0], gate=gate, causal=True, x_out=out, **st)
     for i in range(steps):
         x.copy_(dev(3, blk.d, dtype=F32, seed=30 + i))
         lens = [(2, 1), (1, 2), (0, 3), (3, 0), (1, 1)][i]
