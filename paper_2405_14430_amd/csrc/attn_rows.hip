@@ -111,11 +111,6 @@ struct Tile {
   static constexpr int WGS = SMEM > 80 * 1024 ? 1 : 2;     // workgroups on a CU, by their LDS
 };
 
-// Units of UNIT keys in one chunk when the longest sequence of the launch is cut into `splits` of them: at least 256 keys.
-template <int UNIT> __device__ __forceinline__ int chunk_units(int longest, int splits) {
-  const int c = (longest + splits - 1) / splits;
-  return c < 256 / UNIT ? 256 / UNIT : c;
-}
 // Keys of sequence s, inside what there is.
 template <bool PAGED>
 __device__ __forceinline__ int sequence_keys(const RowsAttn &a, int s, int &k0) {
@@ -131,7 +126,8 @@ __device__ __forceinline__ int sequence_keys(const RowsAttn &a, int s, int &k0) 
 
 // The rows and keys of a workgroup.  Workgroup id -> (key head, row tile, chunk): neighbouring ids are different key heads - ids go
 // round the 8 XCDs, so with 8 or more key heads a head's workgroups meet in one L2 - and later row tiles, which see more
-// keys, come first.  Row tiles of sequence s are slots floor(cu[s] G / ROWS) + s and on: enough of them for any start.
+// keys, come first, all of one chunk before those of the next, whose last ones have no keys where sequences are shorter than the longest or
+// than the launch could take.  Row tiles of sequence s are slots floor(cu[s] G / ROWS) + s and on: enough of them for any start.
 struct Work {
   int hk, sp, s;
   int q0, n;              // the sequence's first row and its number of rows
@@ -147,8 +143,8 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
   const int G = p.group;
   const int rest = blockIdx.x / a.kv_heads;
   w.hk = blockIdx.x % a.kv_heads;
-  w.sp = rest % a.splits;
-  const int slot = p.slots - 1 - rest / a.splits;
+  w.sp = rest / p.slots;
+  const int slot = p.slots - 1 - rest % p.slots;
   w.s = wave_search(a.n_seqs - 1, lane, slot, [&](int i) { return clampi(a.cu_q[i], 0, a.total_q) * G / ROWS + i; });
   if (w.s < 0) return false;
   int q1;
@@ -164,13 +160,18 @@ __device__ __forceinline__ bool find_work(const RowsKernelArgs &p, int lane, Wor
   w.kb = 0;
   w.ke = w.k_end;
   if (a.splits > 1) {
-    int longest = 0;
-    for (int i = lane; i < a.n_seqs; i += 64) {
-      int unused;
-      longest = max(longest, sequence_keys<PAGED>(a, i, unused));
+    // equal parts, in UNITs, of the longest sequence of the launch, at least the plan's
+    int64_t c = a.least_keys;
+    if (w.sp * c < w.k_end) {
+      int longest = 0;
+      for (int i = lane; i < a.n_seqs; i += 64) {
+        int unused;
+        longest = max(longest, sequence_keys<PAGED>(a, i, unused));
+      }
+      for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, kWave));
+      const int units = (longest + UNIT - 1) / UNIT;
+      c = max(c, (int64_t)((units + a.splits - 1) / a.splits) * UNIT);
     }
-    for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, kWave));
-    const int64_t c = (int64_t)chunk_units<UNIT>((longest + UNIT - 1) / UNIT, a.splits) * UNIT;
     w.kb = (int)min((int64_t)w.k_end, w.sp * c);
     w.ke = (int)min((int64_t)w.k_end, (w.sp + 1) * c);
   }
@@ -341,6 +342,17 @@ __device__ __forceinline__ void put_stats(const RowsAttn &a, int sp, int64_t row
   }
 }
 
+// A chunk without keys leaves its rows' statistics only; its partial results are not read.
+template <int ROWS>
+__device__ __forceinline__ bool empty_chunk(const RowsKernelArgs &p, const Work &w) {
+  if (p.a.splits == 1 || w.kb < w.ke) return false;
+  if (threadIdx.x < ROWS) {
+    const LaneRow row(w, p.group, threadIdx.x);
+    if (row.ok) put_stats(p.a, w.sp, w.q0 + row.tok, row.head, -INFINITY, 0.f);
+  }
+  return true;
+}
+
 // What the keys noted in `hidden` (n words, from key0 on; keys at ke and behind are none) bring to the rows that do see them: their
 // infinities and NaN, whatever the weight, added to the rows that the workgroup has stored.  Nearly always there are none.
 template <typename T, bool PAGED, int ROWS, int THREADS>
@@ -386,6 +398,7 @@ __global__ __launch_bounds__(64 * NW * KW, (Tile<T, DHP, NW, KW>::WGS)) void att
   const int dh = a.head_dim, G = p.group;
   Work w;
   if (!find_work<PAGED, CAUSAL, C::ROWS, 64 * KW>(p, lane, w)) return;   // chunks: whole tiles for all waves
+  if (empty_chunk<C::ROWS>(p, w)) return;
   int kb = w.kb, ke = w.ke;
   if constexpr (KW > 1) {            // the wave's quarter
     const int q = ((ke - kb + KW - 1) / KW + TK - 1) / TK * TK;
@@ -664,6 +677,7 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
   const int dh = a.head_dim, G = p.group;
   Work w;
   if (!find_work<PAGED, CAUSAL, 256, 64>(p, lane, w)) return;
+  if (empty_chunk<256>(p, w)) return;
   const int kb = __builtin_amdgcn_readfirstlane(w.kb), ke = __builtin_amdgcn_readfirstlane(w.ke);
   const int tiles = (ke - kb + TK - 1) / TK;
 
@@ -993,28 +1007,39 @@ hipError_t launch_join(const RowsAttn &a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Workgroups of `per` rows that have rows, without chunks.
+int64_t workgroups(int64_t total_q, int group, int n_seqs, int kv_heads, int per) {
+  return std::max((total_q * group + per - 1) / per, (int64_t)n_seqs) * kv_heads;
+}
+// Two workgroups of head size 64, or of the key kernel, fit a CU, and the dispatcher puts them there while other CUs are idle: where
+// there are no more than CUs, each asks for more than half a CU's LDS (4 x 512 rows x 24 heads over 4250 keys 132 -> 95 us; 8 tokens of
+// 8 key heads over 4096 keys in four chunks 37.6 -> 30.4).
+constexpr int kAloneBytes = 82 * 1024;
+bool few_workgroups(const RowsAttn &a, int per) {
+  return workgroups(a.total_q, a.n_heads / a.kv_heads, a.n_seqs, a.kv_heads, per) * a.splits <= 256;
+}
+
 template <typename T, int DHP, bool PAGED, bool CAUSAL, int NW, int KW>
 hipError_t launch_shape(const RowsAttn &a, hipStream_t s) {
   using C = Tile<T, DHP, NW, KW>;
-  if (hipError_t e = allow_dynamic_lds<&attn_rows_kernel<T, DHP, PAGED, CAUSAL, NW, KW>, C::SMEM>(); e != hipSuccess) return e;
+  constexpr int alone = KW > 1 && C::SMEM < kAloneBytes ? kAloneBytes : C::SMEM;
+  if (hipError_t e = allow_dynamic_lds<&attn_rows_kernel<T, DHP, PAGED, CAUSAL, NW, KW>, alone>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   p.slots = (int)((int64_t)a.total_q * p.group / C::ROWS) + a.n_seqs;
   const int64_t grid = (int64_t)p.slots * a.splits * a.kv_heads;
-  attn_rows_kernel<T, DHP, PAGED, CAUSAL, NW, KW><<<dim3((unsigned)grid), 64 * C::WAVES, C::SMEM, s>>>(p);
+  attn_rows_kernel<T, DHP, PAGED, CAUSAL, NW, KW><<<dim3((unsigned)grid), 64 * C::WAVES, few_workgroups(a, C::ROWS) ? alone : C::SMEM, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_join<T>(a, s);
 }
 
 template <int DHP, int KS, bool PAGED, bool CAUSAL>
 hipError_t launch_wide(const RowsAttn &a, hipStream_t s) {
-  constexpr int smem = Tile<bf16_t, DHP, 4, 1>::SMEM, alone = smem > 82 * 1024 ? smem : 82 * 1024;
+  constexpr int smem = Tile<bf16_t, DHP, 4, 1>::SMEM, alone = smem > kAloneBytes ? smem : kAloneBytes;
   if (hipError_t e = allow_dynamic_lds<&attn_rows_wide_kernel<DHP, KS, PAGED, CAUSAL>, alone>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   p.slots = (int)((int64_t)a.total_q * p.group / 256) + a.n_seqs;
-  // Two workgroups of head size 64 fit a CU, and the dispatcher puts them there while other CUs are idle: where there are no more
-  // than CUs, each asks for more than half a CU's LDS (4 x 512 rows x 24 heads over 4250 keys: 132 -> 95 us).
-  const bool few = (int64_t)a.total_q * p.group / 256 * a.kv_heads * a.splits <= 256;
-  attn_rows_wide_kernel<DHP, KS, PAGED, CAUSAL><<<dim3((unsigned)((int64_t)p.slots * a.splits * a.kv_heads)), 256, few ? alone : smem, s>>>(p);
+  const int64_t grid = (int64_t)p.slots * a.splits * a.kv_heads;
+  attn_rows_wide_kernel<DHP, KS, PAGED, CAUSAL><<<dim3((unsigned)grid), 256, few_workgroups(a, 256) ? alone : smem, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess || a.splits == 1 ? e : launch_join<bf16_t>(a, s);
 }
@@ -1052,20 +1077,19 @@ hipError_t launch_type(const RowsAttn &a, hipStream_t s) {
 // sequences make all the estimates too long alike.
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
   const int64_t rows = (int64_t)total_q * (n_heads / kv_heads), tiles = (max_kv + 63) / 64;
-  // workgroups with work, without chunks
-  const auto wgs = [&](int per) { return ((rows + per - 1) / per > n_seqs ? (rows + per - 1) / per : n_seqs) * kv_heads; };
+  const auto wgs = [&](int per) { return workgroups(total_q, n_heads / kv_heads, n_seqs, kv_heads, per); };
   const auto rounds = [](int64_t n, int fit) { return n <= 2 * fit ? (double)((n + fit - 1) / fit) : (double)n / fit + 0.5; };
   // the second launch, and the partial results on their way through memory (4 TB/s)
   const double row_us = (double)total_q * n_heads * head_dim * 4.9e-7;
   const auto join_us = [&](int64_t n) { return n > 1 ? 4.0 + (4 * n + 2) * row_us : 0.0; };
   const int dim = head_dim <= 64 ? 0 : head_dim <= 96 ? 1 : 2;
 
-  RowsPlan p{ROWS_TILES, 1, 0};
+  RowsPlan p{ROWS_TILES, 1, 0, 0};
   double best = 1e300;
   const auto offer = [&](int shape, int64_t n, double us) {
     if (us < best - 1e-9) {
       best = us;
-      p = RowsPlan{shape, (int)n, 0};
+      p = RowsPlan{shape, (int)n, 256, 0};
     }
   };
   // chunks of four tiles or more, and none for launches that fill the chip twice without
@@ -1097,7 +1121,7 @@ RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int k
     int64_t more = std::min((8192 + w - 1) / w, max_kv / 2048);
     if (w < 512) more -= more % (512 / w);
     n = std::max(n, more);
-    p = RowsPlan{ROWS_KEYS, (int)(n < kMaxChunks ? n : kMaxChunks), 0};
+    p = RowsPlan{ROWS_KEYS, (int)(n < kMaxChunks ? n : kMaxChunks), n == more ? 2048 : 256, 0};
   }
   if (p.splits > 1) p.ws_bytes = (size_t)p.splits * total_q * n_heads * (head_dim + 2) * sizeof(float);
   return p;

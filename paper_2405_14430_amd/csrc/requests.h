@@ -97,10 +97,10 @@ struct RowsAttn {
   void *out; int64_t ldo;
   float *lse;
   float *ws;
-  int shape, splits;       // of the plan
+  int shape, splits, least_keys;       // of the plan
 };
 enum { ROWS_TILES, ROWS_WIDE, ROWS_KEYS };   // kernels of attn_rows.hip
-struct RowsPlan { int shape; int splits; size_t ws_bytes; };
+struct RowsPlan { int shape, splits, least_keys; size_t ws_bytes; };   // splits: chunks of the keys, none smaller than least_keys
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv);
 hipError_t launch_rows_attention(const RowsAttn &a, hipStream_t s);
 

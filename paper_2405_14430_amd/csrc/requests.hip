@@ -183,6 +183,7 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
     return refuse(PF_ERR_SHAPE, "%s: %d rows of %d heads in %d sequences are too many for one launch", who, a.total_q, a.n_heads, a.n_seqs);
   a.shape = p.shape;
   a.splits = p.splits;
+  a.least_keys = p.least_keys;
   return launched(launch_rows_attention(a, (hipStream_t)stream), who);
 }
 
