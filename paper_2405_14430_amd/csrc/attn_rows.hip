@@ -17,7 +17,7 @@
 // What bounds them, and what they measured.  Wide: the matrix cores and the power they take: six causal prompts (28223 rows
 // of 32 heads of 128 over 8 key heads) 2.35 ms, 1.20 PFLOP/s (a library product of 8192 cubed: 1.42); at head sizes up to 80 the vector
 // unit as much, one exponential per score: 22256 rows of 16 heads of 72 in six images 0.68 ms, 0.86 PFLOP/s.  Keys: memory: 64 tokens of 32
-// heads of 128 over caches of up to 16384 keys of 8 heads 155 us, 783 MB at 5.0 TB/s; one token over 131072 keys of two heads 30 us, 5 of
+// heads of 128 over caches of up to 16384 keys of 8 heads 150 us, 783 MB at 5.2 TB/s; one token over 131072 keys of two heads 30 us, 5 of
 // them the join's.  Tiles: the LDS (every MFMA takes a fragment from it) and, in fp32, the matrix cores.
 //
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
@@ -1111,13 +1111,14 @@ RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int k
   // rows x 16 heads of 128 over as many keys: 88 us, in tiles 121).
   const double keys_us = 4.0 + (double)wgs(32) * max_kv * head_dim * 2 * dt_size(dt) / 8e6;
   if (rows <= (int64_t)n_seqs * 32 || (dt == DT_BF16 ? keys_us < best : wgs(32) <= 1024)) {
-    // Chunks down to 256 keys until every CU has a workgroup (one token of 8 key heads over 4096 keys: 16 chunks 13.5 us, 4 chunks
-    // 21.3; of 2 key heads over 131072 keys: 128 chunks 30.6 us, 64 chunks 34.0, 256 chunks 33.0).  Behind that, chunks of at least
-    // 2048 keys, whole rounds of the 512 workgroups that the chip holds, up to 8192: caches of different lengths
-    // share the chip evenly (64 tokens over up to 16384 keys of 8 key heads: 156 us, without chunks 211, with chunks of 1024 keys
-    // 177; where lengths are alike it costs little: 32 tokens over 8192 keys each 176, in two chunks 173).
+    // Chunks down to 256 keys while there is no more than a workgroup for every CU (one token of 8 key heads over 4096 keys: 16 chunks
+    // 13.5 us, 4 chunks 21.3; of 2 key heads over 131072 keys: 128 chunks 30.6 us, 64 chunks 34.0, 256 chunks 33.0; 20 tokens of 8
+    // over 4096: whole 54, in two chunks 66).  Behind that, chunks of at least 2048 keys, whole rounds of the 512
+    // workgroups that the chip holds, up to 8192: caches of different lengths share the chip evenly (64 tokens over up to 16384 keys of
+    // 8 key heads: 150 us, without chunks 211, with chunks of 1024 keys 177; where lengths are alike it costs little: 32 tokens
+    // over 8192 keys each 176, in two chunks 173).
     const int64_t w = wgs(32), none = 1;
-    int64_t n = std::min((256 + w - 1) / w, std::max(max_kv / 256, none));
+    int64_t n = std::min(std::max(256 / w, none), std::max(max_kv / 256, none));
     int64_t more = std::min((8192 + w - 1) / w, max_kv / 2048);
     if (w < 512) more -= more % (512 / w);
     n = std::max(n, more);
