@@ -640,3 +640,32 @@ def test_large_norm_equals_its_parts(dtype):
     got = run(slice(0, n))
     want = [run(p) for p in parts]
     assert all(torch.equal(g, torch.cat([w[i] for w in want])) for i, g in enumerate(got))
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("dh,heads,kv_heads,new,first,kv,causal", [
+    (128, 8, 2, [1, 1, 1, 1], [-1, 0, 299, 4095], [0, 1, 300, 4096], True),        # no key, one, part of a chunk, all of them
+    (64, 4, 4, [1, 2, 0, 1], [5, 2300, 0, 0], [6, 2302, 2302, 1], False),
+    (72, 2, 1, [300, 3], [3700, 0], [4000, 3], True),
+    (64, 3, 3, [700, 1, 900], [0, 0, 3000], [700, 1, 3900], True),                 # rows whose chunks behind the first are empty
+])
+def test_attention_paged_lengths_far_apart(dh, heads, kv_heads, new, first, kv, causal, dtype):
+    """Sequences much shorter than the longest, so that most of their chunks hold no keys."""
+    test_attention_paged(dh, heads, kv_heads, 16, new, first, kv, causal, dtype)
+
+
+def test_short_sequences_in_large_tables():
+    """Room for 32768 keys, few of them there: what small tables give, to the rounding of the join."""
+    q = dev(3, 8 * 64, seed=1)
+    small = make_pages(2, 64, 16, [20, 2, 7], BF16)
+    table = torch.full((3, 2048), -1, dtype=torch.int32, device="cuda")
+    table[:, :20] = small.table
+    large = KvPages(small.k, small.v, table)
+    args = (cu([1, 1, 1]), ints(310, 20, 99), ints(311, 21, 100))
+    a, lse_a = pf_op_attention_paged(q, small, *args, want_lse=True)
+    b, lse_b = pf_op_attention_paged(q, large, *args, want_lse=True)
+    # the weights are rounded to bf16 relative to other maxima (2^-8 of a weight, of both), the result to bf16 (2^-8 of it, of both)
+    v = small.v.float().abs().max().item()
+    assert (a.float() - b.float()).abs().max().item() <= 2 * 2.0 ** -8 * v + 2 * 2.0 ** -8 * a.float().abs().max().item()
+    # sums of 311 weights in any order, exponentials and a logarithm in 32 bits
+    assert (lse_a - lse_b).abs().max().item() <= 400 * R.U
