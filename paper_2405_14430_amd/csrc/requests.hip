@@ -9,6 +9,7 @@ using namespace pf;
 
 namespace {
 
+constexpr int64_t kMaxKeys = (1ll << 31) - 4096;   // of a sequence: the kernels round key numbers up to whole tiles of chunks in 32 bits
 constexpr int kMaxRows = 1 << 24;   // rows of one call of the row-wise operators: a launch has less than 2^32 threads
 
 bool dt_ok(int dt) { return dt == PF_F32 || dt == PF_BF16; }
@@ -152,14 +153,14 @@ pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, in
 }
 
 size_t pf_op_attention_rows_ws_bytes(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
-  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1) return 0;
+  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1 || max_kv > kMaxKeys) return 0;
   return rows_attention_plan(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv).ws_bytes;
 }
 
 const char *pf_attention_rows_kernel_name(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv,
                                           int *chunks) {
   static thread_local char name[64];
-  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1) return "";
+  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1 || max_kv > kMaxKeys) return "";
   const RowsPlan p = rows_attention_plan(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
   if (chunks) *chunks = p.splits;
   const int dim = head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128;
@@ -198,6 +199,7 @@ pf_status pf_op_attention_packed(int dtype, const void *q, int64_t ldq, const vo
   if (!q || !out || !cu_q || !cu_k || (total_k && (!k || !v))) return refuse(PF_ERR_NULL, "%s: NULL", who);
   if (!head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads))
     return refuse(PF_ERR_SHAPE, "%s: %d rows, %d heads over %d of %d", who, total_q, n_heads, kv_heads, head_dim);
+  if (total_k > kMaxKeys) return refuse(PF_ERR_SHAPE, "%s: %d rows of keys are more than %lld", who, total_k, (long long)kMaxKeys);
   const int64_t dk = (int64_t)kv_heads * head_dim;
   if (total_k && (!row_stride_ok(ldk, dk, dtype) || !row_stride_ok(ldv, dk, dtype) || !aligned(k, 16) || !aligned(v, 16) ||
                   ldk > (1 << 20) || ldv > (1 << 20)))   // a tile's rows are addressed by 32-bit offsets
@@ -222,7 +224,7 @@ pf_status pf_op_attention_paged(int dtype, const void *q, int64_t ldq, const pf_
   if (!heads_ok(total_q, n_heads, pages->kv_heads))
     return refuse(PF_ERR_SHAPE, "%s: %d rows, %d heads over %d", who, total_q, n_heads, pages->kv_heads);
   const int64_t max_kv = (int64_t)pages->max_pages * pages->page_size;
-  if (max_kv > (1ll << 31) - 4096) return refuse(PF_ERR_SHAPE, "%s: max_pages * page_size = %lld", who, (long long)max_kv);
+  if (max_kv > kMaxKeys) return refuse(PF_ERR_SHAPE, "%s: max_pages * page_size = %lld", who, (long long)max_kv);
   RowsAttn a{};
   a.dt = dtype; a.q = q; a.ldq = ldq; a.pages = pages_of(*pages); a.cu_q = cu_q; a.first = causal ? first : nullptr; a.kv_len = kv_len;
   a.n_seqs = pages->n_seqs; a.total_q = total_q; a.n_heads = n_heads; a.kv_heads = pages->kv_heads; a.head_dim = pages->head_dim;

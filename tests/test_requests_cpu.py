@@ -164,6 +164,18 @@ def test_capacity_past_32_bits_is_refused(lib):
     assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), {}) == SHAPE
 
 
+def test_keys_past_what_32_bits_can_round_up_are_refused(lib):
+    most = 2 ** 31 - 4096
+    for n, status in ((most, WORKSPACE), (most + 1, SHAPE), (2 ** 31 - 1, SHAPE)):
+        assert call(lib, "pf_op_attention_packed", PACKED, dict(total_k=n)) == status, n
+    for max_pages, status in ((most // 16, WORKSPACE), (most // 16 + 1, SHAPE)):
+        pg = pages(max_pages=max_pages)
+        assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), {}) == status, max_pages
+    assert lib.pf_op_attention_rows_ws_bytes(1, 50, 3, 4, 2, 64, most) > 0 and lib.pf_attention_rows_kernel_name(1, 50, 3, 4, 2, 64, most, None)
+    assert lib.pf_op_attention_rows_ws_bytes(1, 50, 3, 4, 2, 64, most + 1) == 0
+    assert lib.pf_attention_rows_kernel_name(1, 50, 3, 4, 2, 64, most + 1, None) == b""
+
+
 def test_workspace_bytes(lib):
     f = lib.pf_op_attention_rows_ws_bytes
     for bad in ((2, 1, 1, 4, 2, 64, 10), (1, 0, 1, 4, 2, 64, 10), (1, 1, 0, 4, 2, 64, 10), (1, 1, 1, 5, 2, 64, 10),
