@@ -405,7 +405,7 @@ int pf_gemm_read_ahead(int M, int N, int K);
  * bounded before it is used, so wrong ones give wrong rows and no access outside the arrays.
  * The conventions above hold here too: nothing is allocated, nothing synchronises, errors of arguments are found before
  * anything is launched.  Calls with no rows or no sequences do nothing and may pass NULL pointers; a call
- * takes at most 2^24 rows (attention: as many workgroups of 32 rows, and 2^31 - 4096 keys).  Outputs may not overlap inputs
+ * takes at most 2^24 rows and 2^30 sequences (attention: 2^24 workgroups of 32 rows, and 2^31 - 4096 keys).  Outputs may not overlap inputs
  * except where it is said.  pf_last_error(NULL) says what was wrong.
  * ---------------------------------------------------------------------------------------------- */
 

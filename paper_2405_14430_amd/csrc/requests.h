@@ -12,7 +12,7 @@ pf_status note_error(pf_status st, const char *text);   // what pf_last_error(NU
 
 // The largest s in [0, n] with key(s) <= x for a non-decreasing key, found by the 64 lanes of a wave together: each round
 // probes 64 evenly spaced places at once, so 64 entries take one memory latency and 4096 two.  Returns -1 if key(0) > x.
-// Keys that decrease somewhere give some s in [-1, n] all the same.
+// Keys that decrease somewhere give some s in [-1, n] all the same.  n is at most 2^30: places behind it are counted in 32 bits.
 template <typename F>
 __device__ __forceinline__ int wave_search(int n, int lane, int64_t x, F &&key) {
   int lo = -1, hi = n + 1;                  // key(lo) <= x < key(hi)

@@ -11,6 +11,7 @@ namespace {
 
 constexpr int64_t kMaxKeys = (1ll << 31) - 4096;   // of a sequence: the kernels round key numbers up to whole tiles of chunks in 32 bits
 constexpr int kMaxRows = 1 << 24;   // rows of one call of the row-wise operators: a launch has less than 2^32 threads
+constexpr int kMaxSeqs = 1 << 30;   // wave_search probes up to 64 places behind the last one, in 32 bits
 
 bool dt_ok(int dt) { return dt == PF_F32 || dt == PF_BF16; }
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -45,7 +46,7 @@ const char *rope_wrong(const pf_rope &r, int head_dim) {
 
 pf_status pages_check(int dtype, const pf_kv_pages *p, const char *who) {
   if (!p->k || !p->v || !p->table) return refuse(PF_ERR_NULL, "%s: k, v or table of the pages is NULL", who);
-  if (!head_ok(p->head_dim) || p->kv_heads < 1 || p->kv_heads > 65536 || p->n_seqs < 0 || p->max_pages < 1 || p->n_pages < 1)
+  if (!head_ok(p->head_dim) || p->kv_heads < 1 || p->kv_heads > 65536 || p->n_seqs < 0 || p->n_seqs > kMaxSeqs || p->max_pages < 1 || p->n_pages < 1)
     return refuse(PF_ERR_SHAPE, "%s: pages: head_dim %d, kv_heads %d, n_seqs %d, max_pages %d, n_pages %d", who, p->head_dim, p->kv_heads,
                   p->n_seqs, p->max_pages, p->n_pages);
   if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
@@ -242,6 +243,7 @@ pf_status pf_op_norm_residual(int dtype, const void *y, int64_t ldy, const pf_no
   if (rows == 0 || (cu && n_seqs == 0)) return PF_OK;
   if (!x || (!x_out && !h)) return refuse(PF_ERR_NULL, "%s: x, or both outputs", who);
   const size_t al = dtype == PF_BF16 ? 8 : 16;
+  if (cu && n_seqs > kMaxSeqs) return refuse(PF_ERR_SHAPE, "%s: %d sequences are more than %d", who, n_seqs, kMaxSeqs);
   if (rows > kMaxRows) return refuse(PF_ERR_SHAPE, "%s: %d rows are more than %d", who, rows, kMaxRows);
   if (d < 8 || d % 8 || d > 8192) return refuse(PF_ERR_SHAPE, "%s: d = %d", who, d);
   if (ldx < d || ldx % 4 || !aligned(x, 16) || (y && (ldy < d || ldy % 4 || !aligned(y, al))) ||

@@ -164,6 +164,15 @@ def test_capacity_past_32_bits_is_refused(lib):
     assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), {}) == SHAPE
 
 
+@pytest.mark.parametrize("n_seqs", [2 ** 30 + 1, 2 ** 31 - 64, 2 ** 31 - 1])
+def test_more_sequences_than_the_search_counts_are_refused(lib, n_seqs):
+    pg = pages(n_seqs=n_seqs)
+    assert call(lib, "pf_op_kv_append", dict(APPEND, pages=C.byref(pg), rope=rope64()), {}) == SHAPE
+    assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), {}) == SHAPE
+    assert call(lib, "pf_op_attention_packed", PACKED, dict(n_seqs=n_seqs)) == SHAPE
+    assert call(lib, "pf_op_norm_residual", NORM, dict(n_seqs=n_seqs)) == SHAPE
+
+
 def test_keys_past_what_32_bits_can_round_up_are_refused(lib):
     most = 2 ** 31 - 4096
     for n, status in ((most, WORKSPACE), (most + 1, SHAPE), (2 ** 31 - 1, SHAPE)):
