@@ -129,11 +129,10 @@ pf_status pf_op_rope(int dtype, const pf_rope *rope, const int32_t *pos, const v
 pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, int64_t ldk, const void *v, int64_t ldv,
                           const int32_t *cu, const int32_t *first, int tokens, const pf_rope *rope, const int32_t *pos,
                           const void *q, int64_t ldq, void *q_out, int64_t ldqo, int n_heads, void *stream) {
-  if (!pages) return refuse(PF_ERR_NULL, "pf_op_kv_append: pages");
   if (tokens < 0 || n_heads < 0 || n_heads > 65536) return refuse(PF_ERR_SHAPE, "pf_op_kv_append: %d tokens, %d heads", tokens, n_heads);
   if (!dt_ok(dtype)) return refuse(PF_ERR_DTYPE, "pf_op_kv_append: dtype %d", dtype);
-  if (tokens == 0 || pages->n_seqs == 0) return PF_OK;
-  if (!k || !v || !cu || !first || (rope && !pos) || (n_heads && (!q || !q_out))) return refuse(PF_ERR_NULL, "pf_op_kv_append: NULL");
+  if (tokens == 0 || (pages && pages->n_seqs == 0)) return PF_OK;
+  if (!pages || !k || !v || !cu || !first || (rope && !pos) || (n_heads && (!q || !q_out))) return refuse(PF_ERR_NULL, "pf_op_kv_append: NULL");
   if (!n_heads && q) return refuse(PF_ERR_SHAPE, "pf_op_kv_append: q without heads");
   if (pf_status st = pages_check(dtype, pages, "pf_op_kv_append"); st != PF_OK) return st;
   const int64_t d = (int64_t)pages->kv_heads * pages->head_dim, dq = (int64_t)n_heads * pages->head_dim;
@@ -216,11 +215,10 @@ pf_status pf_op_attention_paged(int dtype, const void *q, int64_t ldq, const pf_
                                 const int32_t *first, const int32_t *kv_len, int total_q, int n_heads, float scale, int causal,
                                 void *out, int64_t ldo, float *lse, void *ws, size_t ws_bytes, void *stream) {
   const char *who = "pf_op_attention_paged";
-  if (!pages) return refuse(PF_ERR_NULL, "%s: pages", who);
   if (total_q < 0) return refuse(PF_ERR_SHAPE, "%s: %d rows", who, total_q);
   if (!dt_ok(dtype)) return refuse(PF_ERR_DTYPE, "%s: dtype %d", who, dtype);
-  if (total_q == 0 || pages->n_seqs == 0) return PF_OK;
-  if (!q || !out || !cu_q || !kv_len || (causal && !first)) return refuse(PF_ERR_NULL, "%s: NULL", who);
+  if (total_q == 0 || (pages && pages->n_seqs == 0)) return PF_OK;
+  if (!pages || !q || !out || !cu_q || !kv_len || (causal && !first)) return refuse(PF_ERR_NULL, "%s: NULL", who);
   if (pf_status st = pages_check(dtype, pages, who); st != PF_OK) return st;
   if (!heads_ok(total_q, n_heads, pages->kv_heads))
     return refuse(PF_ERR_SHAPE, "%s: %d rows, %d heads over %d", who, total_q, n_heads, pages->kv_heads);

@@ -164,6 +164,16 @@ def test_capacity_past_32_bits_is_refused(lib):
     assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), {}) == SHAPE
 
 
+def test_calls_without_rows_may_pass_null_for_everything(lib):
+    none = lambda base: {k: None for k in base if base[k] == P or base[k] == 2 * P or base[k] == 3 * P or k in ("pages", "rope", "post", "pre")}
+    for name, base, rows in (("pf_op_rope", ROPE, "tokens"), ("pf_op_kv_append", APPEND, "tokens"), ("pf_op_attention_packed", PACKED, "total_q"),
+                             ("pf_op_attention_paged", PAGED, "total_q"), ("pf_op_norm_residual", NORM, "rows")):
+        change = none(base)
+        assert not any(v == P for v in dict(base, **change).values())
+        assert call(lib, name, base, dict(change, **{rows: 0})) == 0, name
+        assert call(lib, name, base, change) == NULL, name
+
+
 @pytest.mark.parametrize("n_seqs", [2 ** 30 + 1, 2 ** 31 - 64, 2 ** 31 - 1])
 def test_more_sequences_than_the_search_counts_are_refused(lib, n_seqs):
     pg = pages(n_seqs=n_seqs)
