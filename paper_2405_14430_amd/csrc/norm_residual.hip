@@ -8,6 +8,7 @@
 // or better; 32 rows of 1536: 4.5 us between two calls of a graph, launch, one wait for memory and three sums behind each other.
 // A row belongs to one wave, or to 2, 4 or 8 that add their sums up through LDS (the rule and what it measured: at the launch).
 // The variance is the mean of (x - mean)^2 over the registers, a second sum and no difference of squares.  Sums in 32 bits.
+#include <algorithm>
 #include <type_traits>
 
 #include "requests.h"
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int slot = wave / W, wr = wave % W;
   // W > 1: every wave of the workgroup reaches every barrier, so a row past the end is worked on as a copy and not stored
-  const int64_t row_at = (int64_t)blockIdx.x * RPB + slot;
+  const int64_t row_at = a.row0 + (int64_t)blockIdx.x * RPB + slot;
   bool live = row_at < a.rows;
   const int64_t row = live ? row_at : a.rows - 1;
   int seg = 0;
@@ -211,10 +212,16 @@ __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(Nor
 }
 
 template <typename T, int NV, int W>
-hipError_t launch_nw(const NormResidual &a, hipStream_t s) {
+hipError_t launch_nw(NormResidual a, hipStream_t s) {
   constexpr int WAVES = W < 4 ? 4 : W, RPB = WAVES / W;
-  norm_residual_kernel<T, NV, W><<<dim3((a.rows + RPB - 1) / RPB), 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
+  static_assert(kLaunchRows % RPB == 0, "a launch ends with whole workgroups");
+  hipError_t e = hipSuccess;
+  for (a.row0 = 0; a.row0 < a.rows && e == hipSuccess; a.row0 += kLaunchRows) {
+    const int n = std::min(a.rows - a.row0, kLaunchRows);
+    norm_residual_kernel<T, NV, W><<<dim3((n + RPB - 1) / RPB), 64 * WAVES, 0, s>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 template <typename T, int W>

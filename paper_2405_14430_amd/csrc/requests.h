@@ -53,6 +53,9 @@ inline Pages pages_of(const pf_kv_pages &p) {
 // 120 -> 109, 16384 rows of 1152, 226 MB: 48 -> 55; the same rows again and again).
 constexpr int64_t kReadOnceBytes = 256ll << 20;
 
+// Rows of one launch of the row kernels, whose workgroups of up to 512 threads take a row each: a launch has less than 2^32 threads.
+constexpr int kLaunchRows = 1 << 22;
+
 struct RopeRows {
   int dt;
   const pf_rope *rope;   // nullptr: rows are copied (append only)
@@ -79,6 +82,7 @@ struct NormResidual {
   void *h; int64_t ldh;
   const int32_t *cu; int n_seqs;
   int rows, d;
+  int row0;                // first row of the launch (set there)
   bool once;               // x and y are read with non-temporal loads (set at the launch)
 };
 hipError_t launch_norm_residual(const NormResidual &a, hipStream_t s);

@@ -10,7 +10,7 @@ using namespace pf;
 namespace {
 
 constexpr int64_t kMaxKeys = (1ll << 31) - 4096;   // of a sequence: the kernels round key numbers up to whole tiles of chunks in 32 bits
-constexpr int kMaxRows = 1 << 24;   // rows of one call of the row-wise operators: a launch has less than 2^32 threads
+constexpr int kMaxRows = 1 << 24;   // rows of one call of the row-wise operators
 constexpr int kMaxSeqs = 1 << 30;   // wave_search probes up to 64 places behind the last one, in 32 bits
 
 bool dt_ok(int dt) { return dt == PF_F32 || dt == PF_BF16; }

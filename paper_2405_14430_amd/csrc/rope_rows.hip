@@ -10,6 +10,8 @@
 // 16896 rows of 32 heads of 128, bf16, three axes: 46 us, 277 MB at 6.0 TB/s (a large device copy: 4.6; the end of what is written stays in the
 // cache in front of the memory).  Append of 7178 fp32 rows of 3 x 16 heads of 72: 45 us, 198 MB at 4.4 TB/s.  48 or 128 rows: 3 - 4
 // us, of launch and two memory latencies behind each other (position or sequence, then page; rows).
+#include <algorithm>
+
 #include "requests.h"
 
 namespace pf {
@@ -32,6 +34,7 @@ struct RowsK {
   Pages pages;
   const int32_t *cu, *first;
   int n_seqs;
+  int t0;                // first token of the launch
 };
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -57,7 +60,7 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
   __shared__ float2 cs[TOK][kMaxPairs];
   __shared__ int64_t k_at[TOK], v_at[TOK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int t0 = blockIdx.x * TOK;
+  const int t0 = a.t0 + blockIdx.x * TOK;
   const int pairs = rk.rot >> 1, dh = a.head_dim;
 
   for (int e = tid; e < TOK * pairs; e += 256) {
@@ -176,6 +179,18 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeK rk, RowsK a) {
   }
 }
 
+template <typename T, int V, bool HALF, bool APPEND, int TOK, bool ONCE>
+hipError_t launch_parts(const RopeK &rk, RowsK a, int y, hipStream_t s) {
+  static_assert(kLaunchRows % TOK == 0, "a launch ends with whole workgroups");
+  hipError_t e = hipSuccess;
+  for (a.t0 = 0; a.t0 < a.tokens && e == hipSuccess; a.t0 += kLaunchRows) {
+    const int n = std::min(a.tokens - a.t0, kLaunchRows);
+    rope_rows_kernel<T, V, HALF, APPEND, TOK, ONCE><<<dim3((n + TOK - 1) / TOK, y), 256, 0, s>>>(rk, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
 template <typename T, int V, bool HALF, bool APPEND, bool ONCE>
 hipError_t launch_tok(const RopeK &rk, const RowsK &a, hipStream_t s) {
   // Workgroups of several tokens where a token has less than 256 threads' work and there are tokens for 2048 of them or more (4
@@ -184,16 +199,11 @@ hipError_t launch_tok(const RopeK &rk, const RowsK &a, hipStream_t s) {
   // workgroups where there are few tokens.
   const int turned = HALF ? (rk.rot / 2 + a.head_dim - rk.rot) / V : a.head_dim / V;
   const int units = (a.n_heads + a.kv_heads) * turned + a.kv_heads * (a.head_dim / V);
-  if (a.tokens >= 4096 && units <= 128) {
-    rope_rows_kernel<T, V, HALF, APPEND, 4, ONCE><<<dim3((a.tokens + 3) / 4), 256, 0, s>>>(rk, a);
-  } else if (a.tokens >= 4096 && units <= 256) {
-    rope_rows_kernel<T, V, HALF, APPEND, 2, ONCE><<<dim3((a.tokens + 1) / 2), 256, 0, s>>>(rk, a);
-  } else {
-    int y = (units + 255) / 256;
-    while (y > 1 && (int64_t)a.tokens * y > 4096) y = (y + 1) / 2;
-    rope_rows_kernel<T, V, HALF, APPEND, 1, ONCE><<<dim3(a.tokens, y), 256, 0, s>>>(rk, a);
-  }
-  return hipGetLastError();
+  if (a.tokens >= 4096 && units <= 128) return launch_parts<T, V, HALF, APPEND, 4, ONCE>(rk, a, 1, s);
+  if (a.tokens >= 4096 && units <= 256) return launch_parts<T, V, HALF, APPEND, 2, ONCE>(rk, a, 1, s);
+  int y = (units + 255) / 256;
+  while (y > 1 && (int64_t)a.tokens * y > 4096) y = (y + 1) / 2;
+  return launch_parts<T, V, HALF, APPEND, 1, ONCE>(rk, a, y, s);
 }
 
 template <typename T, bool APPEND>
@@ -230,7 +240,7 @@ hipError_t launch_rope_rows(const RopeRows &r, hipStream_t s) {
     half = p.layout == PF_ROPE_HALF;
   }
   RowsK a{r.pos, r.tokens, r.head_dim, r.q, r.ldq, r.q_out, r.ldqo, r.n_heads, r.k, r.ldk, r.v, r.ldv, r.n_seqs ? r.kv_heads : 0,
-          r.pages, r.cu, r.first, r.n_seqs};
+          r.pages, r.cu, r.first, r.n_seqs, 0};
   if (r.dt == DT_BF16)
     return r.n_seqs ? launch_layout<bf16_t, true>(rk, a, half, align, s) : launch_layout<bf16_t, false>(rk, a, half, align, s);
   return r.n_seqs ? launch_layout<float, true>(rk, a, half, align, s) : launch_layout<float, false>(rk, a, half, align, s);

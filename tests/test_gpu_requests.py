@@ -669,3 +669,83 @@ def test_short_sequences_in_large_tables():
     assert (a.float() - b.float()).abs().max().item() <= 2 * 2.0 ** -8 * v + 2 * 2.0 ** -8 * a.float().abs().max().item()
     # sums of 311 weights in any order, exponentials and a logarithm in 32 bits
     assert (lse_a - lse_b).abs().max().item() <= 400 * R.U
+
+
+# ---- the most rows of a call ---------------------------------------------------------------------------------------------------
+def periods(base, n):
+    """n rows that repeat `base`, as a whole and as [periods, rows of base, channels]."""
+    torch.cuda.empty_cache()
+    need = (n + 2 * base.shape[0]) * base.shape[1] * base.element_size()
+    if torch.cuda.mem_get_info()[0] < need + 2 ** 32:
+        pytest.skip(f"{need} bytes of GPU memory are not free")
+    x = torch.empty(n, base.shape[1], dtype=base.dtype, device="cuda")
+    return x, x.view(-1, *base.shape).copy_(base)
+
+
+def test_rope_of_the_most_rows():
+    """2^24 rows in place, one to a workgroup of 256 threads: every row turned, and turned once."""
+    n, dh, heads = 2 ** 24, 128, 3
+    base, rope = dev(2 ** 18, heads * dh, seed=1), make_rope((2,), layout="half", theta=100.0)
+    pos = torch.arange(2 ** 18, dtype=torch.int32, device="cuda") % 1000 + 1
+    want = pf_op_rope(base, rope, pos, dh)
+    x, parts = periods(base, n)
+    pf_op_rope(x, rope, pos.repeat(n // 2 ** 18), dh, out=x)
+    assert not torch.equal(want, base) and all(torch.equal(p, want) for p in parts)
+    del x, parts
+    torch.cuda.empty_cache()
+
+
+def test_norm_of_the_most_rows():
+    """2^24 rows in place, four waves to a row: every row scaled, and scaled once."""
+    n, d = 2 ** 24, 2056
+    base = torch.randn(2 ** 20, d, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    x, parts = periods(base, n)
+    pf_op_norm_residual(None, x, x_scale=2.0, x_out=x, dtype=F32, want_h=False)
+    base *= 2.0
+    assert all(torch.equal(p, base) for p in parts)
+    del x, parts, base
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (40, 2)])
+def test_append_past_the_rows_of_one_launch(heads, kv_heads, dtype):
+    """More than 2^22 rows, with sequences that end where a launch does: bit for bit what calls of one sequence give."""
+    dh, n = 8, 2 ** 22
+    lens = [n - 3, 3, 9, 70]
+    total = sum(lens)
+    qkv = torch.randn(total, (heads + 2 * kv_heads) * dh, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(dtype)
+    q, k, v = qkv.split((heads * dh, kv_heads * dh, kv_heads * dh), dim=1)
+    rope, pos = make_rope((8,), layout="half"), torch.arange(total, dtype=torch.int32, device="cuda")
+    need = [(m + 1023) // 1024 for m in lens]
+    table = torch.full((4, max(need)), -1, dtype=torch.int32, device="cuda")
+    for s, m in enumerate(need):
+        table[s, :m] = torch.arange(sum(need[:s]), sum(need[:s + 1]), device="cuda")
+    new = lambda t: KvPages(*(torch.zeros(sum(need), kv_heads, 1024, dh, dtype=dtype, device="cuda") for _ in range(2)), t)
+    one, many = new(table), new(table)
+    got = pf_op_kv_append(one, k, v, cu(lens), ints(0, 0, 0, 0), rope=rope, pos=pos, q=q)
+    at = 0
+    for s, m in enumerate(lens):
+        for a in range(at, at + m, 2 ** 20):
+            r = slice(a, min(a + 2 ** 20, at + m))
+            part = KvPages(many.k, many.v, table[s:s + 1])
+            assert torch.equal(pf_op_kv_append(part, k[r], v[r], cu([r.stop - r.start]), ints(a - at), rope=rope, pos=pos[r], q=q[r]), got[r])
+        at += m
+    assert torch.equal(one.k, many.k) and torch.equal(one.v, many.v)
+
+
+@pytest.mark.parametrize("dtype", R.DTYPES)
+def test_norm_past_the_rows_of_one_launch(dtype):
+    d, n = 8, 2 ** 22
+    lens = [n - 3, 3, 9, 70]
+    gen = torch.Generator("cuda").manual_seed(1)
+    y, x = (torch.randn(sum(lens), d, device="cuda", generator=gen) for _ in range(2))
+    y, gate = y.to(dtype), dev(4, d, dtype=F32, seed=3)
+    run = lambda r, **kw: pf_op_norm_residual(y[r], x[r], post=make_norm("rms"), pre=make_norm("layer"), **kw)
+    got = run(slice(0, None), gate=gate, cu=cu(lens))
+    at = 0
+    for s, m in enumerate(lens):
+        for a in range(at, at + m, 2 ** 20):
+            r = slice(a, min(a + 2 ** 20, at + m))
+            assert all(torch.equal(p, g[r]) for p, g in zip(run(r, gate=gate[s].contiguous()), got))
+        at += m
