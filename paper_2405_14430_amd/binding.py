@@ -452,6 +452,11 @@ def pf_op_axpby(x, y, a, b, out=None):
 _DT = {torch.float32: PF_F32, torch.bfloat16: PF_BF16}
 
 
+# Sizes pass the C boundary as 32-bit ints, and ctypes drops what does not fit: they are looked at before.
+def _too_large(what, *sizes):
+    raise PfError(-3, f"{what}: sizes {sizes}, one is past 2^31 - 1")
+
+
 def _raise(st):
     raise PfError(st, load_library().pf_last_error(None).decode())
 
@@ -529,6 +534,8 @@ def make_rope(axis_dims, layout="interleaved", theta=1e4, scaling="none", factor
     if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
         raise PfError(-2, f"rope: layout {layout!r}, scaling {scaling!r}")
     dims = [int(w) for w in axis_dims]
+    if any(not -2 ** 31 <= n < 2 ** 31 for n in (*dims, original_len)):
+        raise PfError(-2, f"rope: axis_dims {dims}, original_len {original_len}")
     c = PfRopeConfig(layout=ROPE_LAYOUTS[layout], n_axes=len(dims), theta=theta, scaling=ROPE_SCALINGS[scaling], factor=factor,
                      low=low, high=high, original_len=original_len, magnitude=magnitude)
     c.axis_dim[:min(len(dims), PF_ROPE_MAX_AXES)] = dims[:PF_ROPE_MAX_AXES]
@@ -558,6 +565,8 @@ def pf_op_rope(x, rope, pos, head_dim, out=None):
     if index < 0 or dt is None or not _good_rows(x, x.dtype, index):
         _rows("x", x)
     tokens, width = x.shape
+    if (tokens | width) >> 31:
+        _too_large("x", tokens, width)
     heads = _heads("x", x, head_dim)
     _positions(rope, pos, tokens, index, x.device)
     if out is None:
@@ -593,6 +602,8 @@ class KvPages:
         n, self.kv_heads, self.page_size, self.head_dim = k.shape
         block = self.kv_heads * self.page_size * self.head_dim
         self.n_seqs, self.max_pages = table.shape
+        if (n | self.kv_heads | self.page_size | self.head_dim | self.n_seqs | self.max_pages) >> 31:
+            _too_large("pages", *k.shape, *table.shape)
         self.device, self.index = k.device, k.get_device()
         self.c = PfKvPages(k=k.data_ptr(), v=v.data_ptr(), k_page_stride=k.stride(0) if n > 1 else block,
                            v_page_stride=v.stride(0) if n > 1 else block, table=table.data_ptr(), n_pages=n,
@@ -612,6 +623,8 @@ def pf_op_kv_append(pages, k, v, cu, first, rope=None, pos=None, q=None, q_out=N
         _ints("cu", cu, (pages.n_seqs + 1,), dev)
         _ints("first", first, (pages.n_seqs,), dev)
     tokens, width = k.shape
+    if tokens >> 31:
+        _too_large("k", tokens, width)
     if width != pages.kv_heads * pages.head_dim:
         raise PfError(-3, f"k: rows of {width} channels for {pages.kv_heads} heads of {pages.head_dim}")
     if rope is not None:
@@ -627,6 +640,8 @@ def pf_op_kv_append(pages, k, v, cu, first, rope=None, pos=None, q=None, q_out=N
             _rows("q", q, dt, dev)
         if q.shape[0] != tokens:
             raise PfError(-3, f"q: {q.shape[0]} rows, k has {tokens}")
+        if q.shape[1] >> 31:
+            _too_large("q", *q.shape)
         heads = _heads("q", q, pages.head_dim)
         if q_out is None:
             q_out, ldo = _like(q), heads * pages.head_dim
@@ -672,6 +687,8 @@ def pf_op_attention_packed(q, k, v, cu_q, cu_k, head_dim, causal=False, scale=No
             raise PfError(-3, f"cu_q: shape {tuple(cu_q.shape)}, [n_seqs + 1] is needed")
         _ints("cu_q", cu_q, (n_seqs + 1,), q.device)
         _ints("cu_k", cu_k, (n_seqs + 1,), q.device)
+    if (q.shape[0] | q.shape[1] | k.shape[0] | k.shape[1] | n_seqs) >> 31:
+        _too_large("q, k, sequences", *q.shape, *k.shape, n_seqs)
     heads, kv_heads = _heads("q", q, head_dim), _heads("k", k, head_dim)
     if scale is not None and not scale > 0:
         raise PfError(-3, f"scale: {scale}")
@@ -694,6 +711,8 @@ def pf_op_attention_paged(q, pages, cu_q, first, kv_len, causal=True, scale=None
         _ints("kv_len", kv_len, (pages.n_seqs,), pages.device)
         if first is not None:
             _ints("first", first, (pages.n_seqs,), pages.device)
+    if (q.shape[0] | q.shape[1]) >> 31:
+        _too_large("q", *q.shape)
     heads = _heads("q", q, pages.head_dim)
     if scale is not None and not scale > 0:
         raise PfError(-3, f"scale: {scale}")
@@ -761,6 +780,8 @@ def pf_op_norm_residual(y, x, post=None, pre=None, gate=None, gate_tanh=False, x
         n_seqs = cu.shape[0] - 1
         if not _good_ints(cu, (n_seqs + 1,), index):
             _ints("cu", cu, (n_seqs + 1,), dev)
+    if (rows | d | (n_seqs or 0)) >> 31:
+        _too_large("x, sequences", rows, d, n_seqs)
     gs, g_at = _vectors("gate", gate, d, n_seqs, index, dev)
     ms, sc_at = _vectors("scale", scale, d, n_seqs, index, dev)
     ms2, sh_at = _vectors("shift", shift, d, n_seqs, index, dev)

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import requests_ref as R
-from paper_2405_14430_amd import (KvPages, make_norm, make_rope, pf_op_attention_packed, pf_op_attention_paged, pf_op_gemm,
+from paper_2405_14430_amd import (KvPages, PfError, make_norm, make_rope, pf_op_attention_packed, pf_op_attention_paged, pf_op_gemm,
                                   pf_op_kv_append, pf_op_norm_residual, pf_op_rope)
 
 pytestmark = pytest.mark.gpu
@@ -749,3 +749,38 @@ def test_norm_past_the_rows_of_one_launch(dtype):
             r = slice(a, min(a + 2 ** 20, at + m))
             assert all(torch.equal(p, g[r]) for p, g in zip(run(r, gate=gate[s].contiguous()), got))
         at += m
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Row counts, sequences and pages of 2^32 and a little: an error, and not the little (nothing is launched, nothing initialised)."""
+    much = 2 ** 32 + 5
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 2 * much * 16 + much * 8:
+        pytest.skip("200 GB of GPU memory are not free")
+    refused = lambda: pytest.raises(PfError, match="past")
+    x, n = torch.empty(much, 8, dtype=BF16, device="cuda"), torch.empty(much, dtype=torch.int32, device="cuda")
+    q, few = dev(4, 8), cu([4])
+    pages = make_pages(1, 8, 16, [2], BF16)
+    with refused():
+        pf_op_rope(x, make_rope((8,)), n, 8, out=x)
+    with refused():
+        pf_op_kv_append(pages, x, x, few, ints(0))
+    with refused():
+        pf_op_attention_packed(q, x, x, few, few, 8)
+    with refused():
+        pf_op_attention_packed(x, q, q, few, few, 8, out=x)
+    with refused():
+        pf_op_attention_packed(q, q, q, n, n, 8)
+    with refused():
+        pf_op_attention_paged(x, pages, few, ints(0), ints(4), out=x)
+    with refused():
+        KvPages(pages.k, pages.v, n[:, None])
+    with refused():
+        pf_op_norm_residual(None, dev(4, 8, dtype=F32), cu=n, dtype=F32)
+    del x
+    torch.cuda.empty_cache()
+    x = torch.empty(much, 8, device="cuda")
+    with refused():
+        pf_op_norm_residual(None, x, x_out=x, dtype=F32, want_h=False)
+    del x, n
+    torch.cuda.empty_cache()

@@ -174,6 +174,14 @@ def test_calls_without_rows_may_pass_null_for_everything(lib):
         assert call(lib, name, base, change) == NULL, name
 
 
+@pytest.mark.parametrize("kw", [dict(axis_dims=(2 ** 32 + 64,)), dict(axis_dims=(64 - 2 ** 32,)),
+                                dict(scaling="ramp_turns", factor=2.0, original_len=2 ** 32 + 4096)])
+def test_rope_numbers_past_32_bits_are_refused(lib, kw):
+    with pytest.raises(B.PfError) as e:
+        B.make_rope(**dict(dict(axis_dims=(64,)), **kw))
+    assert e.value.status == CONFIG
+
+
 @pytest.mark.parametrize("n_seqs", [2 ** 30 + 1, 2 ** 31 - 64, 2 ** 31 - 1])
 def test_more_sequences_than_the_search_counts_are_refused(lib, n_seqs):
     pg = pages(n_seqs=n_seqs)
