@@ -922,7 +922,7 @@ __global__ __launch_bounds__(256, (DHP == 64 ? 2 : 1)) void attn_rows_wide_kerne
 
 // Joins the chunks of a row: out = sum 2^(m_c - m) O_c / sum 2^(m_c - m) l_c, W waves per (token, head).  A thread sums four channels of
 // every GROUPS-th chunk, the groups are added up through LDS in their order.  Chunks that saw no key of the row left l = 0; their O is
-// not read.  Four to five microseconds, launch included, of three memory latencies behind each other, for a token of 16 heads in 128
+// not used.  One whose weight is 0 only in 32 bits is: its infinities and NaN reach the row, as they do where the keys are one chunk.  Four to five microseconds, launch included, of three memory latencies behind each other, for a token of 16 heads in 128
 // chunks as for 64 of 32 heads in 8.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
@@ -936,6 +936,7 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
   const bool live = id < all && row >= a.cu_q[0] && row < a.cu_q[a.n_seqs];
   const float2 *ml = reinterpret_cast<const float2 *>(a.ws + (int64_t)a.splits * all * dh) + id;
   constexpr int PER = (kMaxChunks + NT - 1) / NT;
+  constexpr float kNone = -1.f;                               // in place of a weight: no key
   float2 v[PER];
   float m = -INFINITY;
 #pragma unroll
@@ -953,9 +954,9 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
 #pragma unroll
   for (int i = 0; i < PER; ++i)
     if (i * NT + tid < a.splits) {
-      const float w = v[i].y != 0.f ? __builtin_amdgcn_exp2f(v[i].x - m) : 0.f;
+      const float w = v[i].y != 0.f ? __builtin_amdgcn_exp2f(v[i].x - m) : kNone;
       weight[slot][i * NT + tid] = w;
-      l = fmaf(w, v[i].y, l);
+      if (w != kNone) l = fmaf(w, v[i].y, l);
     }
   l = wave_sum(l);
   if (lane == 0) stat[slot][W + wave] = l;
@@ -975,11 +976,11 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsAttn a) {
       for (int j = 0; j < 8; ++j) {
         const int i = min(i0 + j * groups, a.splits - 1);
         x[j] = *reinterpret_cast<const float4 *>(a.ws + ((int64_t)i * all + id) * dh + c);
-        w[j] = i0 + j * groups < a.splits ? weight[slot][i] : 0.f;
+        w[j] = i0 + j * groups < a.splits ? weight[slot][i] : kNone;
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (w[j] != 0.f) acc = make_float4(fmaf(w[j], x[j].x, acc.x), fmaf(w[j], x[j].y, acc.y), fmaf(w[j], x[j].z, acc.z), fmaf(w[j], x[j].w, acc.w));
+        if (w[j] != kNone) acc = make_float4(fmaf(w[j], x[j].x, acc.x), fmaf(w[j], x[j].y, acc.y), fmaf(w[j], x[j].z, acc.z), fmaf(w[j], x[j].w, acc.w));
     }
   }
   *reinterpret_cast<float4 *>(&part[slot][tid * 4]) = acc;

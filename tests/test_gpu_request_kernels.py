@@ -172,3 +172,22 @@ def test_scores_that_are_not_finite_reach_their_rows_only(dtype, dh, rows, heads
     # other rows: the same sums, but the wide kernel may form a shared step's weights anew with another reference, which moves each by its
     # rounding: 2 * 2^-8 of sum p |v| (below 1.2 over hundreds of unit normal keys), and the output by its own, below 2^-8 at |out| < 1
     assert (out.float() - ref.float()).abs().max() <= 2.0 ** -7 * 1.2 + 2.0 ** -8 and (lse - ref_lse).abs().max() <= 1e-5
+
+
+@pytest.mark.parametrize("dtype,rows,keys,chunks", [(BF16, 1, 240, False), (BF16, 1, 4096, True), (BF16, 1, 16384, True), (F32, 5, 4096, True)])
+def test_values_whose_weight_underflows_reach_the_row(dtype, rows, keys, chunks):
+    """An infinity and a NaN among the values of keys far below the row's best one, exp(-400) of its weight: the row is not finite there,
+    in one chunk as in many, and what it would be elsewhere."""
+    dh = 64
+    name, cut = kernel_name(dtype, rows, 1, 1, 1, dh, keys)
+    assert cut == chunks, name
+    q, k, v = rand(rows, dh, dtype=dtype, seed=1), rand(keys, dh, dtype=dtype, seed=2), rand(keys, dh, dtype=dtype, seed=3)
+    q[:, 0] = 16.0
+    k[:, 0] = 0.0
+    k[keys - 100:, 0] = 200.0                      # 16 * 200 / sqrt(64) = 400
+    want, _, b16, b32, _ = R.attention(q, k, v, dh, torch.full((rows,), keys))
+    v[20, 3], v[keys // 3, 5] = math.inf, math.nan
+    out = R.d64(pf_op_attention_packed(q, k, v, starts([rows]), starts([keys]), dh))
+    assert not torch.isfinite(out[:, [3, 5]]).any()
+    out[:, [3, 5]] = want[:, [3, 5]]
+    R.check(out, want, R.stored(b16 if dtype == BF16 else b32, want, dtype), "out")
