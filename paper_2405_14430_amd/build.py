@@ -2,8 +2,11 @@
 from __future__ import annotations
 
 import os
+import re
+import shutil
 import subprocess
 import sys
+import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -27,8 +30,8 @@ FILE_FLAGS = {"attn_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 # completion is tracked by hand, so a register spill between a read and its wait would save a value that has not
 # arrived - wrong results, not just slow ones.  The compiler reports every kernel's scratch size; the build checks it.
 # attn_rows.hip: the compiler has been seen to save a register in front of the instruction that makes all lanes active again behind
-# a divergent branch, so that the other lanes' values - addresses of rows - were lost.  Kernels that save none cannot
-# meet that.
+# a divergent branch, so that the other lanes' values - addresses of rows - were lost.  None of its kernels saves one to memory; those
+# that need more than 256 vector registers move values to accumulation registers and back, and the build looks at where these moves stand.
 NO_SCRATCH = {"attn_mfma2.hip": "attn_mfma2_kernel", "attn_rows.hip": "attn_rows"}
 
 
@@ -49,15 +52,53 @@ def _check_no_scratch(src, log):
         raise RuntimeError(f"{src}: the compiler reported no resource usage for {want}; cannot check for spills")
 
 
+MOVES_CHECKED = ("attn_rows.hip",)
+_WIDENS = re.compile(r"s_(or|xor)_b(32|64) exec|s_mov_b(32|64) exec|s_(or|andn2|orn2)_saveexec")
+
+
+def _check_moves(src, asm):
+    """Refuses a move to or from an accumulation register between the start of a block, or the last change of the active lanes, and an
+    instruction that activates others: the lanes that were off would keep what the register held before."""
+    name, moved, kernels = None, None, 0
+    for line in asm.splitlines():
+        text = line.split(";")[0].strip()
+        if text.endswith(":"):
+            if not text.startswith("."):
+                name = text[:-1]
+            moved = None
+        elif text.startswith(".amdhsa_kernel"):
+            kernels += 1
+        elif "v_accvgpr" in text:
+            moved = text
+        elif "exec" in text:
+            if moved and _WIDENS.match(text):
+                raise RuntimeError(f"{src}: {name}: '{moved}' in front of '{text}', which activates other lanes")
+            if re.match(r"s_\w+ exec|s_\w+_saveexec", text):
+                moved = None
+    if kernels == 0:
+        raise RuntimeError(f"{src}: no kernels in the compiler's listing; cannot check its moves")
+
+
 def _compile(src, objdir=OBJ, extra=()):
     obj = os.path.join(objdir, src.replace(".hip", ".o"))
     check = ["-Rpass-analysis=kernel-resource-usage"] if src in NO_SCRATCH else []
-    cmd = [HIPCC, *FLAGS, *FILE_FLAGS.get(src, []), *extra, *check, "-c", os.path.join(CSRC, src), "-o", obj]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    log = r.stdout + r.stderr
+    with tempfile.TemporaryDirectory() as tmp:
+        target = obj
+        if src in MOVES_CHECKED:      # keep the listing
+            target, check = os.path.join(tmp, os.path.basename(obj)), [*check, "-save-temps=obj"]
+        cmd = [HIPCC, *FLAGS, *FILE_FLAGS.get(src, []), *extra, *check, "-c", os.path.join(CSRC, src), "-o", target]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        log = r.stdout + r.stderr
+        asm = ""
+        if src in MOVES_CHECKED and r.returncode == 0:
+            shutil.move(target, obj)
+            with open(os.path.join(tmp, src.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))) as f:
+                asm = f.read()
     out = "\n".join(l for l in log.splitlines() if "packed-fp32-ops" not in l and "kernel-resource-usage" not in l)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{out}")
+    if src in MOVES_CHECKED:
+        _check_moves(src, asm)
     if "-DPF_TUNING" in extra:   # the tuning build's timeline stamps cost registers: report, do not refuse
         try:
             _check_no_scratch(src, log)

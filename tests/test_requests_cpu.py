@@ -267,3 +267,38 @@ def test_reference_attention_equals_torch():
     for h in range(2):
         want = torch.nn.functional.scaled_dot_product_attention(q[None, None, :, 8 * h:8 * h + 8], k[None, None], v[None, None], attn_mask=mask)[0, 0]
         assert (out[:, 8 * h:8 * h + 8] - want).abs().max() < 1e-14
+
+
+LISTING = """
+_Zkernel:                               ; @_Zkernel
+; %bb.0:
+\tv_accvgpr_write_b32 a0, 0
+\ts_and_saveexec_b64 s[0:1], vcc
+\ts_cbranch_execz .LBB0_2
+; %bb.1:
+\tv_accvgpr_write_b32 a1, v3
+{in_branch}
+.LBB0_2:                                ; %join
+{in_front}
+\ts_or_b64 exec, exec, s[0:1]
+\tv_accvgpr_read_b32 v4, a0
+\ts_cbranch_execz .LBB0_3
+{behind}
+.LBB0_3:
+\ts_endpgm
+\t.amdhsa_kernel _Zkernel
+"""
+
+
+def test_build_refuses_register_moves_in_front_of_activated_lanes():
+    from paper_2405_14430_amd import build as bld
+    listing = lambda **kw: LISTING.format(**dict(dict(in_branch="", in_front="", behind=""), **kw))
+    bld._check_moves("attn_rows.hip", listing())
+    bld._check_moves("attn_rows.hip", listing(in_branch="\tv_accvgpr_write_b32 a2, v5", in_front="\tv_mov_b32_e32 v1, v2"))
+    for bad in (dict(in_front="\tv_accvgpr_write_b32 a2, v5"), dict(in_front="\tv_accvgpr_read_b32 v5, a2 ; saved"),
+                dict(in_branch="\tv_accvgpr_write_b32 a2, v5\n\ts_xor_b64 exec, exec, s[2:3]"),
+                dict(behind="\ts_mov_b64 exec, -1"), dict(behind="\ts_or_saveexec_b64 s[2:3], -1")):
+        with pytest.raises(RuntimeError, match="_Zkernel"):
+            bld._check_moves("attn_rows.hip", listing(**bad))
+    with pytest.raises(RuntimeError):
+        bld._check_moves("attn_rows.hip", "")
