@@ -173,8 +173,9 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
   const int64_t d = (int64_t)a.n_heads * a.head_dim;
   if (!row_stride_ok(a.ldq, d, a.dt) || !row_stride_ok(a.ldo, d, a.dt) || !aligned(a.q, 16) || !aligned(a.out, 16) || (a.lse && !aligned(a.lse, 4)))
     return refuse(PF_ERR_SHAPE, "%s: row strides %lld, %lld for rows of %lld, or alignment", who, (long long)a.ldq, (long long)a.ldo, (long long)d);
-  if (!isfinite(a.scale)) return refuse(PF_ERR_SHAPE, "%s: scale", who);
-  if (!(a.scale > 0.f)) a.scale = 1.0f / sqrtf((float)a.head_dim);
+  if (a.scale <= 0.f) a.scale = 1.0f / sqrtf((float)a.head_dim);
+  // the kernels take it times log2(e)
+  if (!isfinite(a.scale * 1.5f)) return refuse(PF_ERR_SHAPE, "%s: scale %g", who, (double)a.scale);
   const RowsPlan p = rows_attention_plan(a.dt, a.total_q, a.n_seqs, a.n_heads, a.kv_heads, a.head_dim, max_kv);
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes || !aligned(ws, 16)))
     return refuse(PF_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes is needed, %zu given", who, p.ws_bytes, ws ? ws_bytes : (size_t)0);

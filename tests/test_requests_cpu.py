@@ -150,6 +150,15 @@ def test_paged_refuses(lib, change, status):
     assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), change) == status
 
 
+def test_scales_that_overflow_in_base_2_are_refused(lib):
+    pg = pages()
+    for scale in (3e38, 2.4e38, math.nan, math.inf):
+        assert call(lib, "pf_op_attention_packed", PACKED, dict(scale=scale)) == SHAPE
+        assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), dict(scale=scale)) == SHAPE
+    for scale in (2e38, 0.0, -3e38):     # (stop at the workspace)
+        assert call(lib, "pf_op_attention_packed", PACKED, dict(scale=scale, total_k=1 << 20)) == WORKSPACE
+
+
 @pytest.mark.parametrize("change,status", BAD_PAGES)
 def test_bad_pages_are_refused(lib, change, status):
     pg = pages(**change)
