@@ -475,7 +475,7 @@ typedef struct {
  * first[s] + i of sequence s - the end of a prompt, or a patch in the middle of a sequence whose other rows stay a step
  * old.  rope != NULL: k is turned on the way (pos as in pf_op_rope), and so is q [tokens, n_heads * head_dim], which goes to q_out
  * (may be q itself).  rope == NULL: q, if there is one, is copied.  q == NULL: n_heads must be 0.  Slots past max_pages *
- * page_size, and negative ones, are dropped.  Two rows for one slot leave either.
+ * page_size, and negative ones, are dropped.  Two rows for one slot leave parts of either, in an order that may change from call to call.
  */
 pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, int64_t ldk, const void *v, int64_t ldv,
                           const int32_t *cu, const int32_t *first, int tokens, const pf_rope *rope, const int32_t *pos,

@@ -195,3 +195,17 @@ def test_norm_of_wrong_lengths(rows, seqs, d, dtype):
             assert torch.equal(x_out, want[0]) and torch.equal(h, want[1])
         if i in (6, 7):                     # all behind the rows, or in front (starts that decrease give some sequence's rows)
             assert not done.any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_append_of_two_rows_for_one_slot(dtype):
+    """Two sequences over the same page: every element is that of one of the rows, and slots of one row have it."""
+    dh, kv_heads, page = 128, 8, 64
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    k, v = (rand(100, kv_heads * dh, dtype=dtype, seed=s) for s in (1, 2))
+    pages = KvPages(*(torch.full((1, kv_heads, page, dh), CANARY, dtype=dtype, device="cuda") for _ in range(2)), ints(0, 0).view(2, 1))
+    pf_op_kv_append(pages, k, v, ints(0, 60, 100), ints(0, 20))
+    for pool, rows in ((pages.k, k), (pages.v, v)):
+        got = pool[0].transpose(0, 1).reshape(page, kv_heads * dh)
+        assert torch.equal(got[:20], rows[:20]) and (got[60:] == CANARY).all()
+        assert ((got[20:60] == rows[20:60]) | (got[20:60] == rows[60:])).all()
