@@ -15,11 +15,16 @@
 // The keys of a launch with few workgroups are cut into chunks, whose partial results a second launch joins.
 //
 // What bounds them, and what they measured.  Wide: the matrix cores and the power they take: six causal prompts (28223 rows
-// of 32 heads of 128 over 8 key heads) 2.35 ms, 1.20 PFLOP/s (a library product of 8192 cubed: 1.42); at head sizes up to 80 the vector
-// unit as much, one exponential per score: 22256 rows of 16 heads of 72 in six images 0.68 ms, 0.86 PFLOP/s.  Keys: memory: 64 tokens of 32
+// of 32 heads of 128 over 8 key heads) 2.38 - 2.45 ms, 1.15 - 1.19 PFLOP/s (a library product of 8192 cubed: 1.42); at head sizes up to 80 the vector
+// unit more, an exponential, a multiply-add and an add per score: 22256 rows of 16 heads of 72 in six images 0.68 - 0.71 ms, 0.83 - 0.86 PFLOP/s.  Keys: memory: 64 tokens of 32
 // heads of 128 over caches of up to 16384 keys of 8 heads 150 us, 783 MB at 5.2 TB/s; one token over 131072 keys of two heads 30 us, 5 of
 // them the join's.  Tiles: the LDS (every MFMA takes a fragment from it) and, in fp32, the matrix cores: 4096 rows of 16 heads of 64 0.54 ms,
 // 126 TFLOP/s (a library product of 4096 cubed: 138).
+//
+// Scores, their exponentials, the running maximum, the denominators and the outputs' sums are in 32 bits.  For bf16 rows the weights are rounded to
+// bf16 for the second product, because the matrix units take both operands in one type and multiply fp32 at a tenth of the rate; the
+// denominator sums them unrounded, which is what the log-sum-exp needs.  Against 64 bits the output's relative error grows from the 0.0017 of its own
+// rounding to 0.0023 at most (0.0021 for single tokens).
 //
 // Tiles come from memory through registers: while the products of tile t run, the loads of tile t + 1 are in flight.  The
 // bounds of the buffer loads give zeros for rows past the last key, for pages that are none and for channels past the head, so
@@ -103,8 +108,9 @@ struct Tile {
   static constexpr int RW = TK / NW;                       // rows of a tile that one wave brings in
   static constexpr int LOADS = RW * ROWB / 1024;           // its 1 KB loads
   static constexpr int BUFS = NW > 1 ? 2 : 1;
-  // The key kernel reads every key once: non-temporal loads (policy bit 1) leave the caches to what is read again (64 tokens over
-  // caches of up to 16k keys 191 -> 172 us).  Row tiles share their keys through the L2s (the wide kernel 2.33 -> 2.49 ms with it).
+  // Where no sequence has more than 32 rows the key kernel reads every key once: non-temporal loads (policy bit 1) leave the caches to
+  // what is read again (64 tokens over caches of up to 16k keys 191 -> 172 us).  It keeps them where the plan gives it more rows, whose tiles
+  // share keys through the L2s (not measured without).  For the wide kernel's they cost time (2.33 -> 2.49 ms).
   static constexpr int POLICY = KW > 1 ? 2 : 0;
   static constexpr int JOIN_B = KW > 1 ? KW * 32 * (DHP + 4 + 2) * 4 : 0;   // the waves' partial results
   static constexpr int SMEM = KW * BUFS * (KTILE_B + VTILE_B) > JOIN_B ? KW * BUFS * (KTILE_B + VTILE_B) : JOIN_B;

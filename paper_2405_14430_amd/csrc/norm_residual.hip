@@ -49,7 +49,7 @@ __device__ __forceinline__ float row_sum(float v, int wave, int lane, float *par
   return v;
 }
 
-// NV groups of four channels per lane; W waves per row, 8 / W rows (at least one) per workgroup of max(W, 4) waves.
+// NV groups of four channels per lane; W waves per row, as many rows as fit a workgroup of max(W, 4) waves.
 template <typename T, int NV, int W>
 __global__ __launch_bounds__(64 * (W < 4 ? 4 : W)) void norm_residual_kernel(NormResidual a) {
   constexpr int WAVES = W < 4 ? 4 : W, RPB = WAVES / W;
