@@ -200,6 +200,16 @@ def test_more_sequences_than_the_search_counts_are_refused(lib, n_seqs):
     assert call(lib, "pf_op_norm_residual", NORM, dict(n_seqs=n_seqs)) == SHAPE
 
 
+def test_rows_past_the_documented_ones_are_refused(lib):
+    pg, n = pages(), 2 ** 24 + 1
+    assert call(lib, "pf_op_rope", dict(ROPE, rope=rope64()), dict(tokens=n)) == SHAPE
+    assert call(lib, "pf_op_kv_append", dict(APPEND, pages=C.byref(pg), rope=rope64()), dict(tokens=n)) == SHAPE
+    assert call(lib, "pf_op_norm_residual", NORM, dict(rows=n)) == SHAPE
+    # 2^24 workgroups of 32 rows, two key heads with two query heads each
+    assert call(lib, "pf_op_attention_packed", PACKED, dict(total_q=2 ** 27, total_k=1)) == SHAPE
+    assert call(lib, "pf_op_attention_paged", dict(PAGED, pages=C.byref(pg)), dict(total_q=2 ** 27)) == SHAPE
+
+
 def test_keys_past_what_32_bits_can_round_up_are_refused(lib):
     most = 2 ** 31 - 4096
     for n, status in ((most, WORKSPACE), (most + 1, SHAPE), (2 ** 31 - 1, SHAPE)):
