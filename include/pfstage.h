@@ -535,6 +535,80 @@ pf_status pf_op_norm_residual(int dtype, const void *y, int64_t ldy, const pf_no
                               const pf_norm *pre, const float *shift, const float *scale, int64_t mod_stride, void *h,
                               int64_t ldh, const int32_t *cu, int n_seqs, int rows, int d, void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A cache in 8 or 4 bits: norm and rotation of new rows, their way into pages of few bits, attention over these, and the way back.
+ * The conventions of the operators on packed rows hold here too.
+ * ---------------------------------------------------------------------------------------------- */
+
+/*
+ * Norm of every head of q and k, then its rotation, in one pass:
+ *   out = turn(norm(x) w + b)      RMS: x / sqrt(mean x^2 + eps), LAYER: the same of x - mean x, over the head's head_dim channels
+ * q, q_out dtype [tokens, n_heads * head_dim], k, k_out dtype [tokens, kv_heads * head_dim]; either side may be missing (no heads: its
+ * pointers are not used).  q_norm, k_norm: NULL or kind NONE: none; weight and bias dtype [head_dim], either NULL, shared by the heads.
+ * rope, pos as in pf_op_rope; rope NULL: no rotation.  Without rounding in between; the output is rounded once.  q_out may be q and
+ * k_out k.  head_dim, strides and alignment as in pf_op_rope; weight and bias 16-byte aligned.
+ */
+pf_status pf_op_qk_norm_rope(int dtype, const void *q, int64_t ldq, const pf_norm *q_norm, void *q_out, int64_t ldqo, int n_heads,
+                             const void *k, int64_t ldk, const pf_norm *k_norm, void *k_out, int64_t ldko, int kv_heads,
+                             const pf_rope *rope, const int32_t *pos, int tokens, int head_dim, void *stream);
+
+/*
+ * Pages of numbers in 8 or 4 bits.  Every PF_MX_BLOCK neighbouring channels of a head (the last block of a head may have fewer) share
+ * a power of two: value = code * 2^(byte - 127), byte 255: the block is NaN.
+ *   E4M3  8 bits: sign, 4 bits of exponent (bias 7), 3 of mantissa; up to 448, 7f and ff are NaN.
+ *   E2M1  4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; channel 2 i in the low half of byte i.
+ * Page p of k holds [kv_heads][page_size] rows of pf_kv_mx_row_bytes bytes from k + p * k_page_stride on (head_dim codes, zeros
+ * behind them up to whole 16 bytes), page p of k_scale [kv_heads][page_size] times ceil(head_dim / 32) bytes from k_scale + p *
+ * k_scale_stride on; likewise v.  Table, slots and missing pages as in pf_kv_pages.
+ */
+#define PF_MX_BLOCK 32
+typedef enum { PF_MX_E4M3 = 0, PF_MX_E2M1 = 1 } pf_mx_format;
+typedef struct {
+  void *k, *v;                                     /* 16-byte aligned */
+  void *k_scale, *v_scale;
+  int64_t k_page_stride, v_page_stride;            /* bytes; at least kv_heads * page_size * row bytes, multiples of 16 */
+  int64_t k_scale_stride, v_scale_stride;          /* bytes; at least kv_heads * page_size * blocks */
+  const int32_t *table;                            /* device [n_seqs][max_pages] */
+  int32_t format;                                  /* pf_mx_format */
+  int32_t n_pages, page_size;                      /* page_size: a power of two, 16 .. 1024 */
+  int32_t kv_heads, head_dim;                      /* head_dim: a multiple of 8, at most 128 */
+  int32_t n_seqs, max_pages;
+} pf_kv_mx_pages;
+/* Bytes of a row of codes: head_dim (E4M3) or head_dim / 2 (E2M1) rounded up to whole 16; 0 where format or head_dim are refused. */
+int pf_kv_mx_row_bytes(int format, int head_dim);
+
+/*
+ * pf_op_kv_append into such pages, with the norms of pf_op_qk_norm_rope in front of the rotation.  k, normed, turned and rounded to
+ * dtype, and v as it is are written in few bits, block by block: the exponent is the least e with max |x| <= 448 * 2^e (E2M1: 6 *
+ * 2^e), kept inside -117 .. 119 (E2M1: -125 .. 125; every value is then a bf16 number), a code the nearest to x / 2^e, ties to even, at
+ * most the largest.  A block with an infinity or a NaN gets byte 255 and codes 0.  q, normed and turned, goes to q_out (may be q itself);
+ * q NULL: n_heads must be 0.  Rows of no sequence and slots without a page as in pf_op_kv_append.  dtype is that of the rows alone.
+ */
+pf_status pf_op_kv_append_mx(int dtype, const pf_kv_mx_pages *pages, const void *k, int64_t ldk, const pf_norm *k_norm, const void *v,
+                             int64_t ldv, const int32_t *cu, const int32_t *first, int tokens, const pf_rope *rope, const int32_t *pos,
+                             const void *q, int64_t ldq, const pf_norm *q_norm, void *q_out, int64_t ldqo, int n_heads, void *stream);
+
+/*
+ * The way back: row cu[s] + i of k_out and v_out (dtype [tokens, kv_heads * head_dim], either NULL) receives slot first[s] + i of
+ * sequence s, exactly.  Slots without a page, past max_pages * page_size and negative ones read as zeros; rows of no sequence are
+ * left as they are.  Exponent bytes above those that append writes give what they stand for, infinities included.
+ */
+pf_status pf_op_kv_read_mx(int dtype, const pf_kv_mx_pages *pages, const int32_t *cu, const int32_t *first, int tokens, void *k_out,
+                           int64_t ldk, void *v_out, int64_t ldv, void *stream);
+
+/*
+ * pf_op_attention_paged over such pages, for rows of either type; the result is that over pages of dtype that hold the decoded rows.
+ * Slots in [0, kv_len[s]) that nothing was written to may hold anything as long as the causal mask hides them.
+ * ws: pf_op_attention_mx_ws_bytes(.., max_kv = max_pages * page_size) bytes.
+ */
+size_t pf_op_attention_mx_ws_bytes(int dtype, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv);
+pf_status pf_op_attention_mx(int dtype, const void *q, int64_t ldq, const pf_kv_mx_pages *pages, const int32_t *cu_q,
+                             const int32_t *first, const int32_t *kv_len, int total_q, int n_heads, float scale, int causal, void *out,
+                             int64_t ldo, float *lse, void *ws, size_t ws_bytes, void *stream);
+/* Host-only: as pf_attention_rows_kernel_name. */
+const char *pf_attention_mx_kernel_name(int dtype, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim,
+                                        int64_t max_kv, int *chunks);
+
 #ifdef __cplusplus
 }
 #endif

@@ -58,12 +58,15 @@ EXPORTS = ["pf_stage_kv_bytes", "pf_stage_workspace_bytes", "pf_stage_create", "
            "pf_op_ln_modulate", "pf_op_gemm", "pf_op_kv_scatter", "pf_op_attention_ws_bytes", "pf_op_attention", "pf_attention_kernel_name", "pf_probe_mfma_loop",
            "pf_gemm_tile_count", "pf_gemm_tile_map", "pf_gemm_read_ahead", "pf_op_gemm_tile", "pf_static_scratch_bytes", "pf_op_attention_static", "pf_gemm_kernel_name", "pf_gemm_qkv_kernel_name", "pf_op_axpy", "pf_kv_view_image", "pf_op_axpby",
            "pf_rope_init", "pf_op_rope", "pf_op_kv_append", "pf_op_attention_rows_ws_bytes", "pf_op_attention_packed",
-           "pf_op_attention_paged", "pf_op_norm_residual", "pf_attention_rows_kernel_name"]
+           "pf_op_attention_paged", "pf_op_norm_residual", "pf_attention_rows_kernel_name", "pf_op_qk_norm_rope", "pf_kv_mx_row_bytes",
+           "pf_op_kv_append_mx", "pf_op_kv_read_mx", "pf_op_attention_mx_ws_bytes", "pf_op_attention_mx", "pf_attention_mx_kernel_name"]
 
 PF_ROPE_MAX_AXES, PF_ROPE_MAX_PAIRS = 3, 64
 ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "ramp_turns": 3, "ramp_index": 4}
 NORM_KINDS = {"none": 0, "rms": 1, "layer": 2}
+PF_MX_BLOCK = 32
+MX_FORMATS = {"e4m3": 0, "e2m1": 1}
 
 
 class PfRopeConfig(C.Structure):
@@ -81,6 +84,14 @@ class PfKvPages(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_page_stride", C.c_int64), ("v_page_stride", C.c_int64),
                 ("table", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class PfKvMxPages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("k_page_stride", C.c_int64), ("v_page_stride", C.c_int64), ("k_scale_stride", C.c_int64),
+                ("v_scale_stride", C.c_int64), ("table", C.c_void_p), ("format", C.c_int32), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_seqs", C.c_int32),
+                ("max_pages", C.c_int32)]
 
 
 class PfNorm(C.Structure):
@@ -189,6 +200,22 @@ def load_library():
     lib.pf_op_norm_residual.restype = i32
     lib.pf_op_norm_residual.argtypes = [i32, vp, i64, C.POINTER(PfNorm), vp, i64, i32, f32, vp, i64, vp, i64, C.POINTER(PfNorm),
                                         vp, vp, i64, vp, i64, vp, i32, i32, i32, vp]
+    lib.pf_op_qk_norm_rope.restype = i32
+    lib.pf_op_qk_norm_rope.argtypes = [i32, vp, i64, C.POINTER(PfNorm), vp, i64, i32, vp, i64, C.POINTER(PfNorm), vp, i64, i32,
+                                       C.POINTER(PfRope), vp, i32, i32, vp]
+    lib.pf_kv_mx_row_bytes.restype = i32
+    lib.pf_kv_mx_row_bytes.argtypes = [i32, i32]
+    lib.pf_op_kv_append_mx.restype = i32
+    lib.pf_op_kv_append_mx.argtypes = [i32, C.POINTER(PfKvMxPages), vp, i64, C.POINTER(PfNorm), vp, i64, vp, vp, i32,
+                                       C.POINTER(PfRope), vp, vp, i64, C.POINTER(PfNorm), vp, i64, i32, vp]
+    lib.pf_op_kv_read_mx.restype = i32
+    lib.pf_op_kv_read_mx.argtypes = [i32, C.POINTER(PfKvMxPages), vp, vp, i32, vp, i64, vp, i64, vp]
+    lib.pf_op_attention_mx_ws_bytes.restype = sz
+    lib.pf_op_attention_mx_ws_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, i64]
+    lib.pf_op_attention_mx.restype = i32
+    lib.pf_op_attention_mx.argtypes = [i32, vp, i64, C.POINTER(PfKvMxPages), vp, vp, vp, i32, i32, f32, i32, vp, i64, vp, vp, sz, vp]
+    lib.pf_attention_mx_kernel_name.restype = C.c_char_p
+    lib.pf_attention_mx_kernel_name.argtypes = [i32, i32, i32, i32, i32, i32, i32, i64, C.POINTER(i32)]
     _lib = lib
     return lib
 
@@ -802,3 +829,215 @@ def pf_op_norm_residual(y, x, post=None, pre=None, gate=None, gate_tanh=False, x
             int(gate_tanh), x_scale, x.data_ptr(), _ld(x), x_out.data_ptr(), ldxo, None if pre is None else pre.ref, sh_at,
             sc_at, max(ms, ms2), *h_args, None if cu is None else cu.data_ptr(), n_seqs or 0, rows, d)
     return x_out, h_out if want_h else None
+
+
+# ---- a cache in 8 or 4 bits ----------------------------------------------------------------------------------------------------
+class KvMxPages:
+    """Keys and values in pages of 8- or 4-bit numbers.  format "e4m3" or "e2m1"; k and v uint8 [n_pages, kv_heads, page_size,
+    pf_kv_mx_row_bytes(format, head_dim)], k_scale and v_scale uint8 [n_pages, kv_heads, page_size, ceil(head_dim / 32)] (pages
+    any distance apart, a page contiguous), table int32 [n_seqs, max_pages] of page numbers (those outside [0, n_pages): no page).  Holds
+    the tensors it was given; their contents may change between calls."""
+
+    def __init__(self, format, k, v, k_scale, v_scale, table, head_dim):
+        if format not in MX_FORMATS:
+            raise PfError(-4, f"format {format!r}")
+        row_bytes = pf_kv_mx_row_bytes(format, head_dim)
+        if k.dim() != 4:
+            raise PfError(-3, f"k pages: shape {tuple(k.shape)}")
+        n, self.kv_heads, self.page_size, _ = k.shape
+        rows = (n, self.kv_heads, self.page_size)
+        for name, t, last in (("k", k, row_bytes), ("v", v, row_bytes), ("k_scale", k_scale, -(-head_dim // PF_MX_BLOCK)),
+                              ("v_scale", v_scale, -(-head_dim // PF_MX_BLOCK))):
+            _plain(name, t, torch.uint8, k.device)
+            if tuple(t.shape) != (*rows, last) or not (n == 0 or t[0].is_contiguous()):
+                raise PfError(-3, f"{name} pages: shape {tuple(t.shape)}, strides {t.stride()}; pages of {(*rows[1:], last)} are needed")
+        if table.dim() != 2:
+            raise PfError(-3, f"table: shape {tuple(table.shape)}, [n_seqs, max_pages] is needed")
+        _ints("table", table, table.shape, k.device)
+        self.format, self.head_dim = format, head_dim
+        self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
+        self.n_seqs, self.max_pages = table.shape
+        if (n | self.kv_heads | self.page_size | self.n_seqs | self.max_pages) >> 31:
+            _too_large("pages", *k.shape, *table.shape)
+        self.device, self.index = k.device, k.get_device()
+        stride = lambda t: t.stride(0) if n > 1 else t.shape[1] * t.shape[2] * t.shape[3]
+        self.c = PfKvMxPages(k=k.data_ptr(), v=v.data_ptr(), k_scale=k_scale.data_ptr(), v_scale=v_scale.data_ptr(),
+                             k_page_stride=stride(k), v_page_stride=stride(v), k_scale_stride=stride(k_scale),
+                             v_scale_stride=stride(v_scale), table=table.data_ptr(), format=MX_FORMATS[format], n_pages=n,
+                             page_size=self.page_size, kv_heads=self.kv_heads, head_dim=head_dim, n_seqs=self.n_seqs,
+                             max_pages=self.max_pages)
+        self.ref = C.byref(self.c)
+
+    @classmethod
+    def zeros(cls, format, n_pages, kv_heads, page_size, head_dim, table):
+        """Pages of zeros on the table's GPU."""
+        if format not in MX_FORMATS:
+            raise PfError(-4, f"format {format!r}")
+        shape = (n_pages, kv_heads, page_size)
+        new = lambda last: torch.zeros(*shape, last, dtype=torch.uint8, device=table.device)
+        row, blocks = pf_kv_mx_row_bytes(format, head_dim), -(-head_dim // PF_MX_BLOCK)
+        return cls(format, new(row), new(row), new(blocks), new(blocks), table, head_dim)
+
+
+def pf_kv_mx_row_bytes(format, head_dim):
+    """Bytes of a row of codes."""
+    n = load_library().pf_kv_mx_row_bytes(MX_FORMATS.get(format, -1), head_dim) if 0 < head_dim < 2 ** 31 else 0
+    if n == 0:
+        raise PfError(-3, f"format {format!r}, heads of {head_dim}")
+    return n
+
+
+def _head_norm(side, norm, dtype, index, device, head_dim):
+    if norm is None:
+        return None
+    if norm.key != (dtype, index, head_dim):
+        norm.check(side, dtype, device, head_dim)
+    return norm.ref
+
+
+def pf_op_qk_norm_rope(q, k, head_dim, q_norm=None, k_norm=None, rope=None, pos=None, q_out=None, k_out=None):
+    """Every head of q [tokens, heads * head_dim] and k [tokens, kv_heads * head_dim] (either may be None) normed (make_norm with
+    weights [head_dim], or None) and turned by its row's position(s) (pos as for pf_op_rope).  Returns (q_out, k_out); the outputs
+    may be the inputs."""
+    x = q if q is not None else k
+    if x is None:
+        raise PfError(-1, "q and k")
+    dt, index, dev = x.dtype, x.get_device(), x.device
+    if index < 0 or dt not in _DT:
+        _rows("q" if q is not None else "k", x)
+    tokens = x.shape[0]
+    sides = []
+    for name, t, out in (("q", q, q_out), ("k", k, k_out)):
+        if t is None:
+            if out is not None:
+                raise PfError(-1, f"{name}_out without {name}")
+            sides.append((None, 0, None, 0, 0))
+            continue
+        if not _good_rows(t, dt, index):
+            _rows(name, t, dt, dev)
+        n, width = t.shape
+        if n != tokens:
+            raise PfError(-3, f"{name}: {n} rows, q has {tokens}")
+        if (n | width) >> 31:
+            _too_large(name, n, width)
+        heads = _heads(name, t, head_dim)
+        if out is None:
+            out, ldo = _like(t), width
+        else:
+            ldo = _ld(_out(name + "_out", out, t.shape, dt, dev))
+        if name == "q":
+            q_out = out
+        else:
+            k_out = out
+        sides.append((t.data_ptr(), _ld(t), out.data_ptr(), ldo, heads))
+    if rope is not None:
+        if pos is None:
+            raise PfError(-1, "pos")
+        _positions(rope, pos, tokens, index, dev)
+    (qp, ldq, qo, ldqo, n_heads), (kp, ldk, ko, ldko, kv_heads) = sides
+    _launch(index, (_lib or load_library()).pf_op_qk_norm_rope, _DT[dt], qp, ldq, _head_norm("q", q_norm, dt, index, dev, head_dim), qo,
+            ldqo, n_heads, kp, ldk, _head_norm("k", k_norm, dt, index, dev, head_dim), ko, ldko, kv_heads,
+            None if rope is None else C.byref(rope), None if rope is None else pos.data_ptr(), tokens, head_dim)
+    return q_out, k_out
+
+
+def pf_op_kv_append_mx(pages, k, v, cu, first, k_norm=None, rope=None, pos=None, q=None, q_norm=None, q_out=None):
+    """Writes rows of k and v [tokens, kv_heads * head_dim] into pages of few bits, row cu[s] + i of sequence s into slot first[s] + i, k
+    normed and turned on the way; returns q normed and turned likewise (None without q)."""
+    dt, dev, index, dh = k.dtype, pages.device, pages.index, pages.head_dim
+    if not (dt in _DT and _good_rows(k, dt, index) and _good_rows(v, dt, index) and v.shape == k.shape and
+            _good_ints(cu, (pages.n_seqs + 1,), index) and _good_ints(first, (pages.n_seqs,), index)):
+        _rows("k", k, None, dev)
+        _out("v", v, k.shape, dt, dev)
+        _ints("cu", cu, (pages.n_seqs + 1,), dev)
+        _ints("first", first, (pages.n_seqs,), dev)
+    tokens, width = k.shape
+    if tokens >> 31:
+        _too_large("k", tokens, width)
+    if width != pages.kv_heads * dh:
+        raise PfError(-3, f"k: rows of {width} channels for {pages.kv_heads} heads of {dh}")
+    if rope is not None:
+        if pos is None:
+            raise PfError(-1, "pos")
+        _positions(rope, pos, tokens, index, dev)
+    if q is None:
+        if q_out is not None:
+            raise PfError(-1, "q_out without q")
+        q_args = (None, 0, None, None, 0, 0)
+    else:
+        if not _good_rows(q, dt, index):
+            _rows("q", q, dt, dev)
+        if q.shape[0] != tokens:
+            raise PfError(-3, f"q: {q.shape[0]} rows, k has {tokens}")
+        if q.shape[1] >> 31:
+            _too_large("q", *q.shape)
+        heads = _heads("q", q, dh)
+        if q_out is None:
+            q_out, ldo = _like(q), heads * dh
+        else:
+            ldo = _ld(_out("q_out", q_out, q.shape, dt, dev))
+        q_args = (q.data_ptr(), _ld(q), _head_norm("q", q_norm, dt, index, dev, dh), q_out.data_ptr(), ldo, heads)
+    _launch(index, (_lib or load_library()).pf_op_kv_append_mx, _DT[dt], pages.ref, k.data_ptr(), _ld(k),
+            _head_norm("k", k_norm, dt, index, dev, dh), v.data_ptr(), _ld(v), cu.data_ptr(), first.data_ptr(), tokens,
+            None if rope is None else C.byref(rope), None if rope is None else pos.data_ptr(), *q_args)
+    return q_out
+
+
+def pf_op_kv_read_mx(pages, cu, first, tokens, dtype, k_out=None, v_out=None):
+    """Rows [tokens, kv_heads * head_dim] of `dtype` from pages of few bits: row cu[s] + i is slot first[s] + i of sequence s, zeros
+    where there is no page.  Returns (k, v); rows of no sequence are not written."""
+    dev, index = pages.device, pages.index
+    if dtype not in _DT:
+        raise PfError(-4, f"dtype {dtype}")
+    if not (_good_ints(cu, (pages.n_seqs + 1,), index) and _good_ints(first, (pages.n_seqs,), index)):
+        _ints("cu", cu, (pages.n_seqs + 1,), dev)
+        _ints("first", first, (pages.n_seqs,), dev)
+    if not 0 <= tokens < 2 ** 31:
+        _too_large("tokens", tokens)
+    shape = (tokens, pages.kv_heads * pages.head_dim)
+    if k_out is None:
+        k_out, ldk = torch.empty(shape, dtype=dtype, device=dev), shape[1]
+    else:
+        ldk = _ld(_out("k_out", k_out, shape, dtype, dev))
+    if v_out is None:
+        v_out, ldv = torch.empty(shape, dtype=dtype, device=dev), shape[1]
+    else:
+        ldv = _ld(_out("v_out", v_out, shape, dtype, dev))
+    _launch(index, (_lib or load_library()).pf_op_kv_read_mx, _DT[dtype], pages.ref, cu.data_ptr(), first.data_ptr(), tokens,
+            k_out.data_ptr(), ldk, v_out.data_ptr(), ldv)
+    return k_out, v_out
+
+
+@functools.lru_cache(maxsize=1024)
+def _mx_ws_bytes(*sizes):
+    return load_library().pf_op_attention_mx_ws_bytes(*sizes)
+
+
+def pf_op_attention_mx(q, pages, cu_q, first, kv_len, causal=True, scale=None, out=None, want_lse=False):
+    """pf_op_attention_paged over pages of few bits; q [total_q, heads * head_dim] of either type."""
+    index, dt, dev = pages.index, q.dtype, pages.device
+    if not (dt in _DT and _good_rows(q, dt, index) and _good_ints(cu_q, (pages.n_seqs + 1,), index) and
+            _good_ints(kv_len, (pages.n_seqs,), index) and (first is None or _good_ints(first, (pages.n_seqs,), index))):
+        _rows("q", q, None, dev)
+        _ints("cu_q", cu_q, (pages.n_seqs + 1,), dev)
+        _ints("kv_len", kv_len, (pages.n_seqs,), dev)
+        if first is not None:
+            _ints("first", first, (pages.n_seqs,), dev)
+    rows, width = q.shape
+    if (rows | width) >> 31:
+        _too_large("q", *q.shape)
+    heads = _heads("q", q, pages.head_dim)
+    if scale is not None and not scale > 0:
+        raise PfError(-3, f"scale: {scale}")
+    if out is None:
+        out, ldo = _like(q), width
+    else:
+        ldo = _ld(_out("out", out, q.shape, dt, dev))
+    lse = torch.empty(rows, heads, dtype=torch.float32, device=dev) if want_lse else None
+    n = _mx_ws_bytes(_DT[dt], MX_FORMATS[pages.format], rows, pages.n_seqs, heads, pages.kv_heads, pages.head_dim,
+                     pages.max_pages * pages.page_size)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _launch(index, (_lib or load_library()).pf_op_attention_mx, _DT[dt], q.data_ptr(), _ld(q), pages.ref, cu_q.data_ptr(),
+            None if first is None else first.data_ptr(), kv_len.data_ptr(), rows, heads, 0.0 if scale is None else scale, int(causal),
+            out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), n)
+    return (out, lse) if want_lse else out

@@ -14,25 +14,26 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpfstage.so")
 SOURCES = ["elementwise.hip", "gemm_simt.hip", "gemm_mfma.hip", "gemm_mfma_dl.hip", "gemm_mfma_f32.hip", "attn_simt.hip", "attn_mfma_f32.hip", "attn_mfma.hip", "attn_mfma2.hip", "probe.hip", "tuning.hip", "stage.hip",
-           "rope_rows.hip", "norm_residual.hip", "attn_rows.hip", "requests.hip"]
+           "rope_rows.hip", "norm_residual.hip", "attn_rows.hip", "attn_rows_mx.hip", "mx_rows.hip", "requests.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed-fp32 arithmetic is kept off for all device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
-# attn_rows.hip: results of matrix instructions in ordinary registers also in the kernels with more than 256 of them.  Left to
+# attn_rows.h: results of matrix instructions in ordinary registers also in the kernels with more than 256 of them.  Left to
 # itself the compiler puts all of them into accumulation registers there, and every score, which the vector unit works on
 # next, is copied out of them.
-FILE_FLAGS = {"attn_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+_ATTN_ROWS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+FILE_FLAGS = {"attn_rows.hip": _ATTN_ROWS, "attn_rows_mx.hip": _ATTN_ROWS}
 
 
 # Kernels that must not use scratch memory: their LDS fragment reads are asynchronous inline-assembly loads whose
 # completion is tracked by hand, so a register spill between a read and its wait would save a value that has not
 # arrived - wrong results, not just slow ones.  The compiler reports every kernel's scratch size; the build checks it.
-# attn_rows.hip: the compiler has been seen to save a register in front of the instruction that makes all lanes active again behind
+# attn_rows.h: the compiler has been seen to save a register in front of the instruction that makes all lanes active again behind
 # a divergent branch, so that the other lanes' values - addresses of rows - were lost.  None of its kernels saves one to memory; those
 # that need more than 256 vector registers move values to accumulation registers and back, and the build looks at where these moves stand.
-NO_SCRATCH = {"attn_mfma2.hip": "attn_mfma2_kernel", "attn_rows.hip": "attn_rows"}
+NO_SCRATCH = {"attn_mfma2.hip": "attn_mfma2_kernel", "attn_rows.hip": "attn_rows", "attn_rows_mx.hip": "attn_rows"}
 
 
 def _check_no_scratch(src, log):
@@ -52,7 +53,7 @@ def _check_no_scratch(src, log):
         raise RuntimeError(f"{src}: the compiler reported no resource usage for {want}; cannot check for spills")
 
 
-MOVES_CHECKED = ("attn_rows.hip",)
+MOVES_CHECKED = ("attn_rows.hip", "attn_rows_mx.hip")
 _WIDENS = re.compile(r"s_(or|xor)_b(32|64) exec|s_mov_b(32|64) exec|s_(or|andn2|orn2)_saveexec")
 
 

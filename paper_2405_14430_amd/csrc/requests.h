@@ -47,6 +47,14 @@ inline Pages pages_of(const pf_kv_pages &p) {
   return Pages{p.k, p.v, p.k_page_stride, p.v_page_stride, p.table, p.n_pages, __builtin_ctz((unsigned)p.page_size), p.max_pages};
 }
 
+// Pages of 8- or 4-bit numbers: `pages` has bytes and strides in bytes; a row of a head is row_bytes of codes and, in arrays of their own,
+// `blocks` exponents.  No scales: pages of rows.
+struct MxPages {
+  int format, row_bytes, blocks;
+  uint8_t *k_scale, *v_scale;
+  int64_t k_scale_stride, v_scale_stride;
+};
+
 // Calls that move more bytes than the 256 MiB cache in front of the memory holds read their rows with non-temporal loads, which do not
 // push out what is being written; smaller ones find rows there that the kernel before has left, and lose by it (append of 16384 rows
 // of 32 + 2 x 8 heads of 128, bf16, 400 MB: 81 -> 66 us, 8192 rows 34 -> 37; norm of 8192 rows of 4096, bf16, 403 MB:
@@ -87,12 +95,41 @@ struct NormResidual {
 };
 hipError_t launch_norm_residual(const NormResidual &a, hipStream_t s);
 
+// Heads of q and k normed and turned; with n_seqs, k and v go into pages of few bits (k_out, ldko are not used then).
+struct HeadRows {
+  int dt;
+  const void *q; int64_t ldq; void *q_out; int64_t ldqo; int n_heads;
+  const void *k; int64_t ldk; void *k_out; int64_t ldko; int kv_heads;
+  const void *v; int64_t ldv;
+  NormSide norm[2];        // of q and of k
+  const int32_t *pos;
+  int tokens, head_dim;
+  Pages pages;             // strides in bytes
+  MxPages mx;
+  const int32_t *cu, *first;
+  int n_seqs;              // 0: no pages
+  bool once;               // rows are read with non-temporal loads (set at the launch)
+};
+hipError_t launch_head_rows(const HeadRows &a, const pf_rope *rope, hipStream_t s);
+
+// Slots of pages of few bits to rows; k_out or v_out may be nullptr.
+struct MxRead {
+  int dt;
+  Pages pages;             // strides in bytes
+  MxPages mx;
+  const int32_t *cu, *first;
+  int n_seqs, tokens, kv_heads, head_dim;
+  void *k_out; int64_t ldk; void *v_out; int64_t ldv;
+};
+hipError_t launch_mx_read(const MxRead &a, hipStream_t s);
+
 // Attention of packed query rows over packed keys (pages.k == nullptr) or over pages.
 struct RowsAttn {
   int dt;
   const void *q; int64_t ldq;
   const void *k; int64_t ldk; const void *v; int64_t ldv;   // packed keys: rows cu_k[s] .. cu_k[s + 1]
   Pages pages;                                              // paged keys: slots [0, kv_len[s])
+  MxPages mx;                                               // pages.k and pages.v hold its numbers (launch_mx_attention)
   const int32_t *cu_q, *cu_k, *first, *kv_len;
   int n_seqs, total_q, total_k;
   int n_heads, kv_heads, head_dim;
@@ -107,5 +144,7 @@ enum { ROWS_TILES, ROWS_WIDE, ROWS_KEYS };   // kernels of attn_rows.hip
 struct RowsPlan { int shape, splits, least_keys; size_t ws_bytes; };   // splits: chunks of the keys, none smaller than least_keys
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv);
 hipError_t launch_rows_attention(const RowsAttn &a, hipStream_t s);
+hipError_t launch_mx_attention(const RowsAttn &a, hipStream_t s);
+hipError_t launch_rows_join(const RowsAttn &a, hipStream_t s);   // of the partial results in a.ws
 
 }  // namespace pf

@@ -3,6 +3,9 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
+
+#include "mx.h"
 #include "requests.h"
 
 using namespace pf;
@@ -44,18 +47,57 @@ const char *rope_wrong(const pf_rope &r, int head_dim) {
   return nullptr;
 }
 
-pf_status pages_check(int dtype, const pf_kv_pages *p, const char *who) {
-  if (!p->k || !p->v || !p->table) return refuse(PF_ERR_NULL, "%s: k, v or table of the pages is NULL", who);
+// what pf_kv_pages and pf_kv_mx_pages have in common
+template <typename P>
+pf_status page_sizes_check(const P *p, const char *who) {
   if (!head_ok(p->head_dim) || p->kv_heads < 1 || p->kv_heads > 65536 || p->n_seqs < 0 || p->n_seqs > kMaxSeqs || p->max_pages < 1 || p->n_pages < 1)
     return refuse(PF_ERR_SHAPE, "%s: pages: head_dim %d, kv_heads %d, n_seqs %d, max_pages %d, n_pages %d", who, p->head_dim, p->kv_heads,
                   p->n_seqs, p->max_pages, p->n_pages);
   if (p->page_size < 16 || p->page_size > 1024 || (p->page_size & (p->page_size - 1)))
     return refuse(PF_ERR_SHAPE, "%s: page_size %d is no power of two in 16 .. 1024", who, p->page_size);
+  return PF_OK;
+}
+
+pf_status pages_check(int dtype, const pf_kv_pages *p, const char *who) {
+  if (!p->k || !p->v || !p->table) return refuse(PF_ERR_NULL, "%s: k, v or table of the pages is NULL", who);
+  if (pf_status st = page_sizes_check(p, who); st != PF_OK) return st;
   const int64_t block = (int64_t)p->kv_heads * p->page_size * p->head_dim;
   if (!row_stride_ok(p->k_page_stride, block, dtype) || !row_stride_ok(p->v_page_stride, block, dtype) || !aligned(p->k, 16) || !aligned(p->v, 16))
     return refuse(PF_ERR_SHAPE, "%s: pages: strides of at least %lld elements in whole 16 bytes, pointers 16-byte aligned", who, (long long)block);
   if (p->k_page_stride > INT64_MAX / 8 / p->n_pages || p->v_page_stride > INT64_MAX / 8 / p->n_pages)
     return refuse(PF_ERR_SHAPE, "%s: pages: n_pages * stride overflows", who);
+  return PF_OK;
+}
+
+pf_status mx_pages_check(const pf_kv_mx_pages *p, const char *who) {
+  if (!p->k || !p->v || !p->k_scale || !p->v_scale || !p->table) return refuse(PF_ERR_NULL, "%s: k, v, their scales or table of the pages is NULL", who);
+  if (p->format != PF_MX_E4M3 && p->format != PF_MX_E2M1) return refuse(PF_ERR_DTYPE, "%s: pages: format %d", who, p->format);
+  if (pf_status st = page_sizes_check(p, who); st != PF_OK) return st;
+  const int64_t rows = (int64_t)p->kv_heads * p->page_size, block = rows * mx_row_bytes(p->format, p->head_dim), scales = rows * mx_blocks(p->head_dim);
+  if (p->k_page_stride < block || p->v_page_stride < block || p->k_page_stride % 16 || p->v_page_stride % 16 || !aligned(p->k, 16) || !aligned(p->v, 16))
+    return refuse(PF_ERR_SHAPE, "%s: pages: strides of at least %lld bytes in whole 16, pointers 16-byte aligned", who, (long long)block);
+  if (p->k_scale_stride < scales || p->v_scale_stride < scales)
+    return refuse(PF_ERR_SHAPE, "%s: pages: strides of at least %lld bytes between the scales of pages", who, (long long)scales);
+  const int64_t most = std::max(std::max(p->k_page_stride, p->v_page_stride), std::max(p->k_scale_stride, p->v_scale_stride));
+  if (most > INT64_MAX / 8 / p->n_pages) return refuse(PF_ERR_SHAPE, "%s: pages: n_pages * stride overflows", who);
+  return PF_OK;
+}
+Pages mx_places(const pf_kv_mx_pages &p) {
+  return Pages{p.k, p.v, p.k_page_stride, p.v_page_stride, p.table, p.n_pages, __builtin_ctz((unsigned)p.page_size), p.max_pages};
+}
+MxPages mx_numbers(const pf_kv_mx_pages &p) {
+  return MxPages{p.format, mx_row_bytes(p.format, p.head_dim), mx_blocks(p.head_dim), (uint8_t *)p.k_scale, (uint8_t *)p.v_scale, p.k_scale_stride, p.v_scale_stride};
+}
+
+// The norm of a side's heads into `to`, or what is wrong with it.
+pf_status head_norm(const pf_norm *n, NormSide &to, const char *who) {
+  to = NormSide{PF_NORM_NONE, 0.f, nullptr, nullptr};
+  if (!n) return PF_OK;
+  if (n->kind < PF_NORM_NONE || n->kind > PF_NORM_LAYER) return refuse(PF_ERR_CONFIG, "%s: norm kind %d", who, n->kind);
+  if (n->kind != PF_NORM_NONE && !(n->eps >= 0.f)) return refuse(PF_ERR_CONFIG, "%s: norm eps", who);
+  if (n->kind == PF_NORM_NONE && (n->weight || n->bias)) return refuse(PF_ERR_CONFIG, "%s: weights of a norm of kind NONE", who);
+  if (!aligned(n->weight, 16) || !aligned(n->bias, 16)) return refuse(PF_ERR_SHAPE, "%s: alignment of norm weights", who);
+  to = NormSide{n->kind, n->eps, n->weight, n->bias};
   return PF_OK;
 }
 
@@ -186,7 +228,7 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
   a.shape = p.shape;
   a.splits = p.splits;
   a.least_keys = p.least_keys;
-  return launched(launch_rows_attention(a, (hipStream_t)stream), who);
+  return launched(a.mx.k_scale ? launch_mx_attention(a, (hipStream_t)stream) : launch_rows_attention(a, (hipStream_t)stream), who);
 }
 
 pf_status pf_op_attention_packed(int dtype, const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv,
@@ -267,6 +309,117 @@ pf_status pf_op_norm_residual(int dtype, const void *y, int64_t ldy, const pf_no
   a.x = x; a.ldx = ldx; a.x_out = x_out; a.ldxo = ldxo; a.shift = shift; a.scale = scale; a.mod_stride = mod_stride; a.h = h; a.ldh = ldh;
   a.cu = cu; a.n_seqs = n_seqs; a.rows = rows; a.d = d;
   return launched(launch_norm_residual(a, (hipStream_t)stream), who);
+}
+
+int pf_kv_mx_row_bytes(int format, int head_dim) {
+  return (format == PF_MX_E4M3 || format == PF_MX_E2M1) && head_ok(head_dim) ? mx_row_bytes(format, head_dim) : 0;
+}
+
+pf_status pf_op_qk_norm_rope(int dtype, const void *q, int64_t ldq, const pf_norm *q_norm, void *q_out, int64_t ldqo, int n_heads,
+                             const void *k, int64_t ldk, const pf_norm *k_norm, void *k_out, int64_t ldko, int kv_heads,
+                             const pf_rope *rope, const int32_t *pos, int tokens, int head_dim, void *stream) {
+  const char *who = "pf_op_qk_norm_rope";
+  if (tokens < 0 || n_heads < 0 || n_heads > 65536 || kv_heads < 0 || kv_heads > 65536)
+    return refuse(PF_ERR_SHAPE, "%s: %d tokens, %d and %d heads", who, tokens, n_heads, kv_heads);
+  if (!dt_ok(dtype)) return refuse(PF_ERR_DTYPE, "%s: dtype %d", who, dtype);
+  if (tokens == 0 || n_heads + kv_heads == 0) return PF_OK;
+  if ((n_heads && (!q || !q_out)) || (kv_heads && (!k || !k_out)) || (rope && !pos)) return refuse(PF_ERR_NULL, "%s: NULL", who);
+  if (!head_ok(head_dim)) return refuse(PF_ERR_SHAPE, "%s: heads of %d", who, head_dim);
+  const int64_t dq = (int64_t)n_heads * head_dim, dk = (int64_t)kv_heads * head_dim;
+  if ((n_heads && (!row_stride_ok(ldq, dq, dtype) || !row_stride_ok(ldqo, dq, dtype) || !aligned(q, 16) || !aligned(q_out, 16))) ||
+      (kv_heads && (!row_stride_ok(ldk, dk, dtype) || !row_stride_ok(ldko, dk, dtype) || !aligned(k, 16) || !aligned(k_out, 16))) ||
+      (rope && !aligned(pos, 4)))
+    return refuse(PF_ERR_SHAPE, "%s: row strides %lld, %lld for rows of %lld (k %lld, %lld for %lld), or alignment", who, (long long)ldq, (long long)ldqo,
+                  (long long)dq, (long long)ldk, (long long)ldko, (long long)dk);
+  if (tokens > kMaxRows) return refuse(PF_ERR_SHAPE, "%s: %d tokens are more than %d", who, tokens, kMaxRows);
+  if ((n_heads && q == q_out && ldq != ldqo) || (kv_heads && k == k_out && ldk != ldko)) return refuse(PF_ERR_SHAPE, "%s: in place with two row strides", who);
+  if (rope)
+    if (const char *w = rope_wrong(*rope, head_dim)) return refuse(PF_ERR_CONFIG, "%s", w);
+  HeadRows a{};
+  if (pf_status st = head_norm(n_heads ? q_norm : nullptr, a.norm[0], who); st != PF_OK) return st;
+  if (pf_status st = head_norm(kv_heads ? k_norm : nullptr, a.norm[1], who); st != PF_OK) return st;
+  a.dt = dtype; a.q = q; a.ldq = ldq; a.q_out = q_out; a.ldqo = ldqo; a.n_heads = n_heads;
+  a.k = k; a.ldk = ldk; a.k_out = k_out; a.ldko = ldko; a.kv_heads = kv_heads;
+  a.pos = pos; a.tokens = tokens; a.head_dim = head_dim;
+  return launched(launch_head_rows(a, rope, (hipStream_t)stream), who);
+}
+
+pf_status pf_op_kv_append_mx(int dtype, const pf_kv_mx_pages *pages, const void *k, int64_t ldk, const pf_norm *k_norm, const void *v,
+                             int64_t ldv, const int32_t *cu, const int32_t *first, int tokens, const pf_rope *rope, const int32_t *pos,
+                             const void *q, int64_t ldq, const pf_norm *q_norm, void *q_out, int64_t ldqo, int n_heads, void *stream) {
+  const char *who = "pf_op_kv_append_mx";
+  if (tokens < 0 || n_heads < 0 || n_heads > 65536) return refuse(PF_ERR_SHAPE, "%s: %d tokens, %d heads", who, tokens, n_heads);
+  if (!dt_ok(dtype)) return refuse(PF_ERR_DTYPE, "%s: dtype %d", who, dtype);
+  if (tokens == 0 || (pages && pages->n_seqs == 0)) return PF_OK;
+  if (!pages || !k || !v || !cu || !first || (rope && !pos) || (n_heads && (!q || !q_out))) return refuse(PF_ERR_NULL, "%s: NULL", who);
+  if (!n_heads && q) return refuse(PF_ERR_SHAPE, "%s: q without heads", who);
+  if (pf_status st = mx_pages_check(pages, who); st != PF_OK) return st;
+  const int64_t d = (int64_t)pages->kv_heads * pages->head_dim, dq = (int64_t)n_heads * pages->head_dim;
+  if (!row_stride_ok(ldk, d, dtype) || !row_stride_ok(ldv, d, dtype) || !aligned(k, 16) || !aligned(v, 16) || (rope && !aligned(pos, 4)) ||
+      (n_heads && (!row_stride_ok(ldq, dq, dtype) || !row_stride_ok(ldqo, dq, dtype) || !aligned(q, 16) || !aligned(q_out, 16))))
+    return refuse(PF_ERR_SHAPE, "%s: row strides %lld, %lld for rows of %lld (q %lld, %lld for %lld), or alignment", who, (long long)ldk, (long long)ldv,
+                  (long long)d, (long long)ldq, (long long)ldqo, (long long)dq);
+  if (tokens > kMaxRows) return refuse(PF_ERR_SHAPE, "%s: %d tokens are more than %d", who, tokens, kMaxRows);
+  if (n_heads && q == q_out && ldq != ldqo) return refuse(PF_ERR_SHAPE, "%s: in place with two row strides", who);
+  if (rope)
+    if (const char *w = rope_wrong(*rope, pages->head_dim)) return refuse(PF_ERR_CONFIG, "%s", w);
+  HeadRows a{};
+  if (pf_status st = head_norm(n_heads ? q_norm : nullptr, a.norm[0], who); st != PF_OK) return st;
+  if (pf_status st = head_norm(k_norm, a.norm[1], who); st != PF_OK) return st;
+  a.dt = dtype; a.q = q; a.ldq = ldq; a.q_out = q_out; a.ldqo = ldqo; a.n_heads = n_heads;
+  a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.kv_heads = pages->kv_heads;
+  a.pos = pos; a.tokens = tokens; a.head_dim = pages->head_dim;
+  a.pages = mx_places(*pages); a.mx = mx_numbers(*pages); a.cu = cu; a.first = first; a.n_seqs = pages->n_seqs;
+  return launched(launch_head_rows(a, rope, (hipStream_t)stream), who);
+}
+
+pf_status pf_op_kv_read_mx(int dtype, const pf_kv_mx_pages *pages, const int32_t *cu, const int32_t *first, int tokens, void *k_out,
+                           int64_t ldk, void *v_out, int64_t ldv, void *stream) {
+  const char *who = "pf_op_kv_read_mx";
+  if (tokens < 0) return refuse(PF_ERR_SHAPE, "%s: %d tokens", who, tokens);
+  if (!dt_ok(dtype)) return refuse(PF_ERR_DTYPE, "%s: dtype %d", who, dtype);
+  if (tokens == 0 || (pages && pages->n_seqs == 0)) return PF_OK;
+  if (!pages || !cu || !first || (!k_out && !v_out)) return refuse(PF_ERR_NULL, "%s: NULL", who);
+  if (pf_status st = mx_pages_check(pages, who); st != PF_OK) return st;
+  const int64_t d = (int64_t)pages->kv_heads * pages->head_dim;
+  if ((k_out && (!row_stride_ok(ldk, d, dtype) || !aligned(k_out, 16))) || (v_out && (!row_stride_ok(ldv, d, dtype) || !aligned(v_out, 16))))
+    return refuse(PF_ERR_SHAPE, "%s: row strides %lld, %lld for rows of %lld, or alignment", who, (long long)ldk, (long long)ldv, (long long)d);
+  if (tokens > kMaxRows) return refuse(PF_ERR_SHAPE, "%s: %d tokens are more than %d", who, tokens, kMaxRows);
+  MxRead a{};
+  a.dt = dtype; a.pages = mx_places(*pages); a.mx = mx_numbers(*pages); a.cu = cu; a.first = first; a.n_seqs = pages->n_seqs;
+  a.tokens = tokens; a.kv_heads = pages->kv_heads; a.head_dim = pages->head_dim; a.k_out = k_out; a.ldk = ldk; a.v_out = v_out; a.ldv = ldv;
+  return launched(launch_mx_read(a, (hipStream_t)stream), who);
+}
+
+size_t pf_op_attention_mx_ws_bytes(int dtype, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
+  if (format != PF_MX_E4M3 && format != PF_MX_E2M1) return 0;
+  return pf_op_attention_rows_ws_bytes(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
+}
+
+const char *pf_attention_mx_kernel_name(int dtype, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim,
+                                        int64_t max_kv, int *chunks) {
+  if (format != PF_MX_E4M3 && format != PF_MX_E2M1) return "";
+  return pf_attention_rows_kernel_name(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv, chunks);
+}
+
+pf_status pf_op_attention_mx(int dtype, const void *q, int64_t ldq, const pf_kv_mx_pages *pages, const int32_t *cu_q,
+                             const int32_t *first, const int32_t *kv_len, int total_q, int n_heads, float scale, int causal, void *out,
+                             int64_t ldo, float *lse, void *ws, size_t ws_bytes, void *stream) {
+  const char *who = "pf_op_attention_mx";
+  if (total_q < 0) return refuse(PF_ERR_SHAPE, "%s: %d rows", who, total_q);
+  if (!dt_ok(dtype)) return refuse(PF_ERR_DTYPE, "%s: dtype %d", who, dtype);
+  if (total_q == 0 || (pages && pages->n_seqs == 0)) return PF_OK;
+  if (!pages || !q || !out || !cu_q || !kv_len || (causal && !first)) return refuse(PF_ERR_NULL, "%s: NULL", who);
+  if (pf_status st = mx_pages_check(pages, who); st != PF_OK) return st;
+  if (!heads_ok(total_q, n_heads, pages->kv_heads))
+    return refuse(PF_ERR_SHAPE, "%s: %d rows, %d heads over %d", who, total_q, n_heads, pages->kv_heads);
+  const int64_t max_kv = (int64_t)pages->max_pages * pages->page_size;
+  if (max_kv > kMaxKeys) return refuse(PF_ERR_SHAPE, "%s: max_pages * page_size = %lld", who, (long long)max_kv);
+  RowsAttn a{};
+  a.dt = dtype; a.q = q; a.ldq = ldq; a.pages = mx_places(*pages); a.mx = mx_numbers(*pages); a.cu_q = cu_q; a.first = causal ? first : nullptr;
+  a.kv_len = kv_len; a.n_seqs = pages->n_seqs; a.total_q = total_q; a.n_heads = n_heads; a.kv_heads = pages->kv_heads; a.head_dim = pages->head_dim;
+  a.scale = scale; a.causal = causal != 0; a.out = out; a.ldo = ldo; a.lse = lse;
+  return rows_attention(a, max_kv, ws, ws_bytes, stream, who);
 }
 
 }  // extern "C"
