@@ -45,4 +45,24 @@ template <int FMT, int I> __device__ float2 mx_decode_f32(unsigned, float) { ret
 #endif
 __device__ __forceinline__ float mx_power(unsigned byte) { return __uint_as_float(byte << 23); }
 
+// Eight codes of a block (one or two words) as bf16 or floats, four to a quadruple.
+typedef unsigned mx_u32x4 __attribute__((ext_vector_type(4)));
+template <int FMT>
+__device__ __forceinline__ void mx_unit(const unsigned (&code)[2], float power, mx_u32x4 (&out)[1]) {
+  if constexpr (FMT == PF_MX_E4M3)
+    out[0] = mx_u32x4{mx_decode_bf16<FMT, 0>(code[0], power), mx_decode_bf16<FMT, 1>(code[0], power), mx_decode_bf16<FMT, 0>(code[1], power),
+                      mx_decode_bf16<FMT, 1>(code[1], power)};
+  else
+    out[0] = mx_u32x4{mx_decode_bf16<FMT, 0>(code[0], power), mx_decode_bf16<FMT, 1>(code[0], power), mx_decode_bf16<FMT, 2>(code[0], power),
+                      mx_decode_bf16<FMT, 3>(code[0], power)};
+}
+template <int FMT>
+__device__ __forceinline__ void mx_unit(const unsigned (&code)[2], float power, mx_u32x4 (&out)[2]) {
+  constexpr bool WIDE = FMT == PF_MX_E4M3;
+  const float2 a = mx_decode_f32<FMT, 0>(code[0], power), b = mx_decode_f32<FMT, 1>(code[0], power);
+  const float2 c = mx_decode_f32<FMT, WIDE ? 0 : 2>(code[WIDE], power), d = mx_decode_f32<FMT, WIDE ? 1 : 3>(code[WIDE], power);
+  out[0] = mx_u32x4{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
+  out[1] = mx_u32x4{__float_as_uint(c.x), __float_as_uint(c.y), __float_as_uint(d.x), __float_as_uint(d.y)};
+}
+
 }  // namespace pf
