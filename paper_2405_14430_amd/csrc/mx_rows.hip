@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kMaxPairs = PF_ROPE_MAX_PAIRS, kMaxDim = 128, kWaves = 4, kMaxTok = 8;
 constexpr int V = 8;                                 // channels of a lane's unit
-enum { TURN_PAIRS, TURN_HALVES, TURN_HALVES_ANY };   // neighbours; an axis' half apart, the halves whole units or not
+enum { TURN_PAIRS, TURN_HALVES, TURN_HALVES_ANY };   // neighbours; an axis' half apart, the halves whole fours of channels or not
 
 struct TurnK {
   double turns[kMaxPairs];
@@ -34,6 +34,7 @@ struct HeadsK {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 // A choice between values: `c ? a : b` of two arguments of a kernel is one of their addresses, from which lanes then load.
 template <typename T>
@@ -58,6 +59,26 @@ struct Unit {
   __device__ __forceinline__ float operator[](int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[i / 4][i % 4]);
     else return __uint_as_float(i & 1 ? w[0][i / 2] & 0xffff0000u : w[0][i / 2] << 16);
+  }
+  // The bits of the largest magnitude, as a float's; those of infinities and NaN are the largest.
+  __device__ __forceinline__ unsigned largest() const {
+    if constexpr (sizeof(T) == 2) {
+      const auto mag = [&](int i) __attribute__((always_inline)) { return __builtin_bit_cast(u16x2, w[0][i] & 0x7fff7fffu); };
+      const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(0), mag(1)), __builtin_elementwise_max(mag(2), mag(3)));
+      return (unsigned)max(m[0], m[1]) << 16;
+    } else {
+      unsigned m = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) m = max(m, w[i / 4][i % 4] & 0x7fffffffu);
+      return m;
+    }
+  }
+  // No magnitude past the float with bits `top` (a bf16 number).
+  __device__ __forceinline__ void bound(unsigned top) {
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = __builtin_amdgcn_fmed3f((*this)[i], -__uint_as_float(top), __uint_as_float(top));
+    round(x);
   }
   __device__ __forceinline__ void round(const float (&x)[V]) {
 #pragma unroll
@@ -131,39 +152,6 @@ __device__ __forceinline__ float inverse_root(float x) {
   return tiny ? r * 0x1p50f : r;
 }
 
-// Codes of the V values of a block whose largest magnitude has the bits `most`, and the exponent's byte.
-template <int FMT>
-__device__ __forceinline__ unsigned encode(const float (&x)[V], unsigned most, unsigned (&code)[V * Mx<FMT>::BITS / 32]) {
-  using M = Mx<FMT>;
-  constexpr unsigned top_mant = M::kTop & 0x7fffffu;
-  const int e = clampi((int)((most + 0x7fffffu - top_mant) >> 23) - (int)(M::kTop >> 23), M::kLeast, M::kMost);
-  const float down = __uint_as_float((unsigned)(127 - e) << 23);   // a power of two: the product is exact
-  const float top = __uint_as_float(M::kTop);
-  const bool none = most >= 0x7f800000u;
-  float y[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) y[i] = __builtin_amdgcn_fmed3f(x[i] * down, -top, top);
-#pragma unroll
-  for (unsigned &w : code) w = 0;
-#if defined(__HIP_DEVICE_COMPILE__)
-  if constexpr (FMT == PF_MX_E4M3) {
-#pragma unroll
-    for (int i = 0; i < V; i += 4) {
-      code[i / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(y[i], y[i + 1], code[i / 4], false);
-      code[i / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(y[i + 2], y[i + 3], code[i / 4], true);
-    }
-  } else {
-    code[0] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code[0], y[0], y[1], 1.0f, 0);
-    code[0] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code[0], y[2], y[3], 1.0f, 1);
-    code[0] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code[0], y[4], y[5], 1.0f, 2);
-    code[0] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code[0], y[6], y[7], 1.0f, 3);
-  }
-#endif
-#pragma unroll
-  for (unsigned &w : code) w = none ? 0 : w;
-  return none ? 255u : (unsigned)(e + 127);
-}
-
 // A lane's heads, step after step: `fit` heads to a wave at a step, the workgroup's tokens behind each other with `heads` heads each, from
 // the wave's place on and `stride` heads further each time.
 struct Walk {
@@ -190,6 +178,11 @@ struct Walk {
   }
 };
 
+// A number that all lanes agree on, in scalar registers.
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v));
+}
+
 // Where packed row `row` of a call goes in the pages: page (-1: none, -2: the row belongs to no sequence) and row of the page.
 __device__ __forceinline__ void find_slot(const Pages &pages, const int32_t *cu, const int32_t *first, int n_seqs, int row, int lane, int64_t &page, int &in_page) {
   page = -2;
@@ -205,9 +198,15 @@ __device__ __forceinline__ void find_slot(const Pages &pages, const int32_t *cu,
   in_page = (int)(slot & ((1 << pages.page_shift) - 1));
 }
 
-// FMT < 0: q and k rows to rows; else k and v into pages.  LAYOUT: of the pairs.  N: lanes of a head (0: any number).  A workgroup takes tok tokens, a wave `fit` heads at a
-// step and kDepth steps' loads at a time, the first of them before the tables are worked out.
-template <typename T> constexpr int kDepth = sizeof(T) == 2 ? 2 : 1;
+// FMT < 0: q and k rows to rows; else k and v into pages.  LAYOUT: of the pairs.  N: lanes of a head (0: any number).
+//
+// A step of a wave is up to `fit` neighbouring heads of one side (q, k or v) of one token, so that all but the channels' own work is the scalar unit's;
+// a token's steps come side after side, and the waves of a workgroup take the steps of its tok tokens in turn.  The rows of the next kDepth
+// steps are on their way meanwhile, the first ones before the tables are worked out.
+template <typename T> constexpr int kDepth = 2;
+struct Step {
+  int t, g;              // token of the workgroup, step of the token
+};
 template <typename T, int FMT, int LAYOUT, int N>
 __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK p) {
 #pragma clang fp contract(off)   // the same rows from all instances: pages get what pf_op_qk_norm_rope gives
@@ -216,75 +215,81 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
   const HeadRows &a = p.r;
   __shared__ __attribute__((aligned(16))) float cosine[kMaxTok][kMaxDim], sine[kMaxTok][kMaxDim];
   __shared__ __attribute__((aligned(16))) float other[HALF ? kWaves : 1][HALF ? 64 * V : 1];   // the wave's units, for the pairs' other channels
-  // of a token: bytes from the pages' start to its row of head 0 of k and v, and to its exponents; -1: no page, -2: the row belongs to no sequence
+  // of a token: bytes from the pages' start to its row of head 0 of k and v (-1: no page, -2: the row belongs to no sequence), and to its exponents
   __shared__ int64_t code_at[kMaxTok][2], exp_at[kMaxTok][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int t0 = p.t0 + blockIdx.x * p.tok, dh = N ? N * V : a.head_dim, pairs = rk.rot >> 1;
-  const int tokens = a.tokens - t0;                         // of this workgroup and behind it
+  const int t0 = p.t0 + blockIdx.x * p.tok, tokens = min(p.tok, a.tokens - t0), pairs = rk.rot >> 1;
 
-  const int n = N ? N : dh / V, fit = 64 / n;               // lanes of a head, heads of a wave
-  const int sub = lane / n, u = lane - sub * n, c0 = u * V; // the lane's head of these, unit and first channel
+  const int dh = N ? N * V : a.head_dim, n = N ? N : dh / V, fit = 64 / n;   // channels and lanes of a head, heads of a step
+  const int sub = lane / n, u = lane - sub * n, c0 = u * V;                  // the lane's head of these, unit and first channel
   const HeadLanes<N> head{lane, u, n};
-  const int n_heads = a.n_heads, from_v = APPEND ? a.n_heads + a.kv_heads : 1 << 30;
-  const Walk walk(a.n_heads + (APPEND ? 2 : 1) * a.kv_heads, p.tok, fit);
-  Walk::At now = walk.first(wave, fit, sub);
-  // rows of the workgroup's first token, and elements from there: with more than one token to a workgroup the launch keeps them inside 32 bits
-  const T *const q = (const T *)a.q + t0 * a.ldq, *const k = (const T *)a.k + t0 * a.ldk, *const v = (const T *)a.v + t0 * a.ldv;
-  T *const q_out = (T *)a.q_out + t0 * a.ldqo, *const k_out = (T *)a.k_out + t0 * a.ldko;
-  const int ldq = (int)a.ldq, ldk = (int)a.ldk, ldv = (int)a.ldv, ldqo = (int)a.ldqo, ldko = (int)a.ldko;
-  const auto there = [&](const Walk::At &w) __attribute__((always_inline)) { return sub < fit && w.at < walk.steps && w.t < tokens; };
-  Unit<T> raw[DEPTH];
-  const auto load = [&](Walk::At w) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < DEPTH; ++j, walk.next(w)) {
-      const bool is_q = w.h < n_heads, is_v = w.h >= from_v;
-      const T *src = pick(is_q, q, pick(is_v, v, k));
-      const int h = w.h - pick(is_q, 0, pick(is_v, from_v, n_heads)), ld = pick(is_q, ldq, pick(is_v, ldv, ldk));
-#pragma unroll
-      for (int i = 0; i < Unit<T>::N; ++i) raw[j].w[i] = u32x4{0, 0, 0, 0};
-      if (there(w)) raw[j].load(src + (w.t * ld + h * dh + c0), a.once);
+  const int q_steps = (a.n_heads + fit - 1) / fit, k_steps = (a.kv_heads + fit - 1) / fit, steps = q_steps + (APPEND ? 2 : 1) * k_steps;
+  const int stride = gridDim.y * kWaves, stride_t = stride / steps, stride_g = stride - stride_t * steps;
+  const auto next = [&](Step &w) __attribute__((always_inline)) {
+    w.t += stride_t;
+    w.g += stride_g;
+    if (w.g >= steps) {
+      w.g -= steps;
+      ++w.t;
     }
   };
-  load(now);
+  // side 0 .. 2, first head, and the lanes that have one
+  struct Where {
+    int side, h0, lanes;
+  };
+  const auto where = [&](const Step &w) __attribute__((always_inline)) {
+    Where x;
+    x.side = w.g < q_steps ? 0 : !APPEND || w.g < q_steps + k_steps ? 1 : 2;
+    x.h0 = (w.g - (x.side == 0 ? 0 : x.side == 1 ? q_steps : q_steps + k_steps)) * fit;
+    x.lanes = min(fit, (x.side == 0 ? a.n_heads : a.kv_heads) - x.h0) * n;
+    return x;
+  };
+  const int from = blockIdx.y * kWaves + wave;
+  Step now{from / steps, from % steps}, ahead = now;
+  Unit<T> raw[DEPTH];
+  const auto load = [&](Unit<T> &to) __attribute__((always_inline)) {
+    if (ahead.t < tokens) {
+      const Where x = where(ahead);
+      const int64_t row = t0 + ahead.t;
+      const T *src = x.side == 0 ? (const T *)a.q + row * a.ldq : x.side == 1 ? (const T *)a.k + row * a.ldk : (const T *)a.v + row * a.ldv;
+      if (lane < x.lanes) to.load(src + x.h0 * dh + lane * V, a.once);
+    }
+    next(ahead);
+  };
+#pragma unroll
+  for (int j = 0; j < DEPTH; ++j) {
+#pragma unroll
+    for (int i = 0; i < Unit<T>::N; ++i) raw[j].w[i] = u32x4{0, 0, 0, 0};   // lanes without a head
+    load(raw[j]);
+  }
 
   // the norms' vectors, the lane's channels of them
-  const bool norms = a.norm[0].kind != PF_NORM_NONE || a.norm[1].kind != PF_NORM_NONE;
-  const bool layer = a.norm[0].kind == PF_NORM_LAYER || a.norm[1].kind == PF_NORM_LAYER;
-  const bool biased = a.norm[0].bias || a.norm[1].bias;
   Unit<T> weight[2], bias[2];
-  if (norms) {
-    float one[V], none[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) one[i] = 1.f, none[i] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      weight[i].round(one);
-      bias[i].round(none);
-      if (a.norm[i].weight) weight[i].load((const T *)a.norm[i].weight + c0, false);
-      if (a.norm[i].bias) bias[i].load((const T *)a.norm[i].bias + c0, false);
-    }
+  for (int i = 0; i < 2; ++i) {
+    if (a.norm[i].weight) weight[i].load((const T *)a.norm[i].weight + c0, false);
+    if (a.norm[i].bias) bias[i].load((const T *)a.norm[i].bias + c0, false);
   }
 
   // cosines and sines of the workgroup's tokens by channel
-  for (int e = tid; e < p.tok * pairs; e += 64 * kWaves) {
+  for (int e = tid; e < tokens * pairs; e += 64 * kWaves) {
     const int t = e / pairs, i = e - t * pairs;
-    if (t >= tokens) break;
     const int end0 = rk.axis_end[0], end1 = rk.axis_end[1];
     const int axis = (i >= end0) + (rk.n_axes > 1 && i >= end1);
     const double turns = (double)a.pos[(int64_t)(t0 + t) * rk.n_axes + axis] * rk.turns[i];
     float sn, c;
     sincospif(2.0f * (float)(turns - rint(turns)), &sn, &c);
-    const int from = pick(axis == 0, 0, pick(axis == 1, end0, end1)), w = pick(axis == 0, end0, pick(axis == 1, end1, rk.axis_end[2])) - from;
-    const int one = HALF ? 2 * from + (i - from) : 2 * i, two = HALF ? one + w : one + 1;
+    const int begin = pick(axis == 0, 0, pick(axis == 1, end0, end1)), w = pick(axis == 0, end0, pick(axis == 1, end1, rk.axis_end[2])) - begin;
+    const int one = HALF ? 2 * begin + (i - begin) : 2 * i, two = HALF ? one + w : one + 1;
     cosine[t][one] = cosine[t][two] = c * rk.magnitude;
     sine[t][one] = -sn * rk.magnitude;
     sine[t][two] = sn * rk.magnitude;
   }
   if constexpr (APPEND) {
-    for (int t = wave; t < p.tok; t += kWaves) {
-      int64_t page = -2;
-      int row = 0;
-      if (t < tokens) find_slot(a.pages, a.cu, a.first, a.n_seqs, t0 + t, lane, page, row);
+    for (int t = wave; t < tokens; t += kWaves) {
+      int64_t page;
+      int row;
+      find_slot(a.pages, a.cu, a.first, a.n_seqs, t0 + t, lane, page, row);
       if (lane == 0) {
         code_at[t][0] = page < 0 ? page : page * a.pages.k_stride + row * a.mx.row_bytes;
         code_at[t][1] = page < 0 ? page : page * a.pages.v_stride + row * a.mx.row_bytes;
@@ -296,127 +301,129 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
   __syncthreads();
 
   const float inv = 1.0f / (float)dh;
-  const int kind_q = a.norm[0].kind, kind_k = a.norm[1].kind;
-  const float eps_q = a.norm[0].eps, eps_k = a.norm[1].eps;
-  // where the pairs' other channels are, from the lane's own
-  int to[LAYOUT == TURN_HALVES_ANY ? V : 1];
+  // where the pairs' other channels are, from the lane's own, for GROUP neighbouring channels each
+  constexpr int GROUP = LAYOUT == TURN_HALVES ? 4 : 1;
+  int to[V / GROUP];
   if constexpr (HALF) {
 #pragma unroll
-    for (int i = 0; i < (LAYOUT == TURN_HALVES_ANY ? V : 1); ++i) {
-      const int c = c0 + i, e0 = 2 * rk.axis_end[0], e1 = rk.n_axes > 1 ? 2 * rk.axis_end[1] : rk.rot;
-      const int from = c < e0 ? 0 : c < e1 ? e0 : e1, end = c < e0 ? e0 : c < e1 ? e1 : rk.rot, w = (end - from) >> 1;
-      to[i] = c >= rk.rot ? 0 : c < from + w ? w : -w;
+    for (int i = 0; i < V / GROUP; ++i) {
+      const int c = c0 + i * GROUP, e0 = 2 * rk.axis_end[0], e1 = rk.n_axes > 1 ? 2 * rk.axis_end[1] : rk.rot;
+      const int begin = c < e0 ? 0 : c < e1 ? e0 : e1, end = c < e0 ? e0 : c < e1 ? e1 : rk.rot, w = (end - begin) >> 1;
+      to[i] = c >= rk.rot ? 0 : c < begin + w ? w : -w;
     }
   }
+  // the lane's bytes of codes and its block's exponent from its wave's first head on
+  constexpr int BYTES = APPEND ? V * Mx<APPEND ? FMT : 0>::BITS / 8 : 0;
+  const int code_off = APPEND ? (sub << a.pages.page_shift) * a.mx.row_bytes + u * BYTES : 0;
+  const int exp_off = APPEND ? (sub << a.pages.page_shift) * a.mx.blocks + u / 4 : 0;
 
-  const auto work = [&](const Walk::At &w, Unit<T> &unit) __attribute__((always_inline)) {
-    const bool is_q = w.h < n_heads, is_v = w.h >= from_v;
-    const int h = w.h - pick(is_q, 0, pick(is_v, from_v, n_heads));
-    const int t = min(w.t, kMaxTok - 1);
-    bool live = there(w);
-    int64_t at = 0;
+  const auto work = [&](const Step &w, Unit<T> &unit) __attribute__((always_inline)) {
+    const Where at = where(w);
+    const int64_t row = t0 + w.t;
+    int64_t codes = 0;
     if constexpr (APPEND) {   // rows that belong to no sequence stay as they are, in q_out too
-      at = code_at[t][is_v];
-      live = live && at >= (is_q ? -1 : 0);
+      codes = uniform64(code_at[w.t][at.side == 2]);
+      if (codes < (at.side == 0 ? -1 : 0)) return;
     }
-    float x[V];
+    if (at.side != 2) {
+      float x[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = unit[i];
-    if (norms) {
-      const int kind = pick(is_v, (int)PF_NORM_NONE, pick(is_q, kind_q, kind_k));
-      if (layer) {
-        float t1 = 0.f;
+      for (int i = 0; i < V; ++i) x[i] = unit[i];
+      const NormSide &norm = a.norm[at.side];
+      if (norm.kind != PF_NORM_NONE) {
+        if (norm.kind == PF_NORM_LAYER) {
+          float t1 = 0.f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) t1 += x[i];
-        float mean = head.sum(t1) * inv;
-        mean = kind == PF_NORM_LAYER ? mean : 0.f;
+          for (int i = 0; i < V; ++i) t1 += x[i];
+          const float mean = head.sum(t1) * inv;
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] -= mean;
+          for (int i = 0; i < V; ++i) x[i] -= mean;
+        }
+        float t2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) t2 = fmaf(x[i], x[i], t2);
+        const float r = inverse_root<T>(fmaf(head.sum(t2), inv, norm.eps));
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] *= r;
+        if (norm.weight) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) x[i] *= at.side == 0 ? weight[0][i] : weight[1][i];
+        }
+        if (norm.bias) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) x[i] += at.side == 0 ? bias[0][i] : bias[1][i];
+        }
       }
-      float t2 = 0.f;
+      if (rk.rot) {
+        float y[V], z[V];
+        if constexpr (HALF) {
+          float *mine = other[wave] + lane * V;     // a head's units are dh floats
 #pragma unroll
-      for (int i = 0; i < V; ++i) t2 = fmaf(x[i], x[i], t2);
-      float r = inverse_root<T>(fmaf(head.sum(t2), inv, pick(is_q, eps_q, eps_k)));
-      r = kind == PF_NORM_NONE ? 1.f : r;
-      Unit<T> g;
+          for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(mine + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+          __builtin_amdgcn_wave_barrier();
+          if (lane < fit * n) {                     // behind the last head there is no other channel
+            if constexpr (LAYOUT == TURN_HALVES) {
 #pragma unroll
-      for (int i = 0; i < Unit<T>::N; ++i) g.w[i] = pick(is_q, weight[0].w[i], weight[1].w[i]);
+              for (int i = 0; i < V; i += 4) {
+                const float4 o = *reinterpret_cast<const float4 *>(mine + i + to[i / 4]);
+                y[i] = o.x, y[i + 1] = o.y, y[i + 2] = o.z, y[i + 3] = o.w;
+              }
+            } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = x[i] * r * (is_v ? 1.f : g[i]);
-      if (biased) {
-#pragma unroll
-        for (int i = 0; i < Unit<T>::N; ++i) g.w[i] = pick(is_q, bias[0].w[i], bias[1].w[i]);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] += is_v ? 0.f : g[i];
-      }
-    }
-    if (rk.rot) {
-      float y[V], cs[V], sn[V];
-      if constexpr (HALF) {
-        float *mine = other[wave] + min(sub * dh + c0, 63 * V);
-#pragma unroll
-        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(mine + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-        __builtin_amdgcn_wave_barrier();
-        if constexpr (LAYOUT == TURN_HALVES) {
-#pragma unroll
-          for (int i = 0; i < V; i += 4) {
-            const float4 z = *reinterpret_cast<const float4 *>(mine + to[0] + i);
-            y[i] = z.x, y[i + 1] = z.y, y[i + 2] = z.z, y[i + 3] = z.w;
+              for (int i = 0; i < V; ++i) y[i] = mine[i + to[i]];
+            }
           }
+          __builtin_amdgcn_wave_barrier();
         } else {
 #pragma unroll
-          for (int i = 0; i < V; ++i) y[i] = mine[i + to[i]];
+          for (int i = 0; i < V; ++i) y[i] = x[i ^ 1];
         }
-        __builtin_amdgcn_wave_barrier();
-      } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = x[i ^ 1];
-      }
+        for (int i = 0; i < V; i += 4) {
+          const float4 c = *reinterpret_cast<const float4 *>(&cosine[w.t][c0 + i]), s = *reinterpret_cast<const float4 *>(&sine[w.t][c0 + i]);
+          z[i] = fmaf(x[i], c.x, y[i] * s.x);
+          z[i + 1] = fmaf(x[i + 1], c.y, y[i + 1] * s.y);
+          z[i + 2] = fmaf(x[i + 2], c.z, y[i + 2] * s.z);
+          z[i + 3] = fmaf(x[i + 3], c.w, y[i + 3] * s.w);
+        }
+        if (rk.rot == dh) {
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 z = *reinterpret_cast<const float4 *>(&cosine[t][c0 + i]), s = *reinterpret_cast<const float4 *>(&sine[t][c0 + i]);
-        cs[i] = z.x, cs[i + 1] = z.y, cs[i + 2] = z.z, cs[i + 3] = z.w;
-        sn[i] = s.x, sn[i + 1] = s.y, sn[i + 2] = s.z, sn[i + 3] = s.w;
-      }
-      const int end = is_v ? 0 : rk.rot;
+          for (int i = 0; i < V; ++i) x[i] = z[i];
+        } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float z = fmaf(x[i], cs[i], y[i] * sn[i]);
-        x[i] = c0 + i < end ? z : x[i];
+          for (int i = 0; i < V; ++i) x[i] = c0 + i < rk.rot ? z[i] : x[i];
+        }
       }
+      unit.round(x);   // to the rows' type, which is what the pages get too
     }
-    // rounded to the rows' type, which is what the pages get too
-    unit.round(x);
-    if (live && (!APPEND || is_q)) unit.store(pick(is_q, q_out, k_out) + (w.t * pick(is_q, ldqo, ldko) + h * dh + c0));
+    if (!APPEND || at.side == 0) {
+      T *dst = (at.side == 0 ? (T *)a.q_out + row * a.ldqo : (T *)a.k_out + row * a.ldko) + at.h0 * dh;
+      if (lane < at.lanes) unit.store(dst + lane * V);
+    }
     if constexpr (APPEND) {
-      unsigned most = 0;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        x[i] = unit[i];
-        most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-      }
-      most = head.block_max(most);
-      constexpr int BYTES = V * Mx<FMT>::BITS / 8;
-      unsigned code[BYTES / 4];
-      const unsigned byte = encode<FMT>(x, most, code);
-      if (!is_q && live) {
-        const int64_t rows = (int64_t)h << a.pages.page_shift;
-        uint8_t *to_row = pick(is_v, (uint8_t *)a.pages.v, (uint8_t *)a.pages.k) + (at + rows * a.mx.row_bytes);
-        if constexpr (BYTES == 8) *reinterpret_cast<u32x2 *>(to_row + u * BYTES) = u32x2{code[0], code[1]};
-        else *reinterpret_cast<unsigned *>(to_row + u * BYTES) = code[0];
-        if (u % 4 == 0) pick(is_v, a.mx.v_scale, a.mx.k_scale)[exp_at[t][is_v] + rows * a.mx.blocks + u / 4] = (uint8_t)byte;
-        if (u == n - 1)   // zeros up to whole 16 bytes: words, as head_dim is a multiple of 8
-          for (int b = n * BYTES; b < a.mx.row_bytes; b += 4) *reinterpret_cast<unsigned *>(to_row + b) = 0;
+      if (at.side == 0) return;
+      unsigned code[2];
+      const unsigned byte = mx_encode<FMT>(unit, head.block_max(unit.largest()), code);
+      if (lane < at.lanes) {
+        const int64_t rows = (int64_t)at.h0 << a.pages.page_shift;
+        uint8_t *to_row = (uint8_t *)(at.side == 2 ? a.pages.v : a.pages.k) + (codes + rows * a.mx.row_bytes) + code_off;
+        uint8_t *to_exp = (at.side == 2 ? a.mx.v_scale : a.mx.k_scale) + (uniform64(exp_at[w.t][at.side == 2]) + rows * a.mx.blocks) + exp_off;
+        if constexpr (BYTES == 8) *reinterpret_cast<u32x2 *>(to_row) = u32x2{code[0], code[1]};
+        else *reinterpret_cast<unsigned *>(to_row) = code[0];
+        if (u % 4 == 0) *to_exp = (uint8_t)byte;
+        if (N == 0 && u == n - 1)   // zeros up to whole 16 bytes: words, as head_dim is a multiple of 8
+          for (int b = n * BYTES; b < a.mx.row_bytes; b += 4) *reinterpret_cast<unsigned *>(to_row + (b - u * BYTES)) = 0;
       }
     }
   };
-  for (;;) {
+  while (now.t < tokens) {
 #pragma unroll
-    for (int j = 0; j < DEPTH; ++j, walk.next(now)) {
-      if (__builtin_amdgcn_readfirstlane(now.at - sub) >= walk.steps) return;
+    for (int j = 0; j < DEPTH; ++j) {
+      if (now.t >= tokens) break;
       work(now, raw[j]);
+      next(now);
+      load(raw[j]);
     }
-    load(now);
   }
 }
 
@@ -491,10 +498,9 @@ int split(int tokens, int parts) {
 
 template <typename T, int FMT, int LAYOUT, int N>
 hipError_t launch_heads(const TurnK &rk, HeadsK p, hipStream_t s) {
-  const int per_turn = 64 / (p.r.head_dim / V) * kWaves, heads = p.r.n_heads + (FMT >= 0 ? 2 : 1) * p.r.kv_heads;
-  const int64_t ld = std::max(std::max(std::max(p.r.ldq, p.r.ldqo), std::max(p.r.ldk, p.r.ldko)), p.r.ldv);
-  p.tok = p.r.tokens < 4096 || ld > INT32_MAX / kMaxTok / 2 ? 1 : std::min(std::max(kDepth<T> * per_turn / heads, 1), kMaxTok);
-  const int y = p.tok == 1 ? split(p.r.tokens, (heads + per_turn - 1) / per_turn) : 1;
+  const int fit = 64 / (p.r.head_dim / V), steps = (p.r.n_heads + fit - 1) / fit + (FMT >= 0 ? 2 : 1) * ((p.r.kv_heads + fit - 1) / fit);
+  p.tok = p.r.tokens < 4096 ? 1 : std::min(std::max((5 * kWaves + steps / 2) / steps, 1), kMaxTok);
+  const int y = p.tok == 1 ? split(p.r.tokens, (steps + kWaves - 1) / kWaves) : 1;
   hipError_t e = hipSuccess;
   for (p.t0 = 0; p.t0 < p.r.tokens && e == hipSuccess; p.t0 += kLaunchRows) {
     const int rows = std::min(p.r.tokens - p.t0, kLaunchRows);
@@ -512,7 +518,7 @@ hipError_t launch_lanes(const TurnK &rk, const HeadsK &p, hipStream_t s) {
 }
 template <typename T, int FMT>
 hipError_t launch_layout(const TurnK &rk, const HeadsK &p, bool half, int align, hipStream_t s) {
-  if (half && align % V) return launch_heads<T, FMT, TURN_HALVES_ANY, 0>(rk, p, s);
+  if (half && align % 4) return launch_heads<T, FMT, TURN_HALVES_ANY, 0>(rk, p, s);
   return half ? launch_lanes<T, FMT, TURN_HALVES>(rk, p, s) : launch_lanes<T, FMT, TURN_PAIRS>(rk, p, s);
 }
 template <typename T>
