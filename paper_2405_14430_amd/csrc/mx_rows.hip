@@ -15,7 +15,7 @@
 namespace pf {
 namespace {
 
-constexpr int kMaxPairs = PF_ROPE_MAX_PAIRS, kMaxDim = 128, kWaves = 4, kMaxTok = 8;
+constexpr int kMaxPairs = PF_ROPE_MAX_PAIRS, kMaxDim = 128, kWaves = 4;
 constexpr int V = 8;                                 // channels of a lane's unit
 enum { TURN_PAIRS, TURN_HALVES, TURN_HALVES_ANY };   // neighbours; an axis' half apart, the halves whole fours of channels or not
 
@@ -26,9 +26,25 @@ struct TurnK {
   int axis_end[PF_ROPE_MAX_AXES];   // running end of the axes, in pairs
 };
 
+// The rows of q, k or v.
+struct SideK {
+  const void *src;
+  void *dst;             // rows, or the first page of codes
+  uint8_t *exp;          // the first page of exponents
+  int64_t ld, ldo;
+  const void *weight, *bias;
+  int kind;
+  float eps;
+  int heads, steps;      // steps of a token
+};
 struct HeadsK {
-  HeadRows r;
-  int tok;               // tokens of a workgroup
+  SideK side[3];
+  int64_t code_stride[2], exp_stride[2];   // of the pages of k and v
+  const int32_t *pos;
+  Pages pages;
+  const int32_t *cu, *first;
+  int n_seqs, row_bytes, blocks;
+  int tokens, head_dim, once;
   int t0;                // first token of the launch
 };
 
@@ -178,16 +194,17 @@ struct Walk {
   }
 };
 
-// A number that all lanes agree on, in scalar registers.
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-  return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v));
-}
-
-// Where packed row `row` of a call goes in the pages: page (-1: none, -2: the row belongs to no sequence) and row of the page.
-__device__ __forceinline__ void find_slot(const Pages &pages, const int32_t *cu, const int32_t *first, int n_seqs, int row, int lane, int64_t &page, int &in_page) {
+// Where packed row `row` of a call (one that all lanes agree on) goes in the pages: page (-1: none, -2: the row belongs to no sequence) and row
+// of the page.  All loads are the scalar unit's: the vector unit's come back in order, so that one behind the rows' would wait for them.
+__device__ __forceinline__ void find_slot(const Pages &pages, const int32_t *cu, const int32_t *first, int n_seqs, int row, int64_t &page, int &in_page) {
   page = -2;
   in_page = 0;
-  const int s = wave_search(n_seqs, lane, row, [&](int i) { return cu[i]; });
+  int s = -1;                                 // the largest in [0, n_seqs] with cu[s] <= row
+  for (int past = n_seqs + 1; past - s > 1;) {
+    const int mid = (s + past) >> 1;
+    if (cu[mid] <= row) s = mid;
+    else past = mid;
+  }
   if (s < 0 || s >= n_seqs) return;
   page = -1;
   const int64_t slot = (int64_t)first[s] + ((int64_t)row - cu[s]);
@@ -200,106 +217,91 @@ __device__ __forceinline__ void find_slot(const Pages &pages, const int32_t *cu,
 
 // FMT < 0: q and k rows to rows; else k and v into pages.  LAYOUT: of the pairs.  N: lanes of a head (0: any number).
 //
-// A step of a wave is up to `fit` neighbouring heads of one side (q, k or v) of one token, so that all but the channels' own work is the scalar unit's;
-// a token's steps come side after side, and the waves of a workgroup take the steps of its tok tokens in turn.  The rows of the next kDepth
-// steps are on their way meanwhile, the first ones before the tables are worked out.
-template <typename T> constexpr int kDepth = 2;
-struct Step {
-  int t, g;              // token of the workgroup, step of the token
-};
+// A wave takes a token, or a share of its heads (gridDim.y shares): its 64 lanes work out the cosines and sines of up to 64 pairs and find the
+// token's slot, then it goes over the heads, side after side (q, k, v), `fit` of them at a step.  A lane has the same channels of every head it
+// meets, so their cosines, sines and weights stay in registers.  The rows of kDepth steps are loaded together, the first ones before
+// all else; what hides a wave's waiting is the other waves, which it has nothing to do with.
+template <typename T> constexpr int kDepth = sizeof(T) == 2 ? 4 : 3;
 template <typename T, int FMT, int LAYOUT, int N>
 __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK p) {
 #pragma clang fp contract(off)   // the same rows from all instances: pages get what pf_op_qk_norm_rope gives
   constexpr bool APPEND = FMT >= 0, HALF = LAYOUT != TURN_PAIRS;
   constexpr int DEPTH = kDepth<T>;
-  const HeadRows &a = p.r;
-  __shared__ __attribute__((aligned(16))) float cosine[kMaxTok][kMaxDim], sine[kMaxTok][kMaxDim];
+  __shared__ __attribute__((aligned(16))) float table[kWaves][2][kMaxDim];                      // cosines and sines by channel
   __shared__ __attribute__((aligned(16))) float other[HALF ? kWaves : 1][HALF ? 64 * V : 1];   // the wave's units, for the pairs' other channels
-  // of a token: bytes from the pages' start to its row of head 0 of k and v (-1: no page, -2: the row belongs to no sequence), and to its exponents
-  __shared__ int64_t code_at[kMaxTok][2], exp_at[kMaxTok][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int t0 = p.t0 + blockIdx.x * p.tok, tokens = min(p.tok, a.tokens - t0), pairs = rk.rot >> 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int token = p.t0 + blockIdx.x * kWaves + wave;
+  if (token >= p.tokens) return;
 
-  const int dh = N ? N * V : a.head_dim, n = N ? N : dh / V, fit = 64 / n;   // channels and lanes of a head, heads of a step
+  const int dh = N ? N * V : p.head_dim, n = N ? N : dh / V, fit = 64 / n;   // channels and lanes of a head, heads of a step
   const int sub = lane / n, u = lane - sub * n, c0 = u * V;                  // the lane's head of these, unit and first channel
   const HeadLanes<N> head{lane, u, n};
-  const int q_steps = (a.n_heads + fit - 1) / fit, k_steps = (a.kv_heads + fit - 1) / fit, steps = q_steps + (APPEND ? 2 : 1) * k_steps;
-  const int stride = gridDim.y * kWaves, stride_t = stride / steps, stride_g = stride - stride_t * steps;
-  const auto next = [&](Step &w) __attribute__((always_inline)) {
-    w.t += stride_t;
-    w.g += stride_g;
-    if (w.g >= steps) {
-      w.g -= steps;
-      ++w.t;
-    }
-  };
-  // side 0 .. 2, first head, and the lanes that have one
+  const int q_steps = p.side[0].steps, k_steps = p.side[1].steps, steps = q_steps + (APPEND ? 2 : 1) * k_steps;
+  const int stride = gridDim.y;
+  const T *const q = (const T *)p.side[0].src + token * p.side[0].ld, *const k = (const T *)p.side[1].src + token * p.side[1].ld;
+  const T *const v = (const T *)p.side[2].src + token * p.side[2].ld;
+  // of step i: side, first head, lanes that have a head
   struct Where {
     int side, h0, lanes;
   };
-  const auto where = [&](const Step &w) __attribute__((always_inline)) {
+  const auto where = [&](int i) __attribute__((always_inline)) {
     Where x;
-    x.side = w.g < q_steps ? 0 : !APPEND || w.g < q_steps + k_steps ? 1 : 2;
-    x.h0 = (w.g - (x.side == 0 ? 0 : x.side == 1 ? q_steps : q_steps + k_steps)) * fit;
-    x.lanes = min(fit, (x.side == 0 ? a.n_heads : a.kv_heads) - x.h0) * n;
+    x.side = i < q_steps ? 0 : !APPEND || i < q_steps + k_steps ? 1 : 2;
+    x.h0 = (i - (x.side == 0 ? 0 : x.side == 1 ? q_steps : q_steps + k_steps)) * fit;
+    x.lanes = min(fit, pick(x.side == 0, p.side[0].heads, p.side[1].heads) - x.h0) * n;
     return x;
   };
-  const int from = blockIdx.y * kWaves + wave;
-  Step now{from / steps, from % steps}, ahead = now;
-  Unit<T> raw[DEPTH];
-  const auto load = [&](Unit<T> &to) __attribute__((always_inline)) {
-    if (ahead.t < tokens) {
-      const Where x = where(ahead);
-      const int64_t row = t0 + ahead.t;
-      const T *src = x.side == 0 ? (const T *)a.q + row * a.ldq : x.side == 1 ? (const T *)a.k + row * a.ldk : (const T *)a.v + row * a.ldv;
-      if (lane < x.lanes) to.load(src + x.h0 * dh + lane * V, a.once);
-    }
-    next(ahead);
-  };
-#pragma unroll
-  for (int j = 0; j < DEPTH; ++j) {
-#pragma unroll
-    for (int i = 0; i < Unit<T>::N; ++i) raw[j].w[i] = u32x4{0, 0, 0, 0};   // lanes without a head
-    load(raw[j]);
-  }
-
-  // the norms' vectors, the lane's channels of them
-  Unit<T> weight[2], bias[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (a.norm[i].weight) weight[i].load((const T *)a.norm[i].weight + c0, false);
-    if (a.norm[i].bias) bias[i].load((const T *)a.norm[i].bias + c0, false);
-  }
-
-  // cosines and sines of the workgroup's tokens by channel
-  for (int e = tid; e < tokens * pairs; e += 64 * kWaves) {
-    const int t = e / pairs, i = e - t * pairs;
-    const int end0 = rk.axis_end[0], end1 = rk.axis_end[1];
-    const int axis = (i >= end0) + (rk.n_axes > 1 && i >= end1);
-    const double turns = (double)a.pos[(int64_t)(t0 + t) * rk.n_axes + axis] * rk.turns[i];
-    float sn, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &c);
-    const int begin = pick(axis == 0, 0, pick(axis == 1, end0, end1)), w = pick(axis == 0, end0, pick(axis == 1, end1, rk.axis_end[2])) - begin;
-    const int one = HALF ? 2 * begin + (i - begin) : 2 * i, two = HALF ? one + w : one + 1;
-    cosine[t][one] = cosine[t][two] = c * rk.magnitude;
-    sine[t][one] = -sn * rk.magnitude;
-    sine[t][two] = sn * rk.magnitude;
-  }
+  int64_t page = 0;
+  int in_page = 0;
   if constexpr (APPEND) {
-    for (int t = wave; t < tokens; t += kWaves) {
-      int64_t page;
-      int row;
-      find_slot(a.pages, a.cu, a.first, a.n_seqs, t0 + t, lane, page, row);
-      if (lane == 0) {
-        code_at[t][0] = page < 0 ? page : page * a.pages.k_stride + row * a.mx.row_bytes;
-        code_at[t][1] = page < 0 ? page : page * a.pages.v_stride + row * a.mx.row_bytes;
-        exp_at[t][0] = page * a.mx.k_scale_stride + row * a.mx.blocks;
-        exp_at[t][1] = page * a.mx.v_scale_stride + row * a.mx.blocks;
-      }
+    find_slot(p.pages, p.cu, p.first, p.n_seqs, token, page, in_page);
+    if (page == -2) return;           // rows that belong to no sequence stay as they are, in q_out too
+  }
+  Unit<T> raw[DEPTH];
+#pragma unroll
+  for (int j = 0; j < DEPTH; ++j)
+#pragma unroll
+    for (int i = 0; i < Unit<T>::N; ++i) {
+      raw[j].w[i] = u32x4{0, 0, 0, 0};                      // lanes without a head
+      asm volatile("" : "+v"(raw[j].w[i]));                 // four registers that stay together
+    }
+  const auto load = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < DEPTH; ++j, i += stride) {
+      if (i >= steps) break;
+      const Where at = where(i);
+      if (lane < at.lanes) raw[j].load(pick(at.side == 0, q, pick(at.side == 1, k, v)) + at.h0 * dh + lane * V, p.once);
+    }
+  };
+  load(blockIdx.y);
+  Unit<T> weight[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (p.side[i].weight) weight[i].load((const T *)p.side[i].weight + c0, false);
+
+  // the token's cosines and sines, a lane to a pair, and from there to the lanes of its channels
+  float cs[V], sn[V];
+  if (rk.rot) {
+    if (2 * lane < rk.rot) {
+      const int end0 = rk.axis_end[0], end1 = rk.axis_end[1];
+      const int axis = (lane >= end0) + (rk.n_axes > 1 && lane >= end1);
+      const double turns = (double)p.pos[(int64_t)token * rk.n_axes + axis] * rk.turns[lane];
+      float s, c;
+      sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+      const int begin = pick(axis == 0, 0, pick(axis == 1, end0, end1)), w = pick(axis == 0, end0, pick(axis == 1, end1, rk.axis_end[2])) - begin;
+      const int one = HALF ? 2 * begin + (lane - begin) : 2 * lane, two = HALF ? one + w : one + 1;
+      table[wave][0][one] = table[wave][0][two] = c * rk.magnitude;
+      table[wave][1][one] = -s * rk.magnitude;
+      table[wave][1][two] = s * rk.magnitude;
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int c = 0; c < V; c += 4) {
+      const float4 x = *reinterpret_cast<const float4 *>(&table[wave][0][c0 + c]), y = *reinterpret_cast<const float4 *>(&table[wave][1][c0 + c]);
+      cs[c] = x.x, cs[c + 1] = x.y, cs[c + 2] = x.z, cs[c + 3] = x.w;
+      sn[c] = y.x, sn[c + 1] = y.y, sn[c + 2] = y.z, sn[c + 3] = y.w;
     }
   }
-  __syncthreads();
-
   const float inv = 1.0f / (float)dh;
   // where the pairs' other channels are, from the lane's own, for GROUP neighbouring channels each
   constexpr int GROUP = LAYOUT == TURN_HALVES ? 4 : 1;
@@ -312,118 +314,120 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
       to[i] = c >= rk.rot ? 0 : c < begin + w ? w : -w;
     }
   }
-  // the lane's bytes of codes and its block's exponent from its wave's first head on
+  // the lane's bytes of codes and its block's exponent from a step's first head on
   constexpr int BYTES = APPEND ? V * Mx<APPEND ? FMT : 0>::BITS / 8 : 0;
-  const int code_off = APPEND ? (sub << a.pages.page_shift) * a.mx.row_bytes + u * BYTES : 0;
-  const int exp_off = APPEND ? (sub << a.pages.page_shift) * a.mx.blocks + u / 4 : 0;
+  const int code_off = APPEND ? (sub << p.pages.page_shift) * p.row_bytes + u * BYTES : 0;
+  const int exp_off = APPEND ? (sub << p.pages.page_shift) * p.blocks + u / 4 : 0;
 
-  const auto work = [&](const Step &w, Unit<T> &unit) __attribute__((always_inline)) {
-    const Where at = where(w);
-    const int64_t row = t0 + w.t;
-    int64_t codes = 0;
-    if constexpr (APPEND) {   // rows that belong to no sequence stay as they are, in q_out too
-      codes = uniform64(code_at[w.t][at.side == 2]);
-      if (codes < (at.side == 0 ? -1 : 0)) return;
-    }
-    if (at.side != 2) {
-      float x[V];
+  for (int i0 = blockIdx.y;;) {
+    // all rows are waited for here: in front of a later step the wait would be one for the stores of the step before, too
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = unit[i];
-      const NormSide &norm = a.norm[at.side];
-      if (norm.kind != PF_NORM_NONE) {
-        if (norm.kind == PF_NORM_LAYER) {
-          float t1 = 0.f;
+    for (int j = 0; j < DEPTH; ++j)
 #pragma unroll
-          for (int i = 0; i < V; ++i) t1 += x[i];
-          const float mean = head.sum(t1) * inv;
-#pragma unroll
-          for (int i = 0; i < V; ++i) x[i] -= mean;
-        }
-        float t2 = 0.f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) t2 = fmaf(x[i], x[i], t2);
-        const float r = inverse_root<T>(fmaf(head.sum(t2), inv, norm.eps));
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] *= r;
-        if (norm.weight) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) x[i] *= at.side == 0 ? weight[0][i] : weight[1][i];
-        }
-        if (norm.bias) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) x[i] += at.side == 0 ? bias[0][i] : bias[1][i];
-        }
-      }
-      if (rk.rot) {
-        float y[V], z[V];
-        if constexpr (HALF) {
-          float *mine = other[wave] + lane * V;     // a head's units are dh floats
-#pragma unroll
-          for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(mine + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-          __builtin_amdgcn_wave_barrier();
-          if (lane < fit * n) {                     // behind the last head there is no other channel
-            if constexpr (LAYOUT == TURN_HALVES) {
-#pragma unroll
-              for (int i = 0; i < V; i += 4) {
-                const float4 o = *reinterpret_cast<const float4 *>(mine + i + to[i / 4]);
-                y[i] = o.x, y[i + 1] = o.y, y[i + 2] = o.z, y[i + 3] = o.w;
-              }
-            } else {
-#pragma unroll
-              for (int i = 0; i < V; ++i) y[i] = mine[i + to[i]];
-            }
-          }
-          __builtin_amdgcn_wave_barrier();
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) y[i] = x[i ^ 1];
-        }
-#pragma unroll
-        for (int i = 0; i < V; i += 4) {
-          const float4 c = *reinterpret_cast<const float4 *>(&cosine[w.t][c0 + i]), s = *reinterpret_cast<const float4 *>(&sine[w.t][c0 + i]);
-          z[i] = fmaf(x[i], c.x, y[i] * s.x);
-          z[i + 1] = fmaf(x[i + 1], c.y, y[i + 1] * s.y);
-          z[i + 2] = fmaf(x[i + 2], c.z, y[i + 2] * s.z);
-          z[i + 3] = fmaf(x[i + 3], c.w, y[i + 3] * s.w);
-        }
-        if (rk.rot == dh) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) x[i] = z[i];
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) x[i] = c0 + i < rk.rot ? z[i] : x[i];
-        }
-      }
-      unit.round(x);   // to the rows' type, which is what the pages get too
-    }
-    if (!APPEND || at.side == 0) {
-      T *dst = (at.side == 0 ? (T *)a.q_out + row * a.ldqo : (T *)a.k_out + row * a.ldko) + at.h0 * dh;
-      if (lane < at.lanes) unit.store(dst + lane * V);
-    }
-    if constexpr (APPEND) {
-      if (at.side == 0) return;
-      unsigned code[2];
-      const unsigned byte = mx_encode<FMT>(unit, head.block_max(unit.largest()), code);
-      if (lane < at.lanes) {
-        const int64_t rows = (int64_t)at.h0 << a.pages.page_shift;
-        uint8_t *to_row = (uint8_t *)(at.side == 2 ? a.pages.v : a.pages.k) + (codes + rows * a.mx.row_bytes) + code_off;
-        uint8_t *to_exp = (at.side == 2 ? a.mx.v_scale : a.mx.k_scale) + (uniform64(exp_at[w.t][at.side == 2]) + rows * a.mx.blocks) + exp_off;
-        if constexpr (BYTES == 8) *reinterpret_cast<u32x2 *>(to_row) = u32x2{code[0], code[1]};
-        else *reinterpret_cast<unsigned *>(to_row) = code[0];
-        if (u % 4 == 0) *to_exp = (uint8_t)byte;
-        if (N == 0 && u == n - 1)   // zeros up to whole 16 bytes: words, as head_dim is a multiple of 8
-          for (int b = n * BYTES; b < a.mx.row_bytes; b += 4) *reinterpret_cast<unsigned *>(to_row + (b - u * BYTES)) = 0;
-      }
-    }
-  };
-  while (now.t < tokens) {
+      for (int c = 0; c < Unit<T>::N; ++c) asm volatile("" : "+v"(raw[j].w[c]));
 #pragma unroll
     for (int j = 0; j < DEPTH; ++j) {
-      if (now.t >= tokens) break;
-      work(now, raw[j]);
-      next(now);
-      load(raw[j]);
+      const int i = i0 + j * stride;
+      if (i >= steps) break;
+      const Where at = where(i);
+      if (APPEND && at.side != 0 && page < 0) break;
+      Unit<T> &unit = raw[j];
+      if (at.side != 2) {
+        float x[V];
+#pragma unroll
+        for (int c = 0; c < V; ++c) x[c] = unit[c];
+        const bool is_q = at.side == 0;
+        const int kind = pick(is_q, p.side[0].kind, p.side[1].kind);
+        const float eps = pick(is_q, p.side[0].eps, p.side[1].eps);
+        const T *const w = (const T *)pick(is_q, p.side[0].weight, p.side[1].weight), *const b = (const T *)pick(is_q, p.side[0].bias, p.side[1].bias);
+        if (kind != PF_NORM_NONE) {
+          if (kind == PF_NORM_LAYER) {
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < V; ++c) sum += x[c];
+            const float mean = head.sum(sum) * inv;
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[c] -= mean;
+          }
+          float sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < V; ++c) sum = fmaf(x[c], x[c], sum);
+          const float r = inverse_root<T>(fmaf(head.sum(sum), inv, eps));
+#pragma unroll
+          for (int c = 0; c < V; ++c) x[c] *= r;
+          if (w) {
+            Unit<T> g;
+#pragma unroll
+            for (int c = 0; c < Unit<T>::N; ++c) g.w[c] = pick(is_q, weight[0].w[c], weight[1].w[c]);
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[c] *= g[c];
+          }
+          if (b) {
+            Unit<T> bias;
+            bias.load(b + c0, false);
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[c] += bias[c];
+          }
+        }
+        if (rk.rot) {
+          float y[V], z[V];
+          if constexpr (HALF) {
+            float *mine = other[wave] + lane * V;     // a head's units are dh floats
+#pragma unroll
+            for (int c = 0; c < V; c += 4) *reinterpret_cast<float4 *>(mine + c) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
+            __builtin_amdgcn_wave_barrier();
+            if (lane < fit * n) {                     // behind the last head there is no other channel
+              if constexpr (LAYOUT == TURN_HALVES) {
+#pragma unroll
+                for (int c = 0; c < V; c += 4) {
+                  const float4 o = *reinterpret_cast<const float4 *>(mine + c + to[c / 4]);
+                  y[c] = o.x, y[c + 1] = o.y, y[c + 2] = o.z, y[c + 3] = o.w;
+                }
+              } else {
+#pragma unroll
+                for (int c = 0; c < V; ++c) y[c] = mine[c + to[c]];
+              }
+            }
+            __builtin_amdgcn_wave_barrier();
+          } else {
+#pragma unroll
+            for (int c = 0; c < V; ++c) y[c] = x[c ^ 1];
+          }
+#pragma unroll
+          for (int c = 0; c < V; ++c) z[c] = fmaf(x[c], cs[c], y[c] * sn[c]);
+          if (rk.rot == dh) {
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[c] = z[c];
+          } else {
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[c] = c0 + c < rk.rot ? z[c] : x[c];
+          }
+        }
+        unit.round(x);   // to the rows' type, which is what the pages get too
+      }
+      if (!APPEND || at.side == 0) {
+        const bool is_q = at.side == 0;
+        T *dst = (T *)pick(is_q, p.side[0].dst, p.side[1].dst) + token * pick(is_q, p.side[0].ldo, p.side[1].ldo) + at.h0 * dh;
+        if (lane < at.lanes) unit.store(dst + lane * V);
+      } else if constexpr (APPEND) {
+        unsigned code[2];
+        const unsigned byte = mx_encode<FMT>(unit, head.block_max(unit.largest()), code);
+        if (lane < at.lanes) {
+          const bool is_v = at.side == 2;
+          const int64_t row = ((int64_t)at.h0 << p.pages.page_shift) + in_page;
+          uint8_t *to_row = (uint8_t *)pick(is_v, p.side[2].dst, p.side[1].dst) + (page * pick(is_v, p.code_stride[1], p.code_stride[0]) + row * p.row_bytes) + code_off;
+          uint8_t *to_exp = pick(is_v, p.side[2].exp, p.side[1].exp) + (page * pick(is_v, p.exp_stride[1], p.exp_stride[0]) + row * p.blocks) + exp_off;
+          if constexpr (BYTES == 8) *reinterpret_cast<u32x2 *>(to_row) = u32x2{code[0], code[1]};
+          else *reinterpret_cast<unsigned *>(to_row) = code[0];
+          if (u % 4 == 0) *to_exp = (uint8_t)byte;
+          if (N == 0 && u == n - 1)   // zeros up to whole 16 bytes: words, as head_dim is a multiple of 8
+            for (int b = n * BYTES; b < p.row_bytes; b += 4) *reinterpret_cast<unsigned *>(to_row + (b - u * BYTES)) = 0;
+        }
+      }
     }
+    i0 += DEPTH * stride;
+    if (i0 >= steps) return;
+    load(i0);
   }
 }
 
@@ -444,7 +448,7 @@ __global__ __launch_bounds__(64 * kWaves) void mx_read_kernel(ReadK p) {
   for (int t = wave; t < p.tok; t += kWaves) {
     int64_t page = -2;
     int in_page = 0;
-    if (t0 + t < a.tokens) find_slot(a.pages, a.cu, a.first, a.n_seqs, t0 + t, lane, page, in_page);
+    if (t0 + t < a.tokens) find_slot(a.pages, a.cu, a.first, a.n_seqs, t0 + t, page, in_page);
     if (lane == 0) {
       page_of[t] = page;
       row_of[t] = in_page;
@@ -498,13 +502,13 @@ int split(int tokens, int parts) {
 
 template <typename T, int FMT, int LAYOUT, int N>
 hipError_t launch_heads(const TurnK &rk, HeadsK p, hipStream_t s) {
-  const int fit = 64 / (p.r.head_dim / V), steps = (p.r.n_heads + fit - 1) / fit + (FMT >= 0 ? 2 : 1) * ((p.r.kv_heads + fit - 1) / fit);
-  p.tok = p.r.tokens < 4096 ? 1 : std::min(std::max((5 * kWaves + steps / 2) / steps, 1), kMaxTok);
-  const int y = p.tok == 1 ? split(p.r.tokens, (steps + kWaves - 1) / kWaves) : 1;
+  int steps = 0;         // of a token
+  for (const SideK &side : p.side) steps += side.steps;
+  const int y = split(p.tokens, steps);
   hipError_t e = hipSuccess;
-  for (p.t0 = 0; p.t0 < p.r.tokens && e == hipSuccess; p.t0 += kLaunchRows) {
-    const int rows = std::min(p.r.tokens - p.t0, kLaunchRows);
-    head_rows_kernel<T, FMT, LAYOUT, N><<<dim3((rows + p.tok - 1) / p.tok, y), 64 * kWaves, 0, s>>>(rk, p);
+  for (p.t0 = 0; p.t0 < p.tokens && e == hipSuccess; p.t0 += kLaunchRows) {
+    const int rows = std::min(p.tokens - p.t0, kLaunchRows);
+    head_rows_kernel<T, FMT, LAYOUT, N><<<dim3((rows + kWaves - 1) / kWaves, y), 64 * kWaves, 0, s>>>(rk, p);
     e = hipGetLastError();
   }
   return e;
@@ -512,8 +516,8 @@ hipError_t launch_heads(const TurnK &rk, HeadsK p, hipStream_t s) {
 
 template <typename T, int FMT, int LAYOUT>
 hipError_t launch_lanes(const TurnK &rk, const HeadsK &p, hipStream_t s) {
-  if (p.r.head_dim == 128) return launch_heads<T, FMT, LAYOUT, 16>(rk, p, s);
-  if (p.r.head_dim == 64) return launch_heads<T, FMT, LAYOUT, 8>(rk, p, s);
+  if (p.head_dim == 128) return launch_heads<T, FMT, LAYOUT, 16>(rk, p, s);
+  if (p.head_dim == 64) return launch_heads<T, FMT, LAYOUT, 8>(rk, p, s);
   return launch_heads<T, FMT, LAYOUT, 0>(rk, p, s);
 }
 template <typename T, int FMT>
@@ -522,9 +526,9 @@ hipError_t launch_layout(const TurnK &rk, const HeadsK &p, bool half, int align,
   return half ? launch_lanes<T, FMT, TURN_HALVES>(rk, p, s) : launch_lanes<T, FMT, TURN_PAIRS>(rk, p, s);
 }
 template <typename T>
-hipError_t launch_format(const TurnK &rk, const HeadsK &p, bool half, int align, hipStream_t s) {
-  if (!p.r.n_seqs) return launch_layout<T, -1>(rk, p, half, align, s);
-  return p.r.mx.format == PF_MX_E4M3 ? launch_layout<T, PF_MX_E4M3>(rk, p, half, align, s) : launch_layout<T, PF_MX_E2M1>(rk, p, half, align, s);
+hipError_t launch_format(const TurnK &rk, const HeadsK &p, int format, bool half, int align, hipStream_t s) {
+  if (format < 0) return launch_layout<T, -1>(rk, p, half, align, s);
+  return format == PF_MX_E4M3 ? launch_layout<T, PF_MX_E4M3>(rk, p, half, align, s) : launch_layout<T, PF_MX_E2M1>(rk, p, half, align, s);
 }
 
 template <typename T, int FMT>
@@ -562,9 +566,22 @@ hipError_t launch_head_rows(const HeadRows &args, const pf_rope *rope, hipStream
     for (int i = 0; i < end; ++i) rk.turns[i] = rope->turns[i];
     half = rope->layout == PF_ROPE_HALF;
   }
-  HeadsK p{args, 1, 0};
-  p.r.once = (int64_t)args.tokens * 2 * (args.n_heads + 2 * args.kv_heads) * args.head_dim * (int64_t)dt_size(args.dt) > kReadOnceBytes;
-  return args.dt == DT_BF16 ? launch_format<bf16_t>(rk, p, half, align, s) : launch_format<float>(rk, p, half, align, s);
+  const bool append = args.n_seqs > 0;
+  const int fit = 64 / (args.head_dim / V);
+  const auto side = [&](const void *src, int64_t ld, void *dst, int64_t ldo, uint8_t *exp, const NormSide &n, int heads) {
+    return SideK{src, dst, exp, ld, ldo, n.weight, n.bias, n.kind, n.eps, heads, (heads + fit - 1) / fit};
+  };
+  HeadsK p{};
+  p.side[0] = side(args.q, args.ldq, args.q_out, args.ldqo, nullptr, args.norm[0], args.n_heads);
+  p.side[1] = side(args.k, args.ldk, append ? args.pages.k : args.k_out, args.ldko, args.mx.k_scale, args.norm[1], args.kv_heads);
+  if (append) p.side[2] = side(args.v, args.ldv, args.pages.v, 0, args.mx.v_scale, NormSide{}, args.kv_heads);
+  p.code_stride[0] = args.pages.k_stride, p.code_stride[1] = args.pages.v_stride;
+  p.exp_stride[0] = args.mx.k_scale_stride, p.exp_stride[1] = args.mx.v_scale_stride;
+  p.pos = args.pos, p.pages = args.pages, p.cu = args.cu, p.first = args.first, p.n_seqs = args.n_seqs;
+  p.row_bytes = args.mx.row_bytes, p.blocks = args.mx.blocks, p.tokens = args.tokens, p.head_dim = args.head_dim;
+  p.once = (int64_t)args.tokens * 2 * (args.n_heads + 2 * args.kv_heads) * args.head_dim * (int64_t)dt_size(args.dt) > kReadOnceBytes;
+  const int format = append ? args.mx.format : -1;
+  return args.dt == DT_BF16 ? launch_format<bf16_t>(rk, p, format, half, align, s) : launch_format<float>(rk, p, format, half, align, s);
 }
 
 hipError_t launch_mx_read(const MxRead &r, hipStream_t s) {

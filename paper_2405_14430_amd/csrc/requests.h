@@ -108,7 +108,6 @@ struct HeadRows {
   MxPages mx;
   const int32_t *cu, *first;
   int n_seqs;              // 0: no pages
-  bool once;               // rows are read with non-temporal loads (set at the launch)
 };
 hipError_t launch_head_rows(const HeadRows &a, const pf_rope *rope, hipStream_t s);
 
