@@ -112,6 +112,7 @@ struct RowsKernelArgs {
   int group;        // query heads per key head
   int slots;        // row tiles the grid has per key head
   float sl2;        // scale * log2(e)
+  int most_items;   // few kernel: more are not worked on (its slots: workgroups per key head)
 };
 
 template <typename T, int DHP, int NW_, int KW_>

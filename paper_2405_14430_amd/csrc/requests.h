@@ -139,9 +139,10 @@ struct RowsAttn {
   float *ws;
   int shape, splits, least_keys;       // of the plan
 };
-enum { ROWS_TILES, ROWS_WIDE, ROWS_KEYS };   // kernels of attn_rows.hip
+enum { ROWS_TILES, ROWS_WIDE, ROWS_KEYS, ROWS_FEW };   // kernels of attn_rows.h; the last one of attn_rows_mx.hip
 struct RowsPlan { int shape, splits, least_keys; size_t ws_bytes; };   // splits: chunks of the keys, none smaller than least_keys
 RowsPlan rows_attention_plan(int dt, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv);
+RowsPlan mx_attention_plan(int dt, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv);
 hipError_t launch_rows_attention(const RowsAttn &a, hipStream_t s);
 hipError_t launch_mx_attention(const RowsAttn &a, hipStream_t s);
 hipError_t launch_rows_join(const RowsAttn &a, hipStream_t s);   // of the partial results in a.ws

@@ -194,21 +194,30 @@ pf_status pf_op_kv_append(int dtype, const pf_kv_pages *pages, const void *k, in
   return launched(launch_rope_rows(a, (hipStream_t)stream), "pf_op_kv_append");
 }
 
+// whether an attention launch of these sizes is planned at all
+static bool rows_sizes_ok(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
+  return dt_ok(dtype) && total_q >= 1 && n_seqs >= 1 && head_ok(head_dim) && heads_ok(total_q, n_heads, kv_heads) && max_kv >= 1 && max_kv <= kMaxKeys;
+}
+static const char *rows_kernel_name(const RowsPlan &p, int dtype, int head_dim) {
+  static thread_local char name[64];
+  const int dim = head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128;
+  if (p.shape == ROWS_FEW) snprintf(name, sizeof(name), "attn_rows_few_kernel<%d>", dim);
+  else if (p.shape == ROWS_WIDE) snprintf(name, sizeof(name), "attn_rows_wide_kernel<%d,%d>", dim, head_dim <= 80 && dim == 96 ? 5 : dim / 16);
+  else snprintf(name, sizeof(name), "attn_rows_kernel<%s,%d,%s>", dtype == PF_BF16 ? "bf16" : "float", dim, p.shape == ROWS_KEYS ? "1,4" : "4,1");
+  return name;
+}
+
 size_t pf_op_attention_rows_ws_bytes(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
-  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1 || max_kv > kMaxKeys) return 0;
+  if (!rows_sizes_ok(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv)) return 0;
   return rows_attention_plan(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv).ws_bytes;
 }
 
 const char *pf_attention_rows_kernel_name(int dtype, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv,
                                           int *chunks) {
-  static thread_local char name[64];
-  if (!dt_ok(dtype) || total_q < 1 || n_seqs < 1 || !head_ok(head_dim) || !heads_ok(total_q, n_heads, kv_heads) || max_kv < 1 || max_kv > kMaxKeys) return "";
+  if (!rows_sizes_ok(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv)) return "";
   const RowsPlan p = rows_attention_plan(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
   if (chunks) *chunks = p.splits;
-  const int dim = head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128;
-  if (p.shape == ROWS_WIDE) snprintf(name, sizeof(name), "attn_rows_wide_kernel<%d,%d>", dim, head_dim <= 80 && dim == 96 ? 5 : dim / 16);
-  else snprintf(name, sizeof(name), "attn_rows_kernel<%s,%d,%s>", dtype == PF_BF16 ? "bf16" : "float", dim, p.shape == ROWS_KEYS ? "1,4" : "4,1");
-  return name;
+  return rows_kernel_name(p, dtype, head_dim);
 }
 
 static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws_bytes, void *stream, const char *who) {
@@ -218,12 +227,13 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
   if (a.scale <= 0.f) a.scale = 1.0f / sqrtf((float)a.head_dim);
   // the kernels take it times log2(e)
   if (!isfinite(a.scale * 1.5f)) return refuse(PF_ERR_SHAPE, "%s: scale %g", who, (double)a.scale);
-  const RowsPlan p = rows_attention_plan(a.dt, a.total_q, a.n_seqs, a.n_heads, a.kv_heads, a.head_dim, max_kv);
+  const RowsPlan p = a.mx.k_scale ? mx_attention_plan(a.dt, a.mx.format, a.total_q, a.n_seqs, a.n_heads, a.kv_heads, a.head_dim, max_kv)
+                                  : rows_attention_plan(a.dt, a.total_q, a.n_seqs, a.n_heads, a.kv_heads, a.head_dim, max_kv);
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes || !aligned(ws, 16)))
     return refuse(PF_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes is needed, %zu given", who, p.ws_bytes, ws ? ws_bytes : (size_t)0);
   a.ws = (float *)ws;
   // a launch has less than 2^32 threads
-  if (((int64_t)a.total_q * (a.n_heads / a.kv_heads) / 32 + a.n_seqs) * a.kv_heads * p.splits >= (1 << 24))
+  if (((int64_t)a.total_q * (a.n_heads / a.kv_heads) / (p.shape == ROWS_FEW ? 16 : 32) + a.n_seqs) * a.kv_heads * p.splits >= (1 << 24))
     return refuse(PF_ERR_SHAPE, "%s: %d rows of %d heads in %d sequences are too many for one launch", who, a.total_q, a.n_heads, a.n_seqs);
   a.shape = p.shape;
   a.splits = p.splits;
@@ -392,14 +402,16 @@ pf_status pf_op_kv_read_mx(int dtype, const pf_kv_mx_pages *pages, const int32_t
 }
 
 size_t pf_op_attention_mx_ws_bytes(int dtype, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
-  if (format != PF_MX_E4M3 && format != PF_MX_E2M1) return 0;
-  return pf_op_attention_rows_ws_bytes(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
+  if ((format != PF_MX_E4M3 && format != PF_MX_E2M1) || !rows_sizes_ok(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv)) return 0;
+  return mx_attention_plan(dtype, format, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv).ws_bytes;
 }
 
 const char *pf_attention_mx_kernel_name(int dtype, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim,
                                         int64_t max_kv, int *chunks) {
-  if (format != PF_MX_E4M3 && format != PF_MX_E2M1) return "";
-  return pf_attention_rows_kernel_name(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv, chunks);
+  if ((format != PF_MX_E4M3 && format != PF_MX_E2M1) || !rows_sizes_ok(dtype, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv)) return "";
+  const RowsPlan p = mx_attention_plan(dtype, format, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
+  if (chunks) *chunks = p.splits;
+  return rows_kernel_name(p, dtype, head_dim);
 }
 
 pf_status pf_op_attention_mx(int dtype, const void *q, int64_t ldq, const pf_kv_mx_pages *pages, const int32_t *cu_q,
