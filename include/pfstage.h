@@ -582,7 +582,8 @@ int pf_kv_mx_row_bytes(int format, int head_dim);
  * dtype, and v as it is are written in few bits, block by block: the exponent is the least e with max |x| <= 448 * 2^e (E2M1: 6 *
  * 2^e), kept inside -117 .. 119 (E2M1: -125 .. 125; every value is then a bf16 number), a code the nearest to x / 2^e, ties to even, at
  * most the largest.  A block with an infinity or a NaN gets byte 255 and codes 0.  q, normed and turned, goes to q_out (may be q itself);
- * q NULL: n_heads must be 0.  Rows of no sequence and slots without a page as in pf_op_kv_append.  dtype is that of the rows alone.
+ * q NULL: n_heads must be 0.  Rows of no sequence and slots without a page as in pf_op_kv_append; two rows for one slot leave bytes of
+ * either, one row's exponents beside the other's codes among them.  dtype is that of the rows alone.
  */
 pf_status pf_op_kv_append_mx(int dtype, const pf_kv_mx_pages *pages, const void *k, int64_t ldk, const pf_norm *k_norm, const void *v,
                              int64_t ldv, const int32_t *cu, const int32_t *first, int tokens, const pf_rope *rope, const int32_t *pos,

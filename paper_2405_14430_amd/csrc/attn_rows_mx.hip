@@ -1,8 +1,8 @@
 // Attention of packed rows over pages of 8- or 4-bit numbers: the kernels of attn_rows.h with a loader that brings codes from memory and
 // writes what they stand for to LDS, in the type of the rows.
 //
-// Every value that the pages can hold is a number of both types, so from the LDS on nothing differs from pages of rows, and the
-// results are bit for bit those over pages that hold the decoded rows.  A tile needs half or a quarter of the bytes from memory, and a
+// Every value that the pages can hold is a number of both types, so from the LDS on nothing differs from pages of rows, and these
+// kernels' results are bit for bit those over pages that hold the decoded rows.  A tile needs half or a quarter of the bytes from memory, and a
 // conversion instruction for two channels on its way to LDS.
 #include "attn_rows.h"
 #include "mx.h"
@@ -216,9 +216,12 @@ __device__ __forceinline__ float over_groups(float v, F &&op) {
 //                            loads and decodes itself.  Channel order is free as long as Q has the same: where a row is a multiple of 64
 //                            channels the four lanes of a key hold a quarter of it each, one after the other, so that they load whole units.
 //   O^T[c][row] += V^T P^T   V through LDS, decoded on its way there and read transposed; P^T are the scores' accumulators as they are.
-// Against 32 rows it has half the accumulators, half the exponentials per key and, with K out of LDS, half the LDS: four workgroups fit a CU.
-// As in the key kernel every wave walks a quarter of the workgroup's keys in tiles of its own, and the loads of the next tile run
-// meanwhile.
+// Against 32 rows it has half the accumulators, half the exponentials per key and, with K out of LDS, half the LDS: three or four
+// workgroups fit a CU instead of two.  As in the key kernel every wave walks a quarter of the workgroup's keys in tiles of its own, and the
+// loads of the next tile run meanwhile.
+//   64 tokens over 514k keys of 8 heads of 128: e4m3 1.09 GB in 104 us, 10.4 TB/s where the Infinity Cache helps, in the key kernel 120;
+//   e2m1 0.56 GB in 61 us against 110.  Heads of 64: 54 and 43 us against 74 and 70, of 72 (16 of them) 165 and 128 against 178 and 138.
+// In 8 bits it waits for memory.  In 4 bits conversions, exponentials and selects of a tile take as long as its bytes.
 constexpr int FEW_ROWS = 16;
 constexpr int few_workgroups_of(int dhp) { return dhp == 64 ? 4 : dhp == 96 ? 2 : 3; }   // on a CU, by their registers
 template <int DHP>
@@ -244,7 +247,7 @@ __device__ __forceinline__ void few_sequence(const RowsAttn &a, int s, int &q0, 
   first = CAUSAL ? a.first[s] : 0;
   if (CAUSAL) keys = (int)min((int64_t)keys, max(first + n, (int64_t)0));   // that its last row sees
 }
-__device__ __forceinline__ int few_chunks(int keys, int chunk) { return max((int)((unsigned)(keys + chunk - 1) / (unsigned)chunk), 1); }
+__device__ __forceinline__ int few_chunks(int keys, int chunk) { return max((int)(((unsigned)keys + chunk - 1) / (unsigned)chunk), 1); }
 template <bool CAUSAL>
 __device__ __forceinline__ int few_ends(const RowsAttn &a, int group, int chunk, int block, int lane) {
   int end = 0;
@@ -312,205 +315,205 @@ __global__ __launch_bounds__(256, (few_workgroups_of(DHP))) void attn_rows_few_k
   int block = 0, ends = few_ends<CAUSAL>(args.a, args.group, chunk, 0, lane);
   int base = 0;                      // items in front of the block
   for (int item = blockIdx.x / kv_heads; item < most_items; item += slots) {
-  while (item >= base + __builtin_amdgcn_readlane(ends, 63)) {
-    base += __builtin_amdgcn_readlane(ends, 63);
-    block += 64;
-    if (block >= args.a.n_seqs || base >= most_items) return;
-    ends = few_ends<CAUSAL>(args.a, args.group, chunk, block, lane);
-  }
-  const RowsKernelArgs &p = again(args);   // read again for every item: kept over all of them they cost more registers than there are
-  const RowsAttn &a = p.a;
-  const int dh = a.head_dim, G = p.group;
-  Work w;
-  int all_chunks;
-  few_item<CAUSAL>(a, G, chunk, block, ends, item - base, w, all_chunks);
-  w.hk = hk;
-  const auto share = [&](int v, int &b, int &e) __attribute__((always_inline)) {   // wave v's keys
-    const int q = ((w.ke - w.kb + C::WAVES - 1) / C::WAVES + TK - 1) / TK * TK;
-    b = min(w.ke, w.kb + v * q);
-    e = min(w.ke, b + q);
-  };
-  int kb, ke;
-  share(wave, kb, ke);
-  kb = uniform(kb);
-  ke = uniform(ke);
-  const int tiles = (ke - kb + TK - 1) / TK;
-
-  const LaneRow row(w, G, l16);
-  int limit = ke;                    // keys before this one are seen
-  if (CAUSAL && row.ok && w.first + row.tok + 1 < limit) limit = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
-  int least = limit;
-  for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
-  least = uniform(least);
-
-  const auto channel = [&](int ks) __attribute__((always_inline)) { return WHOLE ? g * PER + ks * 8 : ks * 32 + g * 8; };   // first of the lane's eight of step ks
-  u32x4 qf[KS];
-  {
-    const T *qp = (const T *)a.q + (int64_t)(w.q0 + row.tok) * a.ldq + (int64_t)row.head * dh;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      qf[ks] = u32x4{0, 0, 0, 0};
-      if (row.ok && channel(ks) < dh) qf[ks] = *reinterpret_cast<const u32x4 *>(qp + channel(ks));
+    while (item >= base + __builtin_amdgcn_readlane(ends, 63)) {
+      base += __builtin_amdgcn_readlane(ends, 63);
+      block += 64;
+      if (block >= args.a.n_seqs || base >= most_items) return;
+      ends = few_ends<CAUSAL>(args.a, args.group, chunk, block, lane);
     }
-  }
+    const RowsKernelArgs &p = again(args);   // read again for every item: kept over all of them they cost more registers than there are
+    const RowsAttn &a = p.a;
+    const int dh = a.head_dim, G = p.group;
+    Work w;
+    int all_chunks;
+    few_item<CAUSAL>(a, G, chunk, block, ends, item - base, w, all_chunks);
+    w.hk = hk;
+    const auto share = [&](int v, int &b, int &e) __attribute__((always_inline)) {   // wave v's keys
+      const int q = ((w.ke - w.kb + C::WAVES - 1) / C::WAVES + TK - 1) / TK * TK;
+      b = min(w.ke, w.kb + v * q);
+      e = min(w.ke, b + q);
+    };
+    int kb, ke;
+    share(wave, kb, ke);
+    kb = uniform(kb);
+    ke = uniform(ke);
+    const int tiles = (ke - kb + TK - 1) / TK;
 
-  Loader ld(a, w, lane, 0, kb, ke);
-  unsigned k_reg[2][KLOADS][KWORDS], k_exp[2][KLOADS][1];
-  unsigned k_off[KLOADS], k_then[KLOADS], k_exp_off[KLOADS];
-#pragma unroll
-  for (int i = 0; i < KLOADS; ++i) {
-    const int c = channel(i), byte = c * BITS / 8;
-    unsigned at = l16 * a.mx.row_bytes + byte, exp_at = l16 * a.mx.blocks + c / PF_MX_BLOCK;
-    k_off[i] = byte < a.mx.row_bytes ? at : Loader::kOutside;
-    k_then[i] = byte + 16 < a.mx.row_bytes ? at + 16 : Loader::kOutside;   // the next row's codes are not this one's, whatever Q has there
-    k_exp_off[i] = byte < a.mx.row_bytes ? exp_at : Loader::kOutside;
-  }
-  const auto load = [&](int t) __attribute__((always_inline)) {
-    ld.aim(t);
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const Buffer<C::POLICY> codes(ld.k_from[b], ld.in_group[b] * a.mx.row_bytes), exps(ld.ks_from[b], ld.in_group[b] * a.mx.blocks);
-#pragma unroll
-      for (int i = 0; i < KLOADS; ++i) {
-        load_units<KBYTES>(codes, k_reg[b][i], k_off[i], k_then[i]);
-        exps.template load<1>(k_exp[b][i], k_exp_off[i], 0);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < C::LOADS; ++i) ld.load_v(i);
-  };
+    const LaneRow row(w, G, l16);
+    int limit = ke;                    // keys before this one are seen
+    if (CAUSAL && row.ok && w.first + row.tok + 1 < limit) limit = w.first + row.tok + 1 < 0 ? 0 : (int)(w.first + row.tok + 1);
+    int least = limit;
+    for (int o = 8; o > 0; o >>= 1) least = min(least, __shfl_xor(least, o, kWave));
+    least = uniform(least);
 
-  // keys with infinities or NaN among those that some row does not see
-  constexpr int ZONE = (C::ROWS + TK - 2) / TK + 1;
-  unsigned *const hidden = hidden_all[wave];
-  const bool zoned = CAUSAL && w.zone < ke;
-  const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
-  if (CAUSAL && lane < ZONE) hidden[lane] = 0;
-
-  f32x4 o[CB];
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) o[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = -INFINITY, l_run = 0.f;    // running maximum of the raw scores; the lane's share of the sum
-  unsigned char *const tile = smem + wave * C::VTILE_B;
-  const unsigned char *const v_at = tile + (4 * g + (l16 >> 2)) * C::VROWB + (l16 & 3) * 8;
-
-  if (tiles > 0) load(0);
-  for (int t = 0; t < tiles; ++t) {
-    const unsigned groups = ld.groups;
-    const bool clear = zoned && t >= zone_tile;
-    if (uniform((int)clear) != 0) ld.clear_v(hidden, t - zone_tile);
-#pragma unroll
-    for (int i = 0; i < C::LOADS; ++i) ld.store_v(tile, i);
-    __builtin_amdgcn_sched_barrier(0);   // here and below: what the next part needs is not brought in early, at the cost of registers
-    f32x4 sc[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const auto channel = [&](int ks) __attribute__((always_inline)) { return WHOLE ? g * PER + ks * 8 : ks * 32 + g * 8; };   // first of the lane's eight of step ks
+    u32x4 qf[KS];
+    {
+      const T *qp = (const T *)a.q + (int64_t)(w.q0 + row.tok) * a.ldq + (int64_t)row.head * dh;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const int i = WHOLE ? 0 : ks;
-        const u32x4 kf = eight<FMT>(k_reg[b][i], mx_power(k_exp[b][i][0]), WHOLE ? ks : 0);
-        sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[ks]), sc[b], 0, 0, 0);
+        qf[ks] = u32x4{0, 0, 0, 0};
+        if (row.ok && channel(ks) < dh) qf[ks] = *reinterpret_cast<const u32x4 *>(qp + channel(ks));
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (t + 1 < tiles) load(t + 1);
-    const int key0 = kb + t * TK;
-    if (key0 + TK > least || groups != Loader::kAllGroups) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (key0 + b * 16 + g * 4 + i >= limit || !((groups >> b) & 1)) sc[b][i] = -INFINITY;
-    }
-    float tmax = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-    tmax = over_groups(tmax, [](float x, float y) { return fmaxf(x, y); });
-    const float m_new = fmaxf(m_run, tmax);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;           // a row that has seen no key yet: weights 2^-inf = 0
-    const float alpha = __builtin_amdgcn_exp2f((m_run - m_use) * p.sl2);
-    const float neg = -m_use * p.sl2;
-    m_run = m_new;
-    float sum = 0.f;
-    bf16x8 pf;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], p.sl2, neg));
-      sum += x;
-      pf[e] = (bf16_t)x;
-    }
-    l_run = l_run * alpha + sum;
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {          // no rescale where no row's maximum moved
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[cb][i] *= alpha;
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    // place e of a lane's eight keys: key 4 g + (e & 3) of the first or second 16, the order in which the accumulators hold the weights
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(v_at + cb * 32), lds_read_transposed(v_at + 16 * C::VROWB + cb * 32)};
-      o[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v8), pf, o[cb], 0, 0, 0);
-    }
-  }
-  float l_tot = over_groups(l_run, [](float x, float y) { return x + y; });
 
-  // join the waves: each leaves (m, l, O), and sums a quarter of the channels in the waves' order
-  __syncthreads();
-  float *om = reinterpret_cast<float *>(smem), *ml = om + C::WAVES * C::ROWS * C::OSTR;
-  float *mine = om + (wave * C::ROWS + l16) * C::OSTR;
+    Loader ld(a, w, lane, 0, kb, ke);
+    unsigned k_reg[2][KLOADS][KWORDS], k_exp[2][KLOADS][1];
+    unsigned k_off[KLOADS], k_then[KLOADS], k_exp_off[KLOADS];
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<f32x4 *>(mine + cb * 16 + g * 4) = o[cb];
-  if (g == 0) {
-    ml[(wave * C::ROWS + l16) * 2] = m_run;
-    ml[(wave * C::ROWS + l16) * 2 + 1] = l_tot;
-  }
-  __syncthreads();
-  float m_all = -INFINITY;
+    for (int i = 0; i < KLOADS; ++i) {
+      const int c = channel(i), byte = c * BITS / 8;
+      unsigned at = l16 * a.mx.row_bytes + byte, exp_at = l16 * a.mx.blocks + c / PF_MX_BLOCK;
+      k_off[i] = byte < a.mx.row_bytes ? at : Loader::kOutside;
+      k_then[i] = byte + 16 < a.mx.row_bytes ? at + 16 : Loader::kOutside;   // the next row's codes are not this one's, whatever Q has there
+      k_exp_off[i] = byte < a.mx.row_bytes ? exp_at : Loader::kOutside;
+    }
+    const auto load = [&](int t) __attribute__((always_inline)) {
+      ld.aim(t);
 #pragma unroll
-  for (int v = 0; v < C::WAVES; ++v) m_all = fmaxf(m_all, ml[(v * C::ROWS + l16) * 2]);
-  const float m_use = m_all == -INFINITY ? 0.f : m_all;
-  float wt[C::WAVES];
-  l_tot = 0.f;
+      for (int b = 0; b < 2; ++b) {
+        const Buffer<C::POLICY> codes(ld.k_from[b], ld.in_group[b] * a.mx.row_bytes), exps(ld.ks_from[b], ld.in_group[b] * a.mx.blocks);
 #pragma unroll
-  for (int v = 0; v < C::WAVES; ++v) {
-    wt[v] = __builtin_amdgcn_exp2f((ml[(v * C::ROWS + l16) * 2] - m_use) * p.sl2);
-    l_tot += wt[v] * ml[(v * C::ROWS + l16) * 2 + 1];
-  }
-  if (row.ok) {
-    const float inv = l_tot != 0.f ? 1.f / l_tot : 0.f;
-#pragma unroll
-    for (int i = 0; i < (CB + 3) / 4; ++i) {
-      const int c = (wave + C::WAVES * i) * 16 + g * 4;            // the lane's channels c .. c + 3
-      if (c < dh) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int v = 0; v < C::WAVES; ++v) {
-          const f32x4 x = *reinterpret_cast<const f32x4 *>(om + (v * C::ROWS + l16) * C::OSTR + c);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] = fmaf(wt[v], x[e], acc[e]);
+        for (int i = 0; i < KLOADS; ++i) {
+          load_units<KBYTES>(codes, k_reg[b][i], k_off[i], k_then[i]);
+          exps.template load<1>(k_exp[b][i], k_exp_off[i], 0);
         }
-        put4<T>(a, w.sp, w.q0 + row.tok, row.head, c, inv, acc[0], acc[1], acc[2], acc[3]);
+      }
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) ld.load_v(i);
+    };
+
+    // keys with infinities or NaN among those that some row does not see
+    constexpr int ZONE = (C::ROWS + TK - 2) / TK + 1;
+    unsigned *const hidden = hidden_all[wave];
+    const bool zoned = CAUSAL && w.zone < ke;
+    const int zone_tile = zoned && w.zone > kb ? (w.zone - kb) / TK : 0;
+    if (CAUSAL && lane < ZONE) hidden[lane] = 0;
+
+    f32x4 o[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) o[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;    // running maximum of the raw scores; the lane's share of the sum
+    unsigned char *const tile = smem + wave * C::VTILE_B;
+    const unsigned char *const v_at = tile + (4 * g + (l16 >> 2)) * C::VROWB + (l16 & 3) * 8;
+
+    if (tiles > 0) load(0);
+    for (int t = 0; t < tiles; ++t) {
+      const unsigned groups = ld.groups;
+      const bool clear = zoned && t >= zone_tile;
+      if (uniform((int)clear) != 0) ld.clear_v(hidden, t - zone_tile);
+#pragma unroll
+      for (int i = 0; i < C::LOADS; ++i) ld.store_v(tile, i);
+      __builtin_amdgcn_sched_barrier(0);   // here and below: what the next part needs is not brought in early, at the cost of registers
+      f32x4 sc[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        sc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int i = WHOLE ? 0 : ks;
+          const u32x4 kf = eight<FMT>(k_reg[b][i], mx_power(k_exp[b][i][0]), WHOLE ? ks : 0);
+          sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[ks]), sc[b], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (t + 1 < tiles) load(t + 1);
+      const int key0 = kb + t * TK;
+      if (key0 + TK > least || groups != Loader::kAllGroups) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key0 + b * 16 + g * 4 + i >= limit || !((groups >> b) & 1)) sc[b][i] = -INFINITY;
+      }
+      float tmax = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      tmax = over_groups(tmax, [](float x, float y) { return fmaxf(x, y); });
+      const float m_new = fmaxf(m_run, tmax);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;           // a row that has seen no key yet: weights 2^-inf = 0
+      const float alpha = __builtin_amdgcn_exp2f((m_run - m_use) * p.sl2);
+      const float neg = -m_use * p.sl2;
+      m_run = m_new;
+      float sum = 0.f;
+      bf16x8 pf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], p.sl2, neg));
+        sum += x;
+        pf[e] = (bf16_t)x;
+      }
+      l_run = l_run * alpha + sum;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {          // no rescale where no row's maximum moved
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[cb][i] *= alpha;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // place e of a lane's eight keys: key 4 g + (e & 3) of the first or second 16, the order in which the accumulators hold the weights
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        struct { s16x4 lo, hi4; } v8 = {lds_read_transposed(v_at + cb * 32), lds_read_transposed(v_at + 16 * C::VROWB + cb * 32)};
+        o[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v8), pf, o[cb], 0, 0, 0);
       }
     }
-    if (g == 0 && wave == 0) put_stats(a, w.sp, w.q0 + row.tok, row.head, m_all * p.sl2, l_tot);
-  }
-  // the tile's last chunk says of those that are not there that they are empty
-  if (a.splits > 1 && w.sp == all_chunks - 1) {
-    for (int i = threadIdx.x; i < (a.splits - all_chunks) * C::ROWS; i += 256) {
-      const LaneRow empty(w, G, i % C::ROWS);
-      if (empty.ok) put_stats(a, all_chunks + i / C::ROWS, w.q0 + empty.tok, empty.head, -INFINITY, 0.f);
+    float l_tot = over_groups(l_run, [](float x, float y) { return x + y; });
+
+    // join the waves: each leaves (m, l, O), and sums a quarter of the channels in the waves' order
+    __syncthreads();
+    float *om = reinterpret_cast<float *>(smem), *ml = om + C::WAVES * C::ROWS * C::OSTR;
+    float *mine = om + (wave * C::ROWS + l16) * C::OSTR;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) *reinterpret_cast<f32x4 *>(mine + cb * 16 + g * 4) = o[cb];
+    if (g == 0) {
+      ml[(wave * C::ROWS + l16) * 2] = m_run;
+      ml[(wave * C::ROWS + l16) * 2 + 1] = l_tot;
     }
-  }
-  if (CAUSAL && w.zone < w.ke) {
-#pragma unroll 1
+    __syncthreads();
+    float m_all = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < C::WAVES; ++v) m_all = fmaxf(m_all, ml[(v * C::ROWS + l16) * 2]);
+    const float m_use = m_all == -INFINITY ? 0.f : m_all;
+    float wt[C::WAVES];
+    l_tot = 0.f;
+#pragma unroll
     for (int v = 0; v < C::WAVES; ++v) {
-      int b, e;
-      share(v, b, e);
-      if (w.zone < e) add_hidden<C, T, SRC, C::ROWS, 256>(p, w, hidden_all[v], ZONE, b + (w.zone > b ? (w.zone - b) / TK : 0) * TK, e);
+      wt[v] = __builtin_amdgcn_exp2f((ml[(v * C::ROWS + l16) * 2] - m_use) * p.sl2);
+      l_tot += wt[v] * ml[(v * C::ROWS + l16) * 2 + 1];
     }
-  }
-  __syncthreads();                   // the next item's tiles take the LDS
+    if (row.ok) {
+      const float inv = l_tot != 0.f ? 1.f / l_tot : 0.f;
+#pragma unroll
+      for (int i = 0; i < (CB + 3) / 4; ++i) {
+        const int c = (wave + C::WAVES * i) * 16 + g * 4;            // the lane's channels c .. c + 3
+        if (c < dh) {
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int v = 0; v < C::WAVES; ++v) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(om + (v * C::ROWS + l16) * C::OSTR + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(wt[v], x[e], acc[e]);
+          }
+          put4<T>(a, w.sp, w.q0 + row.tok, row.head, c, inv, acc[0], acc[1], acc[2], acc[3]);
+        }
+      }
+      if (g == 0 && wave == 0) put_stats(a, w.sp, w.q0 + row.tok, row.head, m_all * p.sl2, l_tot);
+    }
+    // the tile's last chunk says of those that are not there that they are empty
+    if (a.splits > 1 && w.sp == all_chunks - 1) {
+      for (int i = threadIdx.x; i < (a.splits - all_chunks) * C::ROWS; i += 256) {
+        const LaneRow empty(w, G, i % C::ROWS);
+        if (empty.ok) put_stats(a, all_chunks + i / C::ROWS, w.q0 + empty.tok, empty.head, -INFINITY, 0.f);
+      }
+    }
+    if (CAUSAL && w.zone < w.ke) {
+#pragma unroll 1
+      for (int v = 0; v < C::WAVES; ++v) {
+        int b, e;
+        share(v, b, e);
+        if (w.zone < e) add_hidden<C, T, SRC, C::ROWS, 256>(p, w, hidden_all[v], ZONE, b + (w.zone > b ? (w.zone - b) / TK : 0) * TK, e);
+      }
+    }
+    __syncthreads();                   // the next item's tiles take the LDS
   }
 }
 
