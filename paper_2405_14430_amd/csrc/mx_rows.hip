@@ -155,16 +155,14 @@ struct HeadLanes {
   }
 };
 
-// 1 / sqrt(x): the hardware's, within a unit; for fp32 rows with a step of Newton's behind it.  Tiny sums are scaled, it takes no subnormal ones.
-template <typename T>
+// 1 / sqrt(x): the hardware's, within a unit, with a step of Newton's behind it.  Tiny sums are scaled, it takes no subnormal ones.
+// (For bf16 rows, too: it moves a whole head, and each value next to a border of two codes that it takes across shows as a step of 2^-4.)
 __device__ __forceinline__ float inverse_root(float x) {
   const bool tiny = x < 0x1p-100f;
   const float y = tiny ? x * 0x1p100f : x;
   float r = __builtin_amdgcn_rsqf(y);
-  if constexpr (sizeof(T) == 4) {
-    const float better = fmaf(0.5f * r, fmaf(-y * r, r, 1.0f), r);
-    r = r == 0.f || y == 0.f ? r : better;
-  }
+  const float better = fmaf(0.5f * r, fmaf(-y * r, r, 1.0f), r);
+  r = r == 0.f || y == 0.f ? r : better;
   return tiny ? r * 0x1p50f : r;
 }
 
@@ -286,8 +284,11 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
       const int end0 = rk.axis_end[0], end1 = rk.axis_end[1];
       const int axis = (lane >= end0) + (rk.n_axes > 1 && lane >= end1);
       const double turns = (double)p.pos[(int64_t)token * rk.n_axes + axis] * rk.turns[lane];
-      float s, c;
-      sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+      const double part = turns - rint(turns);
+      float sin0, cos0;
+      sincospif(2.0f * (float)part, &sin0, &cos0);
+      const float rest = (float)((part - (float)part) * 6.283185307179586);   // what 24 bits of the fraction leave out, in radians
+      const float s = fmaf(cos0, rest, sin0), c = fmaf(-sin0, rest, cos0);
       const int begin = pick(axis == 0, 0, pick(axis == 1, end0, end1)), w = pick(axis == 0, end0, pick(axis == 1, end1, rk.axis_end[2])) - begin;
       const int one = HALF ? 2 * begin + (lane - begin) : 2 * lane, two = HALF ? one + w : one + 1;
       table[wave][0][one] = table[wave][0][two] = c * rk.magnitude;
@@ -352,7 +353,7 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
           float sum = 0.f;
 #pragma unroll
           for (int c = 0; c < V; ++c) sum = fmaf(x[c], x[c], sum);
-          const float r = inverse_root<T>(fmaf(head.sum(sum), inv, eps));
+          const float r = inverse_root(fmaf(head.sum(sum), inv, eps));
 #pragma unroll
           for (int c = 0; c < V; ++c) x[c] *= r;
           if (w) {
