@@ -354,15 +354,15 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
 #pragma unroll
           for (int c = 0; c < V; ++c) sum = fmaf(x[c], x[c], sum);
           const float r = inverse_root(fmaf(head.sum(sum), inv, eps));
-#pragma unroll
-          for (int c = 0; c < V; ++c) x[c] *= r;
-          if (w) {
+          if (w) {                                    // in front of r: a product of two bf16 numbers is exact
             Unit<T> g;
 #pragma unroll
             for (int c = 0; c < Unit<T>::N; ++c) g.w[c] = pick(is_q, weight[0].w[c], weight[1].w[c]);
 #pragma unroll
             for (int c = 0; c < V; ++c) x[c] *= g[c];
           }
+#pragma unroll
+          for (int c = 0; c < V; ++c) x[c] *= r;
           if (b) {
             Unit<T> bias;
             bias.load(b + c0, false);
