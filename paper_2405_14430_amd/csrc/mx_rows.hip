@@ -218,7 +218,13 @@ __device__ __forceinline__ void find_slot(const Pages &pages, const int32_t *cu,
 // A wave takes a token, or a share of its heads (gridDim.y shares): its 64 lanes work out the cosines and sines of up to 64 pairs and find the
 // token's slot, then it goes over the heads, side after side (q, k, v), `fit` of them at a step.  A lane has the same channels of every head it
 // meets, so their cosines, sines and weights stay in registers.  The rows of kDepth steps are loaded together, the first ones before
-// all else; what hides a wave's waiting is the other waves, which it has nothing to do with.
+// all else; what hides a wave's waiting is the other waves, which it has nothing to do with.  (A workgroup over several tokens, their
+// tables in LDS and their slots found together, took 57 us a call where this takes 49, 100 where 93, and 68 where 59.)
+//   16896 tokens of 32 heads of 128, bf16, to rows: 277 MB in 45 us, 6.1 TB/s with the Infinity Cache's help.
+//   16384 tokens of 72 heads of 64 into e4m3: 254 MB in 60 - 64 us, 4.1 TB/s; memory.
+//   7178 tokens of 48 heads of 72, fp32, layer norm, halves, into e2m1: 144 MB in 46 us, 3.1 TB/s: waits for memory with 14 waves to a CU, whose
+//   109 registers leave room for no more (bounded to 96 they spill: 63 us; two steps' loads at a time 47).
+//   32 tokens of 40 heads of 128: 3.2 us in a graph, launch and two latencies.
 template <typename T> constexpr int kDepth = sizeof(T) == 2 ? 4 : 3;
 template <typename T, int FMT, int LAYOUT, int N>
 __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK p) {
@@ -432,7 +438,8 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
   }
 }
 
-// Slots of pages to rows: a workgroup takes tok tokens, a wave `fit` heads at a step and READ_DEPTH steps' loads at a time.
+// Slots of pages to rows: a workgroup takes tok tokens, a wave `fit` heads at a step and READ_DEPTH steps' loads at a time.  Bound by memory:
+// 24 caches of up to 8192 tokens, 8 heads of 128, e4m3 to bf16, 221 MB in 40 us, 5.5 TB/s.
 struct ReadK {
   MxRead r;
   int tok, t0;
@@ -494,7 +501,9 @@ __global__ __launch_bounds__(64 * kWaves) void mx_read_kernel(ReadK p) {
   }
 }
 
-// Workgroups along y for launches of few tokens: a token's `parts` turns of a workgroup are split over them while they are few.
+// Workgroups along y for launches of few tokens: a token's `parts` turns of a workgroup are split over them while they are few.  Up to 4096 shares:
+// 1024 tokens of 40 heads of 128 are normed and turned in 6.8 us (up to 2048: 7.5, 16384: 7.7, tokens left whole: 9.5), 8 tokens in 3.2 (whole: 7.9), 4096 in
+// 17.7 either way.
 int split(int tokens, int parts) {
   int y = std::max(parts, 1);
   while (y > 1 && (int64_t)tokens * y > 4096) y = (y + 1) / 2;
@@ -535,7 +544,8 @@ hipError_t launch_format(const TurnK &rk, const HeadsK &p, int format, bool half
 template <typename T, int FMT>
 hipError_t launch_read(ReadK p, hipStream_t s) {
   const int per_turn = 64 / (p.r.head_dim / V) * kWaves, heads = ((p.r.k_out != nullptr) + (p.r.v_out != nullptr)) * p.r.kv_heads;
-  p.tok = p.r.tokens < 4096 ? 1 : std::min(std::max(READ_DEPTH * per_turn / heads, 1), kMaxReadTok);
+  // one token to a workgroup, its heads split, or several: 1024 tokens of 2 x 8 heads of 128 4.5 and 4.7 us, 2048 6.3 and 5.9, 4096 9.6 and 8.0
+  p.tok = p.r.tokens < 2048 ? 1 : std::min(std::max(READ_DEPTH * per_turn / heads, 1), kMaxReadTok);
   const int y = p.tok == 1 ? split(p.r.tokens, (heads + per_turn - 1) / per_turn) : 1;
   hipError_t e = hipSuccess;
   for (p.t0 = 0; p.t0 < p.r.tokens && e == hipSuccess; p.t0 += kLaunchRows) {
