@@ -219,9 +219,10 @@ __device__ __forceinline__ float over_groups(float v, F &&op) {
 // Against 32 rows it has half the accumulators, half the exponentials per key and, with K out of LDS, half the LDS: three or four
 // workgroups fit a CU instead of two.  As in the key kernel every wave walks a quarter of the workgroup's keys in tiles of its own, and the
 // loads of the next tile run meanwhile.
-//   64 tokens over 514k keys of 8 heads of 128: e4m3 1.09 GB in 104 us, 10.4 TB/s where the Infinity Cache helps, in the key kernel 120;
-//   e2m1 0.56 GB in 61 us against 110.  Heads of 64: 54 and 43 us against 74 and 70, of 72 (16 of them) 165 and 128 against 178 and 138.
-// In 8 bits it waits for memory.  In 4 bits conversions, exponentials and selects of a tile take as long as its bytes.
+//   64 tokens over 190817 keys in all, 8 heads of 128, in a graph over three such caches, join included: e4m3 404 MB in 104 us against 120 in the key
+//   kernel (alone, some of the keys still in the Infinity Cache, 83: 4.9 TB/s), e2m1 209 MB in 61 against 110.  Heads of 64: 54 and 43 us against
+//   74 and 70, of 72 (16 of them) 165 and 128 against 178 and 138.
+// In 8 bits it is bound by memory.  In 4 bits by latency: 2 to 3 waves to a SIMD, its vector unit busy for a third of the time.
 constexpr int FEW_ROWS = 16;
 constexpr int few_workgroups_of(int dhp) { return dhp == 64 ? 4 : dhp == 96 ? 2 : 3; }   // on a CU, by their registers
 template <int DHP>
