@@ -549,13 +549,18 @@ hipError_t launch_mask(const RowsAttn &a, hipStream_t s) {
 }  // namespace
 
 RowsPlan mx_attention_plan(int dt, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
-  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads);
-  if (dt != DT_BF16 || rows > (int64_t)n_seqs * 16) return rows_attention_plan(dt, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
-  // Chunks of 1024 keys: the workgroups that are resident take them in turn, and share caches of different lengths (64 tokens over up to 16384 keys of
-  // 8 key heads, e4m3: 105 us, chunks of 512 111, of 2048 111; e2m1 62, 69, 67).  Smaller ones, down to 256, for small caches (8 tokens over up to 8192:
-  // 18 us with 256 or 512, 21 with 1024; one over 4096: 13.1 with 256, 16.6 with 512).
+  // Where a sequence has more rows than a tile of the few kernel its keys are read again: against the key kernel's tiles of 32 rows that is dearer in 8
+  // bits (16 sequences of 20 rows over 8192 keys of 8 heads of 128: 125 us and 84) and not in 4 (72 and 72; of 32 rows 65 and 89).  One long
+  // sequence among short ones, which the totals do not show, is read by each of its tiles: 15 of 4 rows and one of 160, 8 bits 101 and 81, 4 bits 64 and 70.
+  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads), few = format == PF_MX_E2M1 ? 32 : 16;
+  if (dt != DT_BF16 || rows > n_seqs * few) return rows_attention_plan(dt, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
+  // Keys to a chunk.  All of them where they are few, or few enough with a tile for every CU (64 tokens over 1000 keys each, 8 / 4 bits: whole 35 / 21 us,
+  // chunks of 512 40 / 27, of 256 43 / 30; over 2500 75 / 43, chunks of 1024 83 / 49).  Else 1024, which workgroups taking them in turn spread
+  // evenly over caches of different lengths (64 tokens over up to 16384 keys 105 / 62, chunks of 512 111 / 69, of 2048 111 / 67); down to 256 with fewer
+  // tiles (8 tokens over up to 8192 keys 18 with 256 or 512, 21 with 1024; one over 4096 13.1 with 256, 16.6 with 512).
   const int64_t w = workgroups(total_q, n_heads / kv_heads, n_seqs, kv_heads, 16);
-  int64_t c = std::min(std::max(w * max_kv / 2048, (int64_t)256), (int64_t)1024);
+  int64_t c = w >= 256 ? 1024 : std::min(std::max(w * max_kv / 2048, (int64_t)256), (int64_t)1024);
+  if (max_kv <= (w >= 256 ? 2560 : 512)) c = max_kv;
   c = (std::max(c, (max_kv + kMaxChunks - 1) / kMaxChunks) + 127) / 128 * 128;
   RowsPlan p{ROWS_FEW, (int)((max_kv + c - 1) / c), (int)c, 0};
   if (p.splits > 1) p.ws_bytes = (size_t)p.splits * total_q * n_heads * (head_dim + 2) * sizeof(float);
