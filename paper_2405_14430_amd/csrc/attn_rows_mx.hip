@@ -220,7 +220,7 @@ __device__ __forceinline__ float over_groups(float v, F &&op) {
 // workgroups fit a CU instead of two.  As in the key kernel every wave walks a quarter of the workgroup's keys in tiles of its own, and the
 // loads of the next tile run meanwhile.
 //   64 tokens over 190817 keys in all, 8 heads of 128, in a graph over three such caches, join included: e4m3 404 MB in 104 us against 120 in the key
-//   kernel (alone, some of the keys still in the Infinity Cache, 83: 4.9 TB/s), e2m1 209 MB in 61 against 110.  Heads of 64: 54 and 43 us against
+//   kernel (alone, some of the keys still in the Infinity Cache, 83: 4.9 TB/s), e2m1 209 MB in 61 against 110.  Heads of 64: 54 - 59 and 43 us against
 //   74 and 70, of 72 (16 of them) 165 and 128 against 178 and 138.
 // In 8 bits it is bound by memory.  In 4 bits by latency: 2 to 3 waves to a SIMD, its vector unit busy for a third of the time.
 constexpr int FEW_ROWS = 16;
@@ -275,9 +275,9 @@ __device__ __forceinline__ void few_item(const RowsAttn &a, int group, int chunk
   int keys;
   few_sequence<CAUSAL>(a, w.s, w.q0, w.n, keys, w.first);
   all_chunks = few_chunks(keys, chunk);
-  const int tile = (at - start) / all_chunks;
-  w.sp = at - start - tile * all_chunks;
-  w.r_first = tile * FEW_ROWS;
+  const int tiles = (w.n * group + FEW_ROWS - 1) / FEW_ROWS;
+  w.sp = (at - start) / tiles;         // tiles of a chunk one after the other: they read the same keys
+  w.r_first = (at - start - w.sp * tiles) * FEW_ROWS;
   w.k_end = keys;
   if (CAUSAL) w.k_end = (int)max(min((int64_t)keys, w.first + (min(w.r_first + FEW_ROWS, w.n * group) - 1) / group + 1), (int64_t)0);
   w.kb = (int)min((int64_t)w.k_end, (int64_t)w.sp * chunk);
@@ -550,9 +550,11 @@ hipError_t launch_mask(const RowsAttn &a, hipStream_t s) {
 
 RowsPlan mx_attention_plan(int dt, int format, int total_q, int n_seqs, int n_heads, int kv_heads, int head_dim, int64_t max_kv) {
   // Where a sequence has more rows than a tile of the few kernel its keys are read again: against the key kernel's tiles of 32 rows that is dearer in 8
-  // bits (16 sequences of 20 rows over 8192 keys of 8 heads of 128: 125 us and 84) and not in 4 (72 and 72; of 32 rows 65 and 89).  One long
-  // sequence among short ones, which the totals do not show, is read by each of its tiles: 15 of 4 rows and one of 160, 8 bits 101 and 81, 4 bits 64 and 70.
-  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads), few = format == PF_MX_E2M1 ? 32 : 16;
+  // bits (16 sequences of 20 rows over 8192 keys of 8 heads of 128: 121 us and 84) and not in 4 (70 and 71; of 32 rows 65 and 89).  In 8 bits one long
+  // sequence among short ones costs, too (63 of 4 rows and one of 400: 306 us and 250, in 4 bits 173 and 205).  The totals do not show it; they are
+  // taken for sequences of as many tokens each where they could be (16 of 16 rows: 76 and 84), and for such a mixture else.
+  const bool alike = total_q <= n_seqs || total_q % n_seqs == 0;
+  const int64_t rows = (int64_t)total_q * (n_heads / kv_heads), few = format == PF_MX_E2M1 ? 32 : alike ? 16 : 8;
   if (dt != DT_BF16 || rows > n_seqs * few) return rows_attention_plan(dt, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
   // Keys to a chunk.  All of them where they are few, or few enough with a tile for every CU (64 tokens over 1000 keys each, 8 / 4 bits: whole 35 / 21 us,
   // chunks of 512 40 / 27, of 256 43 / 30; over 2500 75 / 43, chunks of 1024 83 / 49).  Else 1024, which workgroups taking them in turn spread

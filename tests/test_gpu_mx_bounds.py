@@ -15,7 +15,8 @@ pytestmark = pytest.mark.gpu
 
 ATTENTION = [
     # type, head_dim, rows, sequences, heads, kv_heads, keys, kernel, in chunks
-    (BF16, 64, 40, 3, 4, 4, 3000, "attn_rows_few_kernel<64>", True),
+    (BF16, 64, 39, 3, 4, 4, 3000, "attn_rows_few_kernel<64>", True),
+    (BF16, 64, 40, 3, 4, 4, 3000, ("attn_rows_kernel<bf16,64,1,4>", "attn_rows_few_kernel<64>"), True),   # by format
     (BF16, 72, 3, 3, 16, 1, 3000, "attn_rows_few_kernel<96>", True),
     (BF16, 128, 60, 70, 8, 2, 170, "attn_rows_few_kernel<128>", False),
     (BF16, 128, 33, 3, 14, 2, 3000, "attn_rows_kernel<bf16,128,1,4>", True),
@@ -25,7 +26,7 @@ ATTENTION = [
     (F32, 96, 3, 3, 8, 1, 3000, "attn_rows_kernel<float,96,1,4>", True),
     (F32, 72, 1030, 3, 32, 4, 343, "attn_rows_kernel<float,96,4,1>", False),
 ]
-ids = lambda k: f"{k[7]}{'-chunks' if k[8] else ''}"
+ids = lambda k: f"{k[7] if isinstance(k[7], str) else 'by-format'}{'-chunks' if k[8] else ''}"
 
 
 def some_bytes(fmt, n_pages, kv_heads, page, dh, seed):
@@ -55,6 +56,7 @@ def wrong_table(g, rng, n, width, n_pages, good):
 def test_attention_of_wrong_lengths(case, fmt):
     dtype, dh, rows, seqs, heads, kv_heads, keys, name, chunks = case
     lib, page, n_pages = load_library(), 16, 9
+    name = name if isinstance(name, str) else name[M.FORMATS.index(fmt)]
     width = (keys + page - 1) // page
     n = C.c_int()
     sizes = (int(dtype == BF16), int(fmt == "e2m1"), rows, seqs, heads, kv_heads, dh, width * page)
