@@ -139,7 +139,8 @@ struct HeadLanes {
       }
     return __shfl(v, lane - u, kWave);
   }
-  // The largest of the block of four lanes (the last one of a head may be shorter).
+  // The largest of the block of four lanes.  The last one of a head may be shorter: in place of a lane that is not there the head's last one is asked,
+  // which lies in the same block (with itself in its place the second of three lanes would not hear of the third).
   __device__ __forceinline__ unsigned block_max(unsigned v) const {
     static_assert(PF_MX_BLOCK == 4 * V, "a block is four lanes");
     if constexpr (N != 0) {
@@ -147,10 +148,7 @@ struct HeadLanes {
       return max(v, across<kSwap2>(v));
     }
 #pragma unroll
-    for (int o = 1; o < 4; o *= 2) {
-      const int to = u ^ o;
-      v = max(v, (unsigned)__shfl((int)v, lane - u + (to < n ? to : u), kWave));
-    }
+    for (int o = 1; o < 4; o *= 2) v = max(v, (unsigned)__shfl((int)v, lane - u + min(u ^ o, n - 1), kWave));
     return v;
   }
 };

@@ -185,6 +185,28 @@ def test_append_of_hard_rows(dtype, fmt):
 
 
 @pytest.mark.parametrize("fmt", M.FORMATS)
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("dh", range(8, 136, 8))
+def test_append_of_blocks_of_every_length(dh, dtype, fmt):
+    """A block's largest number, an infinity or a NaN in each unit of eight channels in turn: all codes of the block go by it, also where the last
+    block of a head has one, two or three units."""
+    units, heads = dh // 8, 5
+    x = torch.randn(4 * units, heads, dh, generator=torch.Generator().manual_seed(dh))
+    for u in range(units):
+        x[u, :, 8 * u + u % 8] = -300.0
+        x[units + u, ::2, 8 * u + 7 - u % 8] = 2.0 ** 40
+        x[2 * units + u, u % heads, 8 * u + 3] = math.inf
+        x[3 * units + u, u % heads, 8 * u + 5] = math.nan
+    x = x.flatten(1).to(dtype)
+    k, v = x.cuda(), x.flip(0).contiguous().cuda()
+    n = len(x)
+    pages = M.make_pages(fmt, heads, dh, 16, [(n + 15) // 16], fill=0x5b)
+    pf_op_kv_append_mx(pages, k, v, cu([n]), ints(0))
+    check_written(pages, "k", 0, 0, k, dh)
+    check_written(pages, "v", 0, 0, v, dh)
+
+
+@pytest.mark.parametrize("fmt", M.FORMATS)
 def test_every_bf16_value_is_coded_and_read_back(fmt):
     """All finite bf16 numbers, alone in their blocks and beside a large one."""
     x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(BF16)
