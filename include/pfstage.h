@@ -598,7 +598,9 @@ pf_status pf_op_kv_read_mx(int dtype, const pf_kv_mx_pages *pages, const int32_t
                            int64_t ldk, void *v_out, int64_t ldv, void *stream);
 
 /*
- * pf_op_attention_paged over such pages, for rows of either type; the result is that over pages of dtype that hold the decoded rows.
+ * pf_op_attention_paged over such pages, for rows of either type; the result is that over pages of dtype that hold the decoded rows: bit for
+ * bit where pf_attention_mx_kernel_name and pf_attention_rows_kernel_name name the same kernel and chunks, else but for rounding.  Scores and softmax are
+ * held in 32 bits; bf16 rows weigh V with weights rounded to bf16, as in pf_op_attention_paged.
  * Slots in [0, kv_len[s]) that nothing was written to may hold anything as long as the causal mask hides them.
  * ws: pf_op_attention_mx_ws_bytes(.., max_kv = max_pages * page_size) bytes.
  */

@@ -1,9 +1,10 @@
 // Attention of packed rows over pages of 8- or 4-bit numbers: the kernels of attn_rows.h with a loader that brings codes from memory and
 // writes what they stand for to LDS, in the type of the rows.
 //
-// Every value that the pages can hold is a number of both types, so from the LDS on nothing differs from pages of rows, and these
-// kernels' results are bit for bit those over pages that hold the decoded rows.  A tile needs half or a quarter of the bytes from memory, and a
-// conversion instruction for two channels on its way to LDS.
+// Every value that the pages can hold is a number of both types, so from the LDS on nothing differs from pages of rows, and the tile, key and
+// wide kernels' results are bit for bit those over pages that hold the decoded rows.  A tile needs half or a quarter of the bytes from memory, and a
+// conversion instruction for two channels on its way to LDS.  The few kernel below has tiles, chunks and an order of sums of its own: its results are the
+// same but for rounding.
 #include "attn_rows.h"
 #include "mx.h"
 

@@ -1,4 +1,5 @@
 """The operators around a cache in 8 or 4 bits against their plain 64-bit forms (tests/mx_ref.py)."""
+import ctypes as C
 import math
 
 import pytest
@@ -6,7 +7,7 @@ import torch
 
 import mx_ref as M
 import requests_ref as R
-from paper_2405_14430_amd import (KvMxPages, KvPages, PfError, make_norm, make_rope, pf_op_attention_mx, pf_op_attention_paged,
+from paper_2405_14430_amd import (KvMxPages, KvPages, PfError, load_library, make_norm, make_rope, pf_op_attention_mx, pf_op_attention_paged,
                                   pf_op_kv_append_mx, pf_op_kv_read_mx, pf_op_qk_norm_rope)
 from test_gpu_requests import BF16, CANARY, F32, PAGED, ROPES, cu, dev, ints, make, rope_args, wide
 
@@ -349,3 +350,47 @@ def test_attention_over_anything_that_the_mask_hides(dh, heads, kv_heads, new, f
         assert ok.any() and not ok.all()
         assert torch.equal(a[b.isinf()], b[b.isinf()])
         assert ((a[ok] - b[ok]).abs() <= rel * (b[ok].abs() + 1)).all()
+
+
+SAME = [
+    # type, head_dim, heads, kv_heads, page, new lengths, first slots, causal, kernel, in chunks
+    (BF16, 64, 4, 4, 16, [100, 3, 0, 41], [2000, 0, 5, 17], True, "attn_rows_kernel<bf16,64,1,4>", True),
+    (BF16, 128, 8, 2, 64, [9, 60], [300, 70], True, "attn_rows_kernel<bf16,128,1,4>", False),
+    (BF16, 72, 16, 2, 16, [40], [0], True, "attn_rows_kernel<bf16,96,1,4>", False),
+    (BF16, 56, 4, 4, 32, [800, 330, 0], [3300, 11, 5], False, "attn_rows_kernel<bf16,64,4,1>", True),
+    (BF16, 64, 16, 16, 32, [2500, 500, 7], [0, 300, 2], True, "attn_rows_wide_kernel<64,4>", False),
+    (BF16, 72, 32, 4, 16, [777, 240, 13], [100, 0, 330], False, "attn_rows_wide_kernel<96,5>", False),
+    (BF16, 96, 16, 4, 128, [1500, 90], [33, 0], True, "attn_rows_wide_kernel<96,6>", False),
+    (BF16, 128, 14, 2, 64, [700, 77], [1300, 0], True, "attn_rows_wide_kernel<128,8>", True),
+    (F32, 96, 8, 1, 16, [1, 2, 5], [2990, 0, 700], True, "attn_rows_kernel<float,96,1,4>", True),
+    (F32, 64, 4, 4, 32, [90, 3], [0, 77], False, "attn_rows_kernel<float,64,1,4>", False),
+    (F32, 72, 32, 4, 16, [777, 240, 13], [100, 0, 330], True, "attn_rows_kernel<float,96,4,1>", False),
+]
+
+
+@pytest.mark.parametrize("fmt", M.FORMATS)
+@pytest.mark.parametrize("dtype,dh,heads,kv_heads,page,new,first,causal,name,chunks", SAME, ids=lambda v: v if isinstance(v, str) else None)
+def test_kernels_of_pages_of_rows_give_the_same_bits(dtype, dh, heads, kv_heads, page, new, first, causal, name, chunks, fmt):
+    """The tile, key and wide kernels over pages of few bits: bit for bit what they give over pages of rows that hold the decoded values, with pages
+    missing, and bytes of all kinds where the causal mask hides them from some rows."""
+    kv = [f + n for f, n in zip(first, new)]
+    pages = M.make_pages(fmt, kv_heads, dh, page, [(n + page - 1) // page for n in kv])
+    if kv[0] > 4 * page:
+        pages.table[0, 1] = -1
+    g = torch.Generator().manual_seed(3)
+    for t in torch.randint(first[0], kv[0], (9,), generator=g).tolist() if causal else ():
+        pg, at = int(pages.table[0, t // page]), t % page
+        if pg >= 0:
+            pages.v_scale[pg, :, at, 0] = 254 + t % 2
+    sizes = (sum(new), len(new), heads, kv_heads, dh, pages.max_pages * page)
+    lib, code, n = load_library(), int(dtype == BF16), [C.c_int(), C.c_int()]
+    names = [lib.pf_attention_mx_kernel_name(code, int(fmt == "e2m1"), *sizes, C.byref(n[0])),
+             lib.pf_attention_rows_kernel_name(code, *sizes, C.byref(n[1]))]
+    assert names[0] == names[1] == name.encode() and n[0].value == n[1].value and (n[0].value > 1) == chunks, (names, n)
+    q = wide(sum(new), heads * dh, dtype, 4)
+    args = (cu(new), ints(*first), ints(*kv))
+    got = pf_op_attention_mx(q, pages, *args, causal=causal, want_lse=True)
+    want = pf_op_attention_paged(q, decoded_pages(pages, dtype), *args, causal=causal, want_lse=True)
+    for a, b in zip(got, want):
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a[~a.isnan()], b[~b.isnan()])
+        assert not b.isnan().all()
