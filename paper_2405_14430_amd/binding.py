@@ -983,9 +983,9 @@ def pf_op_kv_append_mx(pages, k, v, cu, first, k_norm=None, rope=None, pos=None,
     return q_out
 
 
-def pf_op_kv_read_mx(pages, cu, first, tokens, dtype, k_out=None, v_out=None):
+def pf_op_kv_read_mx(pages, cu, first, tokens, dtype, k_out=None, v_out=None, want_k=True, want_v=True):
     """Rows [tokens, kv_heads * head_dim] of `dtype` from pages of few bits: row cu[s] + i is slot first[s] + i of sequence s, zeros
-    where there is no page.  Returns (k, v); rows of no sequence are not written."""
+    where there is no page.  Returns (k, v), None for a side that is not wanted; rows of no sequence are not written."""
     dev, index = pages.device, pages.index
     if dtype not in _DT:
         raise PfError(-4, f"dtype {dtype}")
@@ -995,16 +995,23 @@ def pf_op_kv_read_mx(pages, cu, first, tokens, dtype, k_out=None, v_out=None):
     if not 0 <= tokens < 2 ** 31:
         _too_large("tokens", tokens)
     shape = (tokens, pages.kv_heads * pages.head_dim)
-    if k_out is None:
-        k_out, ldk = torch.empty(shape, dtype=dtype, device=dev), shape[1]
+    ldk = ldv = shape[1]
+    if not want_k:
+        if k_out is not None:
+            raise PfError(-1, "k_out without k")
+    elif k_out is None:
+        k_out = torch.empty(shape, dtype=dtype, device=dev)
     else:
         ldk = _ld(_out("k_out", k_out, shape, dtype, dev))
-    if v_out is None:
-        v_out, ldv = torch.empty(shape, dtype=dtype, device=dev), shape[1]
+    if not want_v:
+        if v_out is not None:
+            raise PfError(-1, "v_out without v")
+    elif v_out is None:
+        v_out = torch.empty(shape, dtype=dtype, device=dev)
     else:
         ldv = _ld(_out("v_out", v_out, shape, dtype, dev))
     _launch(index, (_lib or load_library()).pf_op_kv_read_mx, _DT[dtype], pages.ref, cu.data_ptr(), first.data_ptr(), tokens,
-            k_out.data_ptr(), ldk, v_out.data_ptr(), ldv)
+            None if k_out is None else k_out.data_ptr(), ldk, None if v_out is None else v_out.data_ptr(), ldv)
     return k_out, v_out
 
 

@@ -249,6 +249,34 @@ def test_rows_without_a_place(fmt):
         assert (back[:4] == 0).all() and (back[20:] == 0).all()
 
 
+@pytest.mark.parametrize("fmt", M.FORMATS)
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("tokens,kv_heads,dh", [(1, 1, 8), (37, 3, 72), (1, 40, 128), (1500, 8, 64), (2047, 1, 40), (2048, 5, 128), (3001, 40, 72),
+                                                (5003, 1, 64)])
+def test_read_of_one_side(tokens, kv_heads, dh, dtype, fmt):
+    """k alone and v alone: what the read of both gives, and nothing where no row belongs to a sequence."""
+    page = 64
+    pages = M.make_pages(fmt, kv_heads, dh, page, [(tokens + page - 1) // page + 1], spare=1)
+    if tokens > page:
+        pages.table[0, 1] = -1
+    where = (cu([tokens], 2), ints(5), tokens + 5, dtype)
+    new = lambda: torch.full((tokens + 5, kv_heads * dh), CANARY, dtype=dtype, device="cuda")
+    k, v = pf_op_kv_read_mx(pages, *where, k_out=new(), v_out=new())
+    for s, which in ((k, "k"), (v, "v")):
+        assert torch.equal(R.d64(s[2:2 + min(tokens, 50)]), M.slot_rows(pages, which, 0, min(tokens, 50) + 5)[0][5:])
+    alone, none = pf_op_kv_read_mx(pages, *where, k_out=new(), want_v=False)
+    assert none is None and torch.equal(alone, k)
+    none, alone = pf_op_kv_read_mx(pages, *where, v_out=new(), want_k=False)
+    assert none is None and torch.equal(alone, v)
+    assert not torch.equal(k, v) and all((x[:2] == CANARY).all() and (x[-3:] == CANARY).all() for x in (k, v))
+    alone, none = pf_op_kv_read_mx(pages, *where, want_v=False)
+    assert none is None and torch.equal(alone[2:-3], k[2:-3])
+    for wrong in (dict(want_k=False, want_v=False), dict(want_k=False, k_out=new()), dict(want_v=False, v_out=new())):
+        with pytest.raises(PfError) as e:
+            pf_op_kv_read_mx(pages, *where, **wrong)
+        assert e.value.status == -1
+
+
 # ---- attention ---------------------------------------------------------------------------------------------------------------
 MANY = [
     # as PAGED, with rows for the kernels of many rows
