@@ -592,7 +592,8 @@ pf_status pf_op_kv_append_mx(int dtype, const pf_kv_mx_pages *pages, const void 
 /*
  * The way back: row cu[s] + i of k_out and v_out (dtype [tokens, kv_heads * head_dim], either NULL) receives slot first[s] + i of
  * sequence s, exactly.  Slots without a page, past max_pages * page_size and negative ones read as zeros; rows of no sequence are
- * left as they are.  Exponent bytes above those that append writes give what they stand for, infinities included.
+ * left as they are.  Exponent bytes that append does not write give what they stand for, too: infinities above, and below numbers that are not
+ * normal, the nearest where dtype has none.
  */
 pf_status pf_op_kv_read_mx(int dtype, const pf_kv_mx_pages *pages, const int32_t *cu, const int32_t *first, int tokens, void *k_out,
                            int64_t ldk, void *v_out, int64_t ldv, void *stream);

@@ -277,6 +277,24 @@ def test_read_of_one_side(tokens, kv_heads, dh, dtype, fmt):
         assert e.value.status == -1
 
 
+@pytest.mark.parametrize("fmt", M.FORMATS)
+def test_read_of_every_code_under_every_power(fmt):
+    """All bytes of codes under all bytes of exponents, also those that append never writes: infinities past the largest number, numbers below the
+    smallest normal one, NaN."""
+    codes = torch.arange(256).view(-1, 1, 64) if fmt == "e4m3" else (torch.arange(64) % 16).view(1, 1, 64)
+    rows = len(codes) * 256
+    code = M.packed(codes, fmt, 64).repeat(256, 1, 1)
+    exp = torch.arange(256).to(torch.uint8).repeat_interleave(len(codes)).view(-1, 1, 1).repeat(1, 1, 2)
+    pool = lambda t: t.unflatten(0, (-1, 16)).transpose(1, 2).contiguous().cuda()
+    pages = KvMxPages(fmt, pool(code), pool(code), pool(exp), pool(exp), torch.arange(rows // 16).int().cuda()[None], 64)
+    want = M.decode(code, exp, fmt, 64).flatten(1)
+    for dtype in R.DTYPES:
+        for got in pf_op_kv_read_mx(pages, cu([rows]), ints(0), rows, dtype):
+            got, near = R.d64(got), R.d64(want.to(dtype))
+            assert torch.equal(got.isnan(), near.isnan()) and torch.equal(got.nan_to_num(7.5), near.nan_to_num(7.5))
+            assert torch.equal(torch.signbit(got)[~got.isnan()], torch.signbit(near)[~got.isnan()])
+
+
 # ---- attention ---------------------------------------------------------------------------------------------------------------
 MANY = [
     # as PAGED, with rows for the kernels of many rows
