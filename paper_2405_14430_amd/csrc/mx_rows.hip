@@ -44,7 +44,7 @@ struct HeadsK {
   Pages pages;
   const int32_t *cu, *first;
   int n_seqs, row_bytes, blocks;
-  int tokens, head_dim, once;
+  int tokens, head_dim;
   int t0;                // first token of the launch
 };
 
@@ -61,12 +61,9 @@ template <typename T>
 struct Unit {
   static constexpr int N = V * (int)sizeof(T) / 16;
   u32x4 w[N];
-  __device__ __forceinline__ void load(const T *p, bool once) {
+  __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const u32x4 *from = reinterpret_cast<const u32x4 *>(p) + i;
-      w[i] = once ? __builtin_nontemporal_load(from) : *from;
-    }
+    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const u32x4 *>(p)[i];
   }
   __device__ __forceinline__ void store(T *p) const {
 #pragma unroll
@@ -272,14 +269,14 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
     for (int j = 0; j < DEPTH; ++j, i += stride) {
       if (i >= steps) break;
       const Where at = where(i);
-      if (lane < at.lanes) raw[j].load(pick(at.side == 0, q, pick(at.side == 1, k, v)) + at.h0 * dh + lane * V, p.once);
+      if (lane < at.lanes) raw[j].load(pick(at.side == 0, q, pick(at.side == 1, k, v)) + at.h0 * dh + lane * V);
     }
   };
   load(blockIdx.y);
   Unit<T> weight[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    if (p.side[i].weight) weight[i].load((const T *)p.side[i].weight + c0, false);
+    if (p.side[i].weight) weight[i].load((const T *)p.side[i].weight + c0);
 
   // the token's cosines and sines, a lane to a pair, and from there to the lanes of its channels
   float cs[V], sn[V];
@@ -369,7 +366,7 @@ __global__ __launch_bounds__(64 * kWaves) void head_rows_kernel(TurnK rk, HeadsK
           for (int c = 0; c < V; ++c) x[c] *= r;
           if (b) {
             Unit<T> bias;
-            bias.load(b + c0, false);
+            bias.load(b + c0);
 #pragma unroll
             for (int c = 0; c < V; ++c) x[c] += bias[c];
           }
@@ -588,7 +585,6 @@ hipError_t launch_head_rows(const HeadRows &args, const pf_rope *rope, hipStream
   p.exp_stride[0] = args.mx.k_scale_stride, p.exp_stride[1] = args.mx.v_scale_stride;
   p.pos = args.pos, p.pages = args.pages, p.cu = args.cu, p.first = args.first, p.n_seqs = args.n_seqs;
   p.row_bytes = args.mx.row_bytes, p.blocks = args.mx.blocks, p.tokens = args.tokens, p.head_dim = args.head_dim;
-  p.once = (int64_t)args.tokens * 2 * (args.n_heads + 2 * args.kv_heads) * args.head_dim * (int64_t)dt_size(args.dt) > kReadOnceBytes;
   const int format = append ? args.mx.format : -1;
   return args.dt == DT_BF16 ? launch_format<bf16_t>(rk, p, format, half, align, s) : launch_format<float>(rk, p, format, half, align, s);
 }
