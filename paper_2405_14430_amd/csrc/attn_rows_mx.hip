@@ -564,7 +564,13 @@ RowsPlan mx_attention_plan(int dt, int format, int total_q, int n_seqs, int n_he
   const int64_t w = workgroups(total_q, n_heads / kv_heads, n_seqs, kv_heads, 16);
   int64_t c = w >= 256 ? 1024 : std::min(std::max(w * max_kv / 2048, (int64_t)256), (int64_t)1024);
   if (max_kv <= (w >= 256 ? 2560 : 512)) c = max_kv;
-  c = (std::max(c, (max_kv + kMaxChunks - 1) / kMaxChunks) + 127) / 128 * 128;
+  // The host knows how long a cache could be, not how long it is: chunks that are not there cost the join a read each, and all of them their place in the
+  // workspace.  With at most 65536 items (partial results of 16 rows) a wide table costs neither: 1024 tokens over 1000 / 4000 keys each in one for 131072 keys,
+  // 8 bits, take 452 / 1441 us and 136 MB of workspace, without the bound 882 / 2214 and 2.2 GB.  Less is better for caches of one length (8192 items: 384 /
+  // 1359) and worse where a few are long (24 heads of 64, 64 tokens over up to 16384 keys in the same table: 141 us, 32768 items 193, 8192 items 240).
+  const int64_t most = std::max(65536 / w, (int64_t)1);
+  c = std::max(c, std::max((max_kv + most - 1) / most, (max_kv + kMaxChunks - 1) / kMaxChunks));
+  c = (c + 127) / 128 * 128;
   RowsPlan p{ROWS_FEW, (int)((max_kv + c - 1) / c), (int)c, 0};
   if (p.splits > 1) p.ws_bytes = (size_t)p.splits * total_q * n_heads * (head_dim + 2) * sizeof(float);
   return p;

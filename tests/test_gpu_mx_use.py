@@ -168,6 +168,26 @@ def test_attention_of_many_short_sequences(seqs, heads, kv_heads, dh, longest, d
 
 
 @pytest.mark.parametrize("fmt", M.FORMATS)
+@pytest.mark.parametrize("seqs,heads,kv_heads,dh", [(8192, 32, 32, 64), (8192, 64, 16, 64), (9001, 17, 17, 8)])
+def test_many_tokens_over_a_wide_table(seqs, heads, kv_heads, dh, fmt):
+    """Thousands of single tokens with room for 131072 keys each, of which few are there: taken as over pages of rows."""
+    page, pool = 1024, 5
+    pages = M.make_pages(fmt, kv_heads, dh, page, [pool], spare=0)
+    kv = torch.arange(seqs) * 7 % 61
+    pages = KvMxPages(fmt, pages.k, pages.v, pages.k_scale, pages.v_scale, (torch.arange(seqs * 128) % (pool + 1)).int().view(seqs, 128).cuda(), dh)
+    q = dev(seqs, heads * dh, seed=3)
+    lens, kv_len = torch.arange(seqs + 1).int().cuda(), kv.int().cuda()
+    got = pf_op_attention_mx(q, pages, lens, kv_len - 1, kv_len)
+    assert (got[kv.cuda() == 0] == 0).all()
+    for s in (1, 2, 8, 700, 4095, 4096, seqs - 2, seqs - 1):
+        n = int(kv[s])
+        k, have = M.slot_rows(pages, "k", s, n)
+        v, _ = M.slot_rows(pages, "v", s, n)
+        want, _, b16, _, _ = R.attention(q[s:s + 1], k, v, dh, torch.tensor([n]), present=have)
+        R.check(got[s:s + 1], want, R.stored(b16, want, BF16), s)
+
+
+@pytest.mark.parametrize("fmt", M.FORMATS)
 @pytest.mark.parametrize("dtype", R.DTYPES)
 @pytest.mark.parametrize("rows", [2, 40, 700])
 def test_results_do_not_change_from_call_to_call(rows, dtype, fmt):

@@ -158,3 +158,19 @@ def test_binding_refuses_host_tensors_and_wrong_formats(lib):
     with pytest.raises(B.PfError) as e:
         B.pf_op_qk_norm_rope(None, None, 64)
     assert e.value.status == NULL
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_workspace_of_tokens_is_bounded_whatever_the_table_holds(lib, fmt):
+    """Partial results of at most 65536 tiles of 16 rows: a table with room for long caches costs no more than that, and none where there are more tiles."""
+    n = C.c_int()
+    for heads, kv_heads, dh in ((32, 8, 128), (24, 24, 64), (16, 1, 72), (128, 8, 128)):
+        for tokens in (1, 5, 64, 256, 1024, 8192, 100000):
+            for keys in (16, 1000, 4096, 16384, 131072, 1 << 20, (1 << 31) - 4096):
+                sizes = (1, fmt, tokens, tokens, heads, kv_heads, dh, keys)
+                need = lib.pf_op_attention_mx_ws_bytes(*sizes)
+                name = lib.pf_attention_mx_kernel_name(*sizes, C.byref(n))
+                assert b"few" in name and 1 <= n.value <= 256, sizes
+                assert need == (0 if n.value == 1 else n.value * tokens * heads * (dh + 2) * 4), sizes
+                assert need <= 65536 * 16 * (dh + 2) * 4 and n.value <= max(65536 // (tokens * kv_heads), 1), sizes
+    assert lib.pf_op_attention_mx_ws_bytes(1, fmt, 8192, 8192, 32, 8, 128, 131072) == 0
