@@ -525,7 +525,7 @@ hipError_t launch_few(const RowsAttn &a, hipStream_t s) {
   if (hipError_t e = allow_dynamic_lds<&attn_rows_few_kernel<DHP, SRC, CAUSAL>, C::SMEM>(); e != hipSuccess) return e;
   RowsKernelArgs p{a, a.n_heads / a.kv_heads, 0, a.scale * kLog2e};
   // so many workgroups as are resident at a time, or as there can be items
-  p.most_items = (int)(((int64_t)a.total_q * p.group / C::ROWS + a.n_seqs) * a.splits);   // less than 2^24, looked at by the caller
+  p.most_items = (int)(((int64_t)a.total_q * p.group / C::ROWS + a.n_seqs) * a.splits);   // less than 2^25 by the caller's limit, in chunks 2^17 by the plan's
   const int resident = 256 * few_workgroups_of(DHP);
   p.slots = std::min(p.most_items, std::max(resident / a.kv_heads, 1));
   attn_rows_few_kernel<DHP, SRC, CAUSAL><<<dim3((unsigned)(p.slots * a.kv_heads)), 256, C::SMEM, s>>>(p);

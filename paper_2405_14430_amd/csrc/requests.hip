@@ -232,8 +232,8 @@ static pf_status rows_attention(RowsAttn &a, int64_t max_kv, void *ws, size_t ws
   if (p.ws_bytes && (!ws || ws_bytes < p.ws_bytes || !aligned(ws, 16)))
     return refuse(PF_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes is needed, %zu given", who, p.ws_bytes, ws ? ws_bytes : (size_t)0);
   a.ws = (float *)ws;
-  // a launch has less than 2^32 threads
-  if (((int64_t)a.total_q * (a.n_heads / a.kv_heads) / (p.shape == ROWS_FEW ? 16 : 32) + a.n_seqs) * a.kv_heads * p.splits >= (1 << 24))
+  // A launch has less than 2^32 threads.  The few kernel's is bounded by what is resident; it takes what pages of rows take without chunks.
+  if (((int64_t)a.total_q * (a.n_heads / a.kv_heads) / 32 + a.n_seqs) * a.kv_heads * (p.shape == ROWS_FEW ? 1 : p.splits) >= (1 << 24))
     return refuse(PF_ERR_SHAPE, "%s: %d rows of %d heads in %d sequences are too many for one launch", who, a.total_q, a.n_heads, a.n_seqs);
   a.shape = p.shape;
   a.splits = p.splits;

@@ -188,6 +188,22 @@ def test_many_tokens_over_a_wide_table(seqs, heads, kv_heads, dh, fmt):
 
 
 @pytest.mark.parametrize("fmt", M.FORMATS)
+def test_as_many_sequences_as_over_pages_of_rows(fmt):
+    """2^20 tokens of 16 query heads to a key head: bit for bit what calls of 4096 of them give."""
+    part, times, heads, kv_heads, dh, page, pool = 4096, 256, 128, 8, 8, 16, 7
+    small = M.make_pages(fmt, kv_heads, dh, page, [pool], spare=0)
+    i = torch.arange(part * times, device="cuda") % part
+    table, kv = (i % (pool + 1)).int()[:, None], (i % 17).int()
+    q = dev(part, heads * dh, seed=3)
+
+    def run(q, n):
+        pages = KvMxPages(fmt, small.k, small.v, small.k_scale, small.v_scale, table[:n], dh)
+        return pf_op_attention_mx(q, pages, torch.arange(n + 1).int().cuda(), kv[:n] - 1, kv[:n])
+    want, got = run(q, part), run(q.repeat(times, 1), part * times)
+    assert torch.equal(got.view(times, part, -1), want.expand(times, -1, -1)) and want.isfinite().all() and (want != 0).any()
+
+
+@pytest.mark.parametrize("fmt", M.FORMATS)
 @pytest.mark.parametrize("dtype", R.DTYPES)
 @pytest.mark.parametrize("rows", [2, 40, 700])
 def test_results_do_not_change_from_call_to_call(rows, dtype, fmt):
