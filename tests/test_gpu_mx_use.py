@@ -286,3 +286,40 @@ def test_large_calls_equal_their_parts(n, heads, kv_heads, dh, page, dtype, fmt)
     for p in parts:
         some = pf_op_kv_read_mx(caches[0], cu([p.stop - p.start]), ints(p.start), p.stop - p.start, dtype)
         assert all(torch.equal(a, b[p]) for a, b in zip(some, back))
+
+
+@pytest.mark.parametrize("fmt", M.FORMATS)
+@pytest.mark.parametrize("dtype", R.DTYPES)
+@pytest.mark.parametrize("dh", range(8, 136, 8))
+def test_a_layer_of_every_head_size(dh, dtype, fmt):
+    """Normed and turned rows into the pages and attention over these, tokens and prompts: every head size, rotation of a part of the channels and of
+    axes of odd halves, either pair layout."""
+    heads, kv_heads, page = 6, 3, 16
+    layout = "half" if dh % 16 else "interleaved"
+    axes = [(dh,), (dh // 2 - dh // 2 % 2, 2), (max(dh // 4 * 2 - 2, 2),)][dh // 8 % 3]
+    args = dict(axes=axes, head_dim=dh, layout=layout, theta=1e4)
+    rope = make_rope(axes, layout=layout, theta=1e4)
+    w = (1 + 0.3 * dev(dh, dtype=F32, seed=7)).to(dtype)
+    norm, plain = make_norm("rms", w, eps=1e-5), ("rms", w, None, 1e-5)
+    for new, first in (([1, 2, 1], [40, 0, 129]), ([70, 1], [9, 200])):
+        n, kv = sum(new), [a + b for a, b in zip(new, first)]
+        pages = M.make_pages(fmt, kv_heads, dh, page, [(m + page - 1) // page for m in kv], seed=1)
+        q, k, v = (dev(n, h * dh, dtype=dtype, seed=s) for s, h in enumerate((heads, kv_heads, kv_heads)))
+        pos = torch.randint(-300, 300, (n, len(axes)), generator=torch.Generator().manual_seed(2), dtype=torch.int32).cuda()
+        k_turned = pf_op_qk_norm_rope(None, k, dh, k_norm=norm, rope=rope, pos=pos)[1]
+        want, bound = M.turn(k, dh, plain, pos, args)
+        R.check(k_turned, want, R.stored(bound, want, dtype), "k")
+        q = pf_op_kv_append_mx(pages, k, v, cu(new), ints(*first), k_norm=norm, rope=rope, pos=pos, q=q, q_norm=norm, q_out=q)
+        want, bound = M.turn(dev(n, heads * dh, dtype=dtype, seed=0), dh, plain, pos, args)
+        R.check(q, want, R.stored(bound, want, dtype), "q")
+        got = pf_op_attention_mx(q, pages, cu(new), ints(*first), ints(*kv))
+        at = 0
+        for s, m in enumerate(new):
+            rows = {}
+            for which, src in (("k", k_turned), ("v", v)):
+                rows[which] = M.slot_rows(pages, which, s, kv[s])[0]
+                codes, exps = M.encode(R.d64(src[at:at + m]).unflatten(1, (-1, dh)), fmt)
+                assert torch.equal(rows[which][first[s]:], M.decode(M.packed(codes, fmt, dh), exps, fmt, dh).flatten(1)), (which, s)
+            want, _, b16, b32, _ = R.attention(q[at:at + m], rows["k"], rows["v"], dh, torch.arange(first[s], kv[s]) + 1)
+            R.check(got[at:at + m], want, R.stored(b16 if dtype == BF16 else b32, want, dtype), s)
+            at += m
