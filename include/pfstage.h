@@ -545,7 +545,8 @@ pf_status pf_op_norm_residual(int dtype, const void *y, int64_t ldy, const pf_no
  *   out = turn(norm(x) w + b)      RMS: x / sqrt(mean x^2 + eps), LAYER: the same of x - mean x, over the head's head_dim channels
  * q, q_out dtype [tokens, n_heads * head_dim], k, k_out dtype [tokens, kv_heads * head_dim]; either side may be missing (no heads: its
  * pointers are not used).  q_norm, k_norm: NULL or kind NONE: none; weight and bias dtype [head_dim], either NULL, shared by the heads.
- * rope, pos as in pf_op_rope; rope NULL: no rotation.  Without rounding in between; the output is rounded once.  q_out may be q and
+ * rope, pos as in pf_op_rope; rope NULL: no rotation.  In 32 bits, angles in 64 up to the fraction of a turn, sums of a head's squares among
+ * them: heads whose squares add up past 3.4e38 are out of range.  Without rounding to dtype in between; the output is rounded once.  q_out may be q and
  * k_out k.  head_dim, strides and alignment as in pf_op_rope; weight and bias 16-byte aligned.
  */
 pf_status pf_op_qk_norm_rope(int dtype, const void *q, int64_t ldq, const pf_norm *q_norm, void *q_out, int64_t ldqo, int n_heads,

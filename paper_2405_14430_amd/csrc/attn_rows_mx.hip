@@ -216,14 +216,16 @@ __device__ __forceinline__ float over_groups(float v, F &&op) {
 //   S^T[key][row] = K Q^T    in matrix instructions of 16 keys x 16 rows x 32 channels: a lane's K operand are channels of one key, which it
 //                            loads and decodes itself.  Channel order is free as long as Q has the same: where a row is a multiple of 64
 //                            channels the four lanes of a key hold a quarter of it each, one after the other, so that they load whole units.
-//   O^T[c][row] += V^T P^T   V through LDS, decoded on its way there and read transposed; P^T are the scores' accumulators as they are.
+//   O^T[c][row] += V^T P^T   V through LDS, decoded on its way there and read transposed; P^T are the scores' accumulators as they are, the weights
+//                            rounded to bf16 for the matrix units (half a step of 2^-8 each, as in the kernels of attn_rows.h); their sum is of 32 bits.
 // Against 32 rows it has half the accumulators, half the exponentials per key and, with K out of LDS, half the LDS: three or four
 // workgroups fit a CU instead of two.  As in the key kernel every wave walks a quarter of the workgroup's keys in tiles of its own, and the
 // loads of the next tile run meanwhile.
 //   64 tokens over 190817 keys in all, 8 heads of 128, in a graph over three such caches, join included: e4m3 404 MB in 104 us against 120 in the key
 //   kernel (alone, some of the keys still in the Infinity Cache, 83: 4.9 TB/s), e2m1 209 MB in 61 against 110.  Heads of 64: 54 - 59 and 43 us against
 //   74 and 70, of 72 (16 of them) 165 and 128 against 178 and 138.
-// In 8 bits it is bound by memory.  In 4 bits by latency: 2 to 3 waves to a SIMD, its vector unit busy for a third of the time.
+// In 8 bits it is bound by memory.  In 4 bits by latency: 2 to 3 waves to a SIMD, its vector unit busy for a third of the time.  Head sizes of 72 to 96 load
+// K by 8 or 4 bytes, with an exponent for each, and two workgroups fit a CU: 2.7 and 1.8 TB/s at 72, 3.3 and 2.3 at 96.
 constexpr int FEW_ROWS = 16;
 constexpr int few_workgroups_of(int dhp) { return dhp == 64 ? 4 : dhp == 96 ? 2 : 3; }   // on a CU, by their registers
 template <int DHP>
@@ -553,7 +555,8 @@ RowsPlan mx_attention_plan(int dt, int format, int total_q, int n_seqs, int n_he
   // Where a sequence has more rows than a tile of the few kernel its keys are read again: against the key kernel's tiles of 32 rows that is dearer in 8
   // bits (16 sequences of 20 rows over 8192 keys of 8 heads of 128: 121 us and 84) and not in 4 (70 and 71; of 32 rows 65 and 89).  In 8 bits one long
   // sequence among short ones costs, too (63 of 4 rows and one of 400: 306 us and 250, in 4 bits 173 and 205).  The totals do not show it; they are
-  // taken for sequences of as many tokens each where they could be (16 of 16 rows: 76 and 84), and for such a mixture else.
+  // taken for sequences of as many tokens each where they could be (16 of 16 rows: 76 and 84), and for such a mixture else.  Where a mixture's total happens to
+  // divide it is taken wrongly (63 of 4 rows and one of 772: 330 us, of 760 in the key kernel 246).
   const bool alike = total_q <= n_seqs || total_q % n_seqs == 0;
   const int64_t rows = (int64_t)total_q * (n_heads / kv_heads), few = format == PF_MX_E2M1 ? 32 : alike ? 16 : 8;
   if (dt != DT_BF16 || rows > n_seqs * few) return rows_attention_plan(dt, total_q, n_seqs, n_heads, kv_heads, head_dim, max_kv);
